@@ -403,6 +403,158 @@ fka_status fka_prefill_paged(const fka_plan *plan, const void *q, const void *k_
                              const int32_t *page_table, const int32_t *suffix_len, float *out, float *out_lse,
                              void *stream);
 
+/* -------------------------------------------------- new tokens: norm, rotation, store */
+
+/*
+ * What a model does between its q/k/v projections and the attention, in one pass: an RMS norm of every
+ * query and key head, the rotation by the token's position, and the store of K and V into their cache rows.
+ * For a head x of d channels at position m, with a norm weight w (a null weight: no norm, y = x):
+ *   y_c = x_c w_c / sqrt(mean(x^2) + eps)
+ *   (z_a, z_b) = (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = m freq[p], for pair p < rotary_dim / 2 of
+ *   channels (a, b) = (p, p + rotary_dim / 2), or (2p, 2p + 1) if interleaved; other channels z = y.
+ * Computed in fp32, the angle reduced in fp64, rounded once to bf16.  V is copied.  Every sequence has n_tokens
+ * tokens: one in a decode step, an instruction's, or (one sequence, suffix_len NULL, cap the prefix buffer's
+ * length) a whole context written as a prefix [Hkv][Lp][d].
+ */
+typedef struct {
+    int32_t n_seqs;      /* N >= 1 */
+    int32_t n_tokens;    /* n >= 1 per sequence; N x n at most 2^25 */
+    int32_t n_q_heads, n_kv_heads;
+    int32_t head_dim;    /* 64 or 128 */
+    int32_t rotary_dim;  /* channels that turn: a multiple of 16 in [0, head_dim]; 0: none */
+    int32_t interleaved; /* which channels form a pair, see above */
+    int32_t max_len;     /* bound on suffix_len[b] + n_tokens (contiguous: at most suffix_cap) */
+    int32_t advance;     /* 1: suffix_len[b] += n_tokens (0: the caller advances it, as fka_prefill asks) */
+    float eps;
+    int64_t q_stride, k_stride, v_stride; /* elements from one token's row to the next, multiples of 8: a projection's
+                                             joint output [tokens][(Hq + 2 Hkv) d] is read where it lies */
+} fka_rotate_desc;
+
+/*
+ *   q, k, v            bf16, token b n + t at + (b n + t) stride: [Hq][d], [Hkv][d], [Hkv][d]
+ *   q_weight, k_weight bf16 [d] or NULL
+ *   freq               fp64 [rotary_dim / 2] (device), radians per position
+ *   positions          int32 [N][n] (device)
+ *   q_out              bf16 [N][n][Hq][d]; may be q itself where q is dense
+ *   suffix_k           bf16 [N][Hkv][suffix_cap][d], rows [suffix_len[b], suffix_len[b] + n) written (suffix_v likewise)
+ *   suffix_len         int32 [N] (device), or NULL: rows from 0
+ *   err                int32 (device) or NULL
+ * A sequence without room (suffix_len[b] negative, or past max_len with the new tokens) keeps its cache and length
+ * and bit 2 is or-ed into *err; its q_out is written.  Errors: FKA_ERR_INVALID_ARG, FKA_ERR_UNSUPPORTED (head_dim,
+ * rotary_dim not a multiple of 16, too many tokens).
+ */
+fka_status fka_rotate_append(const fka_rotate_desc *desc, const void *q, const void *k, const void *v, const void *q_weight,
+                             const void *k_weight, const double *freq, const int32_t *positions, void *q_out, void *suffix_k,
+                             void *suffix_v, int32_t suffix_cap, int32_t *suffix_len, int32_t *err, void *stream);
+
+/* The same into the page pool: suffix position u of sequence b is in page page_table[b][ceil(prefix_len[b] / 16) + u / 16]
+ * (prefix_len int32 [N], device), slot u % 16.  A token whose page id is outside [0, n_pool_pages), or whose index is past
+ * max_pages_per_seq, is not stored (bit 2), and its sequence's length does not advance. */
+fka_status fka_rotate_append_paged(const fka_rotate_desc *desc, const void *q, const void *k, const void *v, const void *q_weight,
+                                   const void *k_weight, const double *freq, const int32_t *positions, void *q_out, void *k_pool,
+                                   void *v_pool, const int32_t *page_table, const int32_t *prefix_len, int32_t max_pages_per_seq,
+                                   int32_t n_pool_pages, int32_t *suffix_len, int32_t *err, void *stream);
+
+/* ---------------------------------------------------------------- 4-bit prefix tiles */
+
+/*
+ * A snapshot's prefix in 4 bits: 17/64 of its bf16 bytes, which are what a decode step's time is.  Values are
+ * e2m1 (sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6); 32 of them share a power-of-two scale 2^E: 32 channels of a key, or 32
+ * consecutive tokens of a value channel.  With amax the largest magnitude of the 32, 2^E is the power of two at or below amax,
+ * over 4, doubled where amax > 7 2^E, E kept in [-125, 125]; each value is rounded to the nearest code (ties to the even one),
+ * at most 6 2^E.  A block that holds an infinity or a NaN becomes all NaN.  Values on normal data come back with 19 dB
+ * signal to noise.
+ * The prefix is cut into tiles of 128 tokens (all KV heads; fka_mx_tile_bytes bytes, 136 d per KV head, in an order of the
+ * library's own), which live in a pool indexed by tile id.  A tile's unused tokens are written as zeros.  fka_pool_*
+ * can count the tiles' references as it does the pages'.
+ */
+
+/* Bytes of one tile of all KV heads; 0 for a head_dim other than 64 and 128. */
+size_t fka_mx_tile_bytes(int32_t n_kv_heads, int32_t head_dim);
+
+/* Pack positions [from, len) of a prefix, from a multiple of 128 (the last tile of a prefix that grows is packed again).
+ *   k_src, v_src  bf16 [Hkv][src_cap][d], position p in row p - from
+ *   tiles         pool of n_pool_tiles tiles, 16-byte aligned
+ *   tile_row      int32 [ceil(len / 128)] (device), the id of the tile of positions 128 i ..; NULL: id i
+ *   err           int32 (device) or NULL: bit 4 for an id outside [0, n_pool_tiles), whose tile is not written */
+fka_status fka_mx_pack(int32_t n_kv_heads, int32_t head_dim, int32_t from, int32_t len, const void *k_src, const void *v_src,
+                       int32_t src_cap, void *tiles, const int32_t *tile_row, int32_t n_pool_tiles, int32_t *err, void *stream);
+
+/* The values of positions [from, len) (any from) back as bf16, exactly; an id outside the pool gives zeros and bit 4. */
+fka_status fka_mx_unpack(int32_t n_kv_heads, int32_t head_dim, int32_t from, int32_t len, const void *tiles,
+                         const int32_t *tile_row, int32_t n_pool_tiles, void *k_dst, void *v_dst, int32_t dst_cap, int32_t *err,
+                         void *stream);
+
+/* Forks whose prefixes are in 4-bit tiles and whose suffixes are contiguous bf16 buffers (Sec. 3.3: the snapshot is
+ * fixed at the fork, so it is packed once and read by every step). */
+typedef struct {
+    int32_t n_seqs;              /* S sequences over all groups, at most 512 */
+    int32_t n_groups;            /* groups, each with one prefix */
+    int32_t max_tiles_per_group; /* columns of tile_table */
+    int32_t n_pool_tiles;        /* tiles in the pool; ids outside [0, n_pool_tiles) are never read */
+    int32_t suffix_cap;          /* rows allocated per (sequence, kv head) in the suffix buffers, >= 1 */
+    int32_t max_suffix_len;      /* upper bound on suffix_len[i] over the plan's lifetime, <= suffix_cap */
+    int32_t blocks;              /* 0 = automatic (those resident at once); else about this many blocks (at most sixteen
+                                    times the resident ones) */
+} fka_mx_desc;
+
+/* Build a plan (device workspace as fka_plan_create_contig).  host_group_start and host_group_prefix_len as in
+ * fka_plan_create_paged.  Only fka_fork_decode_mx, fka_fork_step_mx, fka_append_kv, fka_plan_get_info,
+ * fka_plan_device_error and fka_plan_destroy take it. */
+fka_status fka_plan_create_mx(const fka_heads *heads, const fka_mx_desc *desc, const int32_t *host_group_start,
+                              const int32_t *host_group_prefix_len, fka_plan **out);
+
+/*
+ * One decode step, as fka_fork_decode, over the values that the tiles stand for.
+ *   tiles        the pool
+ *   tile_table   int32 [n_groups][max_tiles_per_group] (device): the tile ids of each group's prefix; NULL: the groups'
+ *                tiles lie one after the other in the pool, those of group 0 from id 0
+ *   others       as in fka_fork_decode, with the sequences of all groups
+ * A tile id outside [0, n_pool_tiles) is not read: its keys count as zeros and flag 4 is raised.  A NaN block of V makes its
+ * channel NaN in every row of the group, one of K the rows themselves.  A group's prefix_len is that of its pack (a tile's unused
+ * tokens have to be the zeros that the pack wrote).
+ */
+fka_status fka_fork_decode_mx(const fka_plan *plan, const void *q, const void *tiles, const int32_t *tile_table,
+                              const void *suffix_k, const void *suffix_v, const int32_t *suffix_len, float *out, float *out_lse,
+                              void *stream);
+
+/* Append and decode, as fka_fork_step. */
+fka_status fka_fork_step_mx(const fka_plan *plan, const void *q, const void *k_new, const void *v_new, const void *tiles,
+                            const int32_t *tile_table, void *suffix_k, void *suffix_v, int32_t *suffix_len, float *out,
+                            float *out_lse, void *stream);
+
+/* ------------------------------------------------------- shortening a prefix by weight */
+
+/*
+ * The attention weight that query rows give each prefix key, summed over the rows and the query heads of a KV head:
+ *   weights[g][j] = decay weights[g][j] + sum_{r, h of g} exp(scale q[r][h] . k[g][j] - lse[r][h])
+ * lse is the rows' log-sum-exp over all their keys (out_lse of a decode or prefill), so a row whose keys are all in the prefix
+ * adds one in all.  A row with lse = -inf adds nothing.  decay = 0 writes without reading.
+ *   n_rows   decode sequences or prompt tokens (an observation window), >= 0
+ *   q        bf16 [n_rows][Hq][d];  lse fp32 [n_rows][Hq]
+ *   k        bf16 [Hkv][k_cap][d], the first len rows read
+ *   weights  fp32 [Hkv][weights_cap], the first len entries updated
+ * The sums' order is fixed: the same call gives the same bits.
+ */
+fka_status fka_key_weights(const fka_heads *heads, int32_t n_rows, int32_t len, const void *q, const float *lse, const void *k,
+                           int32_t k_cap, float *weights, int32_t weights_cap, float decay, void *stream);
+
+/* Device bytes of fka_evict's workspace for up to len positions (0 for sizes that it refuses). */
+size_t fka_evict_bytes(int32_t n_kv_heads, int32_t len);
+
+/*
+ * Keep `keep` of the positions [0, len) of each KV head: the first n_first, the last n_last, and of those between the ones with
+ * the largest weights, equal ones from the lowest position (-0 equals 0; a NaN is above every number).  K, V rows and weights of the kept
+ * positions are copied in order; the next plan's prefix_len is keep (keys carry their rotation, so their positions stay theirs).
+ *   k, v         bf16 [Hkv][kv_cap][d];  weights fp32 [Hkv][weights_cap]
+ *   index        int32 [Hkv][keep]: the kept positions, ascending
+ *   k_out, v_out bf16 [Hkv][keep][d];  weights_out fp32 [Hkv][keep] or NULL; none may overlap an input
+ *   workspace    fka_evict_bytes(Hkv, len) device bytes, used by one call at a time; its contents before and after do not matter
+ */
+fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t keep, int32_t n_first, int32_t n_last,
+                     const void *k, const void *v, int32_t kv_cap, const float *weights, int32_t weights_cap, int32_t *index,
+                     void *k_out, void *v_out, float *weights_out, void *workspace, size_t workspace_bytes, void *stream);
+
 /* -------------------------------------------------------------- stage entry points */
 
 /* The first stage (Sec. 3.3: the prefix is read once for all branches) runs as one kernel

@@ -49,6 +49,11 @@ struct fka_plan {
     int32_t rounds = 1;        // launches n_blocks * rounds blocks
     int32_t n_slots = 0;       // partial-result slots in the workspace
     size_t workspace_bytes = 0;
+    // decode over 4-bit tiles: the blocks' jobs and each output row's merge record, fixed by the plan
+    bool mx = false;
+    int32_t max_tiles = 0, n_pool_tiles = 0;
+    std::vector<fka::MxJob> jobs;
+    std::vector<int32_t> rowrec;
     int device = 0;
     // device memory (one allocation, carved)
     void *mem = nullptr;
@@ -59,6 +64,7 @@ struct fka_plan {
     int32_t *d_lens = nullptr;
     float *part_o = nullptr;
     float *part_lse = nullptr;
+    fka::MxJob *d_jobs = nullptr;
 };
 
 // Page pool: reference count per page id; free ids kept ordered so allocation takes the lowest.
@@ -249,7 +255,8 @@ fka_status finish_plan(fka_plan *p)
         return fail(FKA_ERR_UNSUPPORTED, "partial results of %zu bytes exceed the 2 GiB the merge addresses", b_po);
     const size_t b_pl = up((size_t)p->n_slots * p->slot_rows * sizeof(float));
     const size_t b_zero = b_err + b_rec + b_seq;  // err, records, lengths: zeroed
-    const size_t total = b_units + b_seq + b_zero + b_po + b_pl;
+    const size_t b_jobs = up(p->jobs.size() * sizeof(fka::MxJob));
+    const size_t total = b_units + b_seq + b_zero + b_po + b_pl + b_jobs;
     e = hipMalloc(&p->mem, total);
     if (e != hipSuccess) {
         p->mem = nullptr;
@@ -271,6 +278,8 @@ fka_status finish_plan(fka_plan *p)
     p->part_o = reinterpret_cast<float *>(m);
     m += b_po;
     p->part_lse = reinterpret_cast<float *>(m);
+    m += b_pl;
+    p->d_jobs = reinterpret_cast<fka::MxJob *>(m);
     p->workspace_bytes = total;
     auto put = [&](void *dst, const void *src, size_t bytes, const char *what) -> fka_status {
         if (bytes == 0) return FKA_OK;
@@ -283,7 +292,8 @@ fka_status finish_plan(fka_plan *p)
                   "hipMemcpy(sequence tables)")) != FKA_OK)
         return st;
     if ((e = hipMemset(zero, 0, b_zero)) != hipSuccess) return hip_fail(e, "hipMemset(flags and records)");
-    return FKA_OK;
+    if ((st = put(p->d_jobs, p->jobs.data(), p->jobs.size() * sizeof(fka::MxJob), "hipMemcpy(jobs)")) != FKA_OK) return st;
+    return put(p->d_rowrec, p->rowrec.data(), p->rowrec.size() * sizeof(int32_t), "hipMemcpy(merge records)");
 }
 
 fka_status check_contig(const fka_heads *heads, const fka_contig_desc *desc)
@@ -712,6 +722,253 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
     return ok();
 }
 
+// ---------------------------------------------------------------------------------------
+// The operators around a snapshot's cache.
+
+// Largest device id range of the copies below: a launch's threads stay below 2^32.
+constexpr int32_t kMaxRotateTokens = 1 << 25;
+
+// The jobs of a decode over 4-bit tiles.  A job's unit of work is a prefix tile (17 KiB at d = 128) or a
+// suffix slice of 32 keys (16 KiB); every job gets about the same number, so that the jobs fill the resident
+// blocks once with every suffix at max_suffix_len, and at least one unit for each of a block's four waves.
+fka_status build_mx_jobs(fka_plan *p, int32_t blocks)
+{
+    const int n_groups = p->n_groups;
+    int64_t units = 0;
+    int32_t max_nseq = 1;
+    for (int t = 0; t < n_groups; ++t) {
+        units += ceil_div(p->group_prefix_len[t], fka::kMxTile);
+        max_nseq = std::max(max_nseq, p->group_start[t + 1] - p->group_start[t]);
+    }
+    const int32_t slices = fka::slices_of(p->max_suffix_len);
+    units += (int64_t)p->n_seqs * slices;
+    if (units * p->Hkv > (int64_t)1 << 30)
+        return fail(FKA_ERR_UNSUPPORTED, "prefix and suffixes of %lld tiles are too long", (long long)(units * p->Hkv));
+    p->slot_rows = max_nseq * p->G;
+    p->row_tiles = ceil_div(p->slot_rows, 16);
+    hipError_t e = hipGetDevice(&p->device);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+    int cus = 0;
+    if ((e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, p->device)) != hipSuccess)
+        return hip_fail(e, "hipDeviceGetAttribute");
+    const int per_cu = fka::mx_blocks_per_cu(p->d, p->row_tiles);
+    if (per_cu <= 0) return fail(FKA_ERR_HIP, "occupancy query of the 4-bit decode kernel failed");
+    p->waves = 4;
+    const int64_t resident = (int64_t)cus * per_cu;
+    const int64_t want = blocks > 0 ? std::min<int64_t>(blocks, 16 * resident) : resident;
+    const int64_t per = std::max<int64_t>(p->waves, (units * p->Hkv + want - 1) / want);
+    const int32_t shares = ceil_div(slices, per);  // of every suffix
+    p->rowrec.assign((size_t)p->n_seqs * p->Hq * fka::kRowRec, 0);
+    int64_t slot = 0;
+    int32_t tile0 = 0;
+    std::vector<fka::MxJob> tail;  // the suffixes' jobs, behind the prefixes': short ones fill the end
+    for (int t = 0; t < n_groups; ++t) {
+        const int32_t s0 = p->group_start[t], nseq = p->group_start[t + 1] - s0, lp = p->group_prefix_len[t];
+        const int32_t tiles = ceil_div(lp, fka::kMxTile), parts = ceil_div(tiles, per);
+        for (int32_t g = 0; g < p->Hkv; ++g) {
+            fka::MxJob j{};
+            j.group = t;
+            j.head = g;
+            j.prefix_len = lp;
+            j.tile0 = tile0;
+            for (int32_t i = 0; i < parts; ++i) {
+                j.slot = (int32_t)slot + i;
+                j.seq0 = s0;
+                j.rows = nseq * p->G;
+                j.begin = (int32_t)((int64_t)i * tiles / parts);
+                j.end = (int32_t)((int64_t)(i + 1) * tiles / parts);
+                p->jobs.push_back(j);
+            }
+            j.suffix = 1;
+            for (int32_t s = 0; s < nseq; ++s) {
+                j.seq0 = s0 + s;
+                j.end = shares;
+                for (j.first = 0; j.first < p->G; j.first += 16) {
+                    j.rows = std::min(16, p->G - j.first);
+                    j.row0 = s * p->G + j.first;
+                    for (j.begin = 0; j.begin < shares; ++j.begin) {
+                        j.slot = (int32_t)slot + parts + j.begin;
+                        tail.push_back(j);
+                    }
+                }
+                for (int32_t r = 0; r < p->G; ++r) {
+                    int32_t *rec = &p->rowrec[((size_t)(s0 + s) * p->Hq + (size_t)g * p->G + r) * fka::kRowRec];
+                    rec[0] = (int32_t)(slot * p->slot_rows) + s * p->G + r;
+                    rec[1] = parts + shares;
+                }
+            }
+            slot += parts + shares;
+            // the merge addresses the partials with 32-bit byte offsets
+            if (slot * p->slot_rows * p->d * 4 >= (int64_t)1 << 31)
+                return fail(FKA_ERR_UNSUPPORTED, "partial results exceed the 2 GiB the merge addresses");
+        }
+        tile0 += tiles;
+    }
+    p->jobs.insert(p->jobs.end(), tail.begin(), tail.end());
+    p->n_slots = (int32_t)slot;
+    p->n_items = n_groups * p->Hkv;
+    p->n_blocks = (int32_t)p->jobs.size();
+    return FKA_OK;
+}
+
+fka_status check_mx_call(const fka_plan *p, const void *q, const void *tiles, const int32_t *tile_table, const void *suffix_k,
+                         const void *suffix_v, const int32_t *suffix_len, const float *out, const float *out_lse)
+{
+    REQUIRE(p != nullptr, "plan is null");
+    REQUIRE(p->mx, "plan is not for 4-bit tiles: make it with fka_plan_create_mx");
+    REQUIRE_PTR16(q);
+    if (p->n_pool_tiles > 0) REQUIRE_PTR16(tiles);
+    REQUIRE_OPT4(tile_table);
+    REQUIRE_PTR16(suffix_k);
+    REQUIRE_PTR16(suffix_v);
+    REQUIRE_PTR4(suffix_len);
+    REQUIRE_PTR16(out);
+    REQUIRE_OPT4(out_lse);
+    return FKA_OK;
+}
+
+fka_status run_mx(const fka_plan *p, const void *q, const void *tiles, const int32_t *tile_table, const void *suffix_k,
+                  const void *suffix_v, const int32_t *suffix_len, const fka::MergeArgs &m, hipStream_t s)
+{
+    fka::MxArgs a{};
+    a.jobs = p->d_jobs;
+    a.q = static_cast<const uint16_t *>(q);
+    a.tiles = static_cast<const uint8_t *>(tiles);
+    a.tile_table = tile_table;
+    a.suffix_k = static_cast<const uint16_t *>(suffix_k);
+    a.suffix_v = static_cast<const uint16_t *>(suffix_v);
+    a.suffix_len = suffix_len;
+    a.lens = p->d_lens;
+    a.part_o = p->part_o;
+    a.part_lse = p->part_lse;
+    a.err = p->err;
+    a.max_tiles = p->max_tiles;
+    a.n_pool_tiles = p->n_pool_tiles;
+    a.suffix_cap = p->suffix_cap;
+    a.max_suffix_len = p->max_suffix_len;
+    a.n_seqs = p->n_seqs;
+    a.n_q_heads = p->Hq;
+    a.n_kv_heads = p->Hkv;
+    a.group = p->G;
+    a.group_magic = fka::magic_of((uint32_t)p->G);
+    a.slot_rows = p->slot_rows;
+    a.scale_log2 = p->scale * 1.4426950408889634f;
+    hipError_t e = fka::launch_mx_partials(a, p->n_blocks, p->d, p->row_tiles, s);
+    if (e != hipSuccess) return hip_fail(e, "4-bit decode kernel launch");
+    e = fka::launch_merge(m, p->d, s);
+    if (e != hipSuccess) return hip_fail(e, "merge kernel launch");
+    return ok();
+}
+
+fka_status run_mx_copy(bool pack, int32_t n_kv_heads, int32_t head_dim, int32_t from, int32_t len, int32_t cap, const void *k,
+                       const void *v, void *tiles, const int32_t *tile_row, int32_t n_pool_tiles, int32_t *err, void *stream)
+{
+    REQUIRE(n_kv_heads >= 1 && n_kv_heads <= 65535, "n_kv_heads %d outside [1, 65535]", n_kv_heads);
+    if (head_dim != 64 && head_dim != 128)
+        return fail(FKA_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", head_dim);
+    REQUIRE(len >= 0 && from >= 0 && from <= len, "need 0 <= from <= len (from %d, len %d)", from, len);
+    if (len > kMaxTokens) return fail(FKA_ERR_UNSUPPORTED, "%d tokens are too many (limit %d)", len, kMaxTokens);
+    REQUIRE(!pack || from % fka::kMxTile == 0, "from (%d) must be a multiple of %d: tiles are written whole", from, fka::kMxTile);
+    REQUIRE(cap >= len - from, "cap (%d) is less than len - from (%d)", cap, len - from);
+    REQUIRE(n_pool_tiles >= 0, "n_pool_tiles must be >= 0");
+    REQUIRE(tile_row != nullptr || ceil_div(len, fka::kMxTile) <= n_pool_tiles, "%d tokens need %d tiles, n_pool_tiles is %d", len,
+            ceil_div(len, fka::kMxTile), n_pool_tiles);
+    if (len == from) return ok();
+    REQUIRE_PTR16(k);
+    REQUIRE_PTR16(v);
+    REQUIRE_PTR16(tiles);
+    REQUIRE_OPT4(tile_row);
+    REQUIRE_OPT4(err);
+    fka::MxCopyArgs a{};
+    if (pack) {
+        a.k_src = static_cast<const uint16_t *>(k);
+        a.v_src = static_cast<const uint16_t *>(v);
+    } else {
+        a.k_dst = static_cast<uint16_t *>(const_cast<void *>(k));
+        a.v_dst = static_cast<uint16_t *>(const_cast<void *>(v));
+    }
+    a.tiles = static_cast<uint8_t *>(tiles);
+    a.tile_row = tile_row;
+    a.from = from;
+    a.len = len;
+    a.cap = cap;
+    a.n_kv_heads = n_kv_heads;
+    a.n_pool_tiles = n_pool_tiles;
+    a.err = err;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = pack ? fka::launch_mx_pack(a, head_dim, s) : fka::launch_mx_unpack(a, head_dim, s);
+    if (e != hipSuccess) return hip_fail(e, pack ? "pack kernel launch" : "unpack kernel launch");
+    return ok();
+}
+
+// The checks and arguments that the contiguous and the paged store share.
+fka_status rotate_args(const fka_rotate_desc *desc, const void *q, const void *k, const void *v, const void *q_weight,
+                       const void *k_weight, const double *freq, const int32_t *positions, void *q_out, void *k_dst, void *v_dst,
+                       const int32_t *suffix_len, int32_t *err, fka::RotateArgs &a)
+{
+    REQUIRE(desc != nullptr, "desc is null");
+    REQUIRE(desc->n_seqs >= 1 && desc->n_tokens >= 1, "n_seqs (%d) and n_tokens (%d) must be >= 1", desc->n_seqs, desc->n_tokens);
+    REQUIRE(desc->n_q_heads >= 1 && desc->n_kv_heads >= 1, "head counts must be positive");
+    if (desc->head_dim != 64 && desc->head_dim != 128)
+        return fail(FKA_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", desc->head_dim);
+    if ((int64_t)desc->n_seqs * desc->n_tokens > kMaxRotateTokens)
+        return fail(FKA_ERR_UNSUPPORTED, "%lld tokens exceed the limit of %d", (long long)desc->n_seqs * desc->n_tokens,
+                    kMaxRotateTokens);
+    REQUIRE(desc->rotary_dim >= 0 && desc->rotary_dim <= desc->head_dim, "rotary_dim (%d) must be in [0, head_dim=%d]",
+            desc->rotary_dim, desc->head_dim);
+    if (desc->rotary_dim % 16 != 0)
+        return fail(FKA_ERR_UNSUPPORTED, "rotary_dim %d not supported (a multiple of 16)", desc->rotary_dim);
+    REQUIRE(desc->interleaved == 0 || desc->interleaved == 1, "interleaved must be 0 or 1");
+    REQUIRE(desc->advance == 0 || desc->advance == 1, "advance must be 0 or 1");
+    REQUIRE(std::isfinite(desc->eps) && desc->eps >= 0.f, "eps must be finite and >= 0");
+    REQUIRE(desc->max_len >= 0, "max_len (%d) must be >= 0", desc->max_len);
+    if (desc->max_len > kMaxTokens) return fail(FKA_ERR_UNSUPPORTED, "max_len %d is too long (limit %d)", desc->max_len, kMaxTokens);
+    const int64_t qw = (int64_t)desc->n_q_heads * desc->head_dim, kw = (int64_t)desc->n_kv_heads * desc->head_dim;
+    REQUIRE(desc->q_stride >= qw && desc->k_stride >= kw && desc->v_stride >= kw, "a token stride is shorter than the token's heads");
+    REQUIRE(desc->q_stride % 8 == 0 && desc->k_stride % 8 == 0 && desc->v_stride % 8 == 0,
+            "token strides must be multiples of 8 elements");
+    REQUIRE_PTR16(q);
+    REQUIRE_PTR16(k);
+    REQUIRE_PTR16(v);
+    REQUIRE(aligned16(q_weight) && aligned16(k_weight), "a norm weight is not 16-byte aligned");
+    if (desc->rotary_dim > 0) {
+        REQUIRE(freq != nullptr, "freq is null");
+        REQUIRE((reinterpret_cast<uintptr_t>(freq) & 7u) == 0, "freq is not 8-byte aligned");
+        REQUIRE_PTR4(positions);
+    }
+    REQUIRE_PTR16(q_out);
+    REQUIRE_PTR16(k_dst);
+    REQUIRE_PTR16(v_dst);
+    REQUIRE_OPT4(suffix_len);
+    REQUIRE_OPT4(err);
+    REQUIRE(!desc->advance || suffix_len != nullptr, "advance needs suffix_len");
+    a.q = static_cast<const uint16_t *>(q);
+    a.k = static_cast<const uint16_t *>(k);
+    a.v = static_cast<const uint16_t *>(v);
+    a.q_stride = desc->q_stride;
+    a.k_stride = desc->k_stride;
+    a.v_stride = desc->v_stride;
+    a.q_weight = static_cast<const uint16_t *>(q_weight);
+    a.k_weight = static_cast<const uint16_t *>(k_weight);
+    a.freq = freq;
+    a.positions = positions;
+    a.q_out = static_cast<uint16_t *>(q_out);
+    a.k_dst = static_cast<uint16_t *>(k_dst);
+    a.v_dst = static_cast<uint16_t *>(v_dst);
+    a.suffix_len = const_cast<int32_t *>(suffix_len);  // written only with advance
+    a.n_seqs = desc->n_seqs;
+    a.n_tokens = desc->n_tokens;
+    a.by_tokens = fka::exact_div(desc->n_tokens);
+    a.n_q_heads = desc->n_q_heads;
+    a.n_kv_heads = desc->n_kv_heads;
+    a.rotary_dim = desc->rotary_dim;
+    a.max_len = desc->max_len;
+    a.advance = desc->advance;
+    a.eps = desc->eps;
+    a.err = err;
+    return FKA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -875,6 +1132,7 @@ fka_status fka_plan_slots(const fka_plan *p, const int32_t *host_suffix_len, fka
 {
     REQUIRE(p != nullptr && host_suffix_len != nullptr && n_slots != nullptr, "null argument");
     REQUIRE(!p->prefill_n, "plan is an instruction-prefill plan: its slots follow the cyclic placement");
+    REQUIRE(!p->mx, "plan is for 4-bit tiles: its slots follow its jobs");
     REQUIRE(capacity >= 0 && (capacity == 0 || slots != nullptr), "slots is null");
     const int N = p->n_seqs, Hkv = p->Hkv, NW = p->waves;
     const int32_t NV = p->n_blocks * p->rounds * NW;
@@ -940,6 +1198,7 @@ fka_status fka_fork_decode(const fka_plan *p, const void *q, const void *prefix_
     REQUIRE(p != nullptr, "plan is null");
     REQUIRE(!p->prefill_n, "plan is an instruction-prefill plan: use fka_prefill");
     REQUIRE(!p->paged, "plan is paged: use fka_fork_decode_paged");
+    REQUIRE(!p->mx, "plan is for 4-bit tiles: use fka_fork_decode_mx");
     REQUIRE_PTR16(q);
     if (p->prefix_len > 0) {
         REQUIRE_PTR16(prefix_k);
@@ -1078,6 +1337,7 @@ fka_status fka_partials(const fka_plan *p, const void *q, const void *prefix_k, 
     REQUIRE(p != nullptr, "plan is null");
     REQUIRE(!p->prefill_n, "plan is an instruction-prefill plan: use fka_prefill");
     REQUIRE(!p->paged, "plan is paged: use fka_partials_paged");
+    REQUIRE(!p->mx, "plan is for 4-bit tiles: use fka_fork_decode_mx");
     REQUIRE_PTR16(q);
     if (p->prefix_len > 0) {
         REQUIRE_PTR16(prefix_k);
@@ -1164,6 +1424,7 @@ fka_status fka_fork_step(const fka_plan *p, const void *q, const void *k_new, co
     REQUIRE(p != nullptr, "plan is null");
     REQUIRE(!p->prefill_n, "plan is an instruction-prefill plan: use fka_prefill");
     REQUIRE(!p->paged, "plan is paged: use fka_fork_step_paged");
+    REQUIRE(!p->mx, "plan is for 4-bit tiles: use fka_fork_step_mx");
     REQUIRE_PTR16(q);
     REQUIRE_PTR16(k_new);
     REQUIRE_PTR16(v_new);
@@ -1641,6 +1902,253 @@ fka_status fka_scatter_pages(const void *k_src, const void *v_src, int32_t len, 
     s.err = err;
     hipError_t e = fka::launch_scatter(s, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "scatter kernel launch");
+    return ok();
+}
+
+/* ------------------------------------------------------------------ the operators around a snapshot's cache */
+
+fka_status fka_rotate_append(const fka_rotate_desc *desc, const void *q, const void *k, const void *v, const void *q_weight,
+                             const void *k_weight, const double *freq, const int32_t *positions, void *q_out, void *suffix_k,
+                             void *suffix_v, int32_t suffix_cap, int32_t *suffix_len, int32_t *err, void *stream)
+{
+    fka::RotateArgs a{};
+    fka_status st = rotate_args(desc, q, k, v, q_weight, k_weight, freq, positions, q_out, suffix_k, suffix_v, suffix_len, err, a);
+    if (st != FKA_OK) return st;
+    REQUIRE(desc->max_len <= suffix_cap, "max_len (%d) must be at most suffix_cap (%d)", desc->max_len, suffix_cap);
+    a.suffix_cap = suffix_cap;
+    hipError_t e = fka::launch_rotate(a, desc->head_dim, desc->interleaved != 0, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "rotate kernel launch");
+    return ok();
+}
+
+fka_status fka_rotate_append_paged(const fka_rotate_desc *desc, const void *q, const void *k, const void *v, const void *q_weight,
+                                   const void *k_weight, const double *freq, const int32_t *positions, void *q_out, void *k_pool,
+                                   void *v_pool, const int32_t *page_table, const int32_t *prefix_len, int32_t max_pages_per_seq,
+                                   int32_t n_pool_pages, int32_t *suffix_len, int32_t *err, void *stream)
+{
+    fka::RotateArgs a{};
+    fka_status st = rotate_args(desc, q, k, v, q_weight, k_weight, freq, positions, q_out, k_pool, v_pool, suffix_len, err, a);
+    if (st != FKA_OK) return st;
+    REQUIRE_PTR4(page_table);
+    REQUIRE_PTR4(prefix_len);
+    REQUIRE(max_pages_per_seq >= 1, "max_pages_per_seq must be >= 1");
+    REQUIRE(n_pool_pages >= 0, "n_pool_pages must be >= 0");
+    a.page_table = page_table;
+    a.seq_prefix_len = prefix_len;
+    a.max_pages = max_pages_per_seq;
+    a.n_pool_pages = n_pool_pages;
+    hipError_t e = fka::launch_rotate(a, desc->head_dim, desc->interleaved != 0, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "rotate kernel launch");
+    return ok();
+}
+
+size_t fka_mx_tile_bytes(int32_t n_kv_heads, int32_t head_dim)
+{
+    return n_kv_heads >= 1 && (head_dim == 64 || head_dim == 128) ? (size_t)n_kv_heads * 136 * head_dim : 0;
+}
+
+fka_status fka_mx_pack(int32_t n_kv_heads, int32_t head_dim, int32_t from, int32_t len, const void *k_src, const void *v_src,
+                       int32_t src_cap, void *tiles, const int32_t *tile_row, int32_t n_pool_tiles, int32_t *err, void *stream)
+{
+    return run_mx_copy(true, n_kv_heads, head_dim, from, len, src_cap, k_src, v_src, tiles, tile_row, n_pool_tiles, err, stream);
+}
+
+fka_status fka_mx_unpack(int32_t n_kv_heads, int32_t head_dim, int32_t from, int32_t len, const void *tiles,
+                         const int32_t *tile_row, int32_t n_pool_tiles, void *k_dst, void *v_dst, int32_t dst_cap, int32_t *err,
+                         void *stream)
+{
+    return run_mx_copy(false, n_kv_heads, head_dim, from, len, dst_cap, k_dst, v_dst, const_cast<void *>(tiles), tile_row,
+                       n_pool_tiles, err, stream);
+}
+
+fka_status fka_plan_create_mx(const fka_heads *heads, const fka_mx_desc *desc, const int32_t *host_group_start,
+                              const int32_t *host_group_prefix_len, fka_plan **out)
+{
+    REQUIRE(out != nullptr, "out is null");
+    *out = nullptr;
+    fka_status st = check_heads(heads);
+    if (st != FKA_OK) return st;
+    REQUIRE(desc != nullptr, "desc is null");
+    REQUIRE(host_group_start != nullptr && host_group_prefix_len != nullptr, "group arrays are null");
+    REQUIRE(desc->n_seqs >= 1 && desc->n_groups >= 1, "n_seqs and n_groups must be >= 1");
+    REQUIRE(desc->max_tiles_per_group >= 1, "max_tiles_per_group must be >= 1");
+    REQUIRE(desc->n_pool_tiles >= 0, "n_pool_tiles must be >= 0");
+    REQUIRE(desc->suffix_cap >= 1, "suffix_cap (%d) must be >= 1", desc->suffix_cap);
+    REQUIRE(desc->max_suffix_len >= 0 && desc->max_suffix_len <= desc->suffix_cap,
+            "max_suffix_len (%d) must be in [0, suffix_cap=%d]", desc->max_suffix_len, desc->suffix_cap);
+    REQUIRE(desc->blocks >= 0, "blocks (%d) must be >= 0", desc->blocks);
+    if (desc->n_seqs > fka::kMaxSeqs || desc->n_groups > desc->n_seqs)
+        return fail(FKA_ERR_UNSUPPORTED, "%d sequences in %d groups: at most %d, none empty", desc->n_seqs, desc->n_groups,
+                    fka::kMaxSeqs);
+    if (desc->max_suffix_len > kMaxTokens)
+        return fail(FKA_ERR_UNSUPPORTED, "max_suffix_len %d is too long (limit %d)", desc->max_suffix_len, kMaxTokens);
+    REQUIRE(host_group_start[0] == 0 && host_group_start[desc->n_groups] == desc->n_seqs,
+            "group_start must begin at 0 and end at n_seqs");
+    const int G = heads->n_q_heads / heads->n_kv_heads;
+    int64_t max_group = 0;
+    for (int t = 0; t < desc->n_groups; ++t) {
+        const int64_t n = (int64_t)host_group_start[t + 1] - host_group_start[t];
+        REQUIRE(n >= 1, "group %d is empty", t);
+        const int lp = host_group_prefix_len[t];
+        REQUIRE(lp >= 0, "group %d has a negative prefix length", t);
+        if (lp > kMaxTokens) return fail(FKA_ERR_UNSUPPORTED, "prefix of %d tokens is too long (limit %d)", lp, kMaxTokens);
+        REQUIRE(ceil_div(lp, fka::kMxTile) <= desc->max_tiles_per_group, "group %d needs %d tiles, max_tiles_per_group is %d", t,
+                ceil_div(lp, fka::kMxTile), desc->max_tiles_per_group);
+        max_group = std::max(max_group, n);
+    }
+    if (G > fka::kMaxRows || max_group * G > fka::kMaxRows)
+        return fail(FKA_ERR_UNSUPPORTED, "%lld query rows per KV head exceed the limit of %d", (long long)max_group * G,
+                    fka::kMaxRows);
+    fka_plan *p = new (std::nothrow) fka_plan();
+    if (!p) return fail(FKA_ERR_NOMEM, "host allocation failed");
+    try {
+        init_heads(p, heads);
+        p->mx = true;
+        p->n_seqs = desc->n_seqs;
+        p->n_groups = desc->n_groups;
+        p->max_tiles = desc->max_tiles_per_group;
+        p->n_pool_tiles = desc->n_pool_tiles;
+        p->suffix_cap = desc->suffix_cap;
+        p->max_suffix_len = desc->max_suffix_len;
+        p->group_start.assign(host_group_start, host_group_start + desc->n_groups + 1);
+        p->group_prefix_len.assign(host_group_prefix_len, host_group_prefix_len + desc->n_groups);
+        p->seq_prefix_len.assign(p->n_seqs, 0);
+        for (int t = 0; t < desc->n_groups; ++t) {
+            fka::UnitRec r{};
+            r.seq0 = p->group_start[t];
+            r.nseq = p->group_start[t + 1] - r.seq0;
+            r.plen = p->group_prefix_len[t];
+            p->units.push_back(r);
+            for (int s = r.seq0; s < r.seq0 + r.nseq; ++s) p->seq_prefix_len[s] = r.plen;
+        }
+        if ((st = build_mx_jobs(p, desc->blocks)) != FKA_OK || (st = finish_plan(p)) != FKA_OK) {
+            fka_plan_destroy(p);
+            return st;
+        }
+    } catch (...) {
+        fka_plan_destroy(p);
+        return fail(FKA_ERR_NOMEM, "host allocation failed");
+    }
+    *out = p;
+    return ok();
+}
+
+fka_status fka_fork_decode_mx(const fka_plan *p, const void *q, const void *tiles, const int32_t *tile_table, const void *suffix_k,
+                              const void *suffix_v, const int32_t *suffix_len, float *out, float *out_lse, void *stream)
+{
+    fka_status st = check_mx_call(p, q, tiles, tile_table, suffix_k, suffix_v, suffix_len, out, out_lse);
+    if (st != FKA_OK) return st;
+    return run_mx(p, q, tiles, tile_table, suffix_k, suffix_v, suffix_len, merge_args(p, suffix_len, out, out_lse),
+                  static_cast<hipStream_t>(stream));
+}
+
+fka_status fka_fork_step_mx(const fka_plan *p, const void *q, const void *k_new, const void *v_new, const void *tiles,
+                            const int32_t *tile_table, void *suffix_k, void *suffix_v, int32_t *suffix_len, float *out,
+                            float *out_lse, void *stream)
+{
+    fka_status st = check_mx_call(p, q, tiles, tile_table, suffix_k, suffix_v, suffix_len, out, out_lse);
+    if (st != FKA_OK) return st;
+    REQUIRE_PTR16(k_new);
+    REQUIRE_PTR16(v_new);
+    fka::MergeArgs m = merge_args(p, suffix_len, out, out_lse);
+    m.step_mode = 1;
+    m.q = static_cast<const uint16_t *>(q);
+    m.k_new = static_cast<const uint16_t *>(k_new);
+    m.v_new = static_cast<const uint16_t *>(v_new);
+    m.k_dst = static_cast<uint16_t *>(suffix_k);
+    m.v_dst = static_cast<uint16_t *>(suffix_v);
+    return run_mx(p, q, tiles, tile_table, suffix_k, suffix_v, suffix_len, m, static_cast<hipStream_t>(stream));
+}
+
+fka_status fka_key_weights(const fka_heads *heads, int32_t n_rows, int32_t len, const void *q, const float *lse, const void *k,
+                           int32_t k_cap, float *weights, int32_t weights_cap, float decay, void *stream)
+{
+    fka_status st = check_heads(heads);
+    if (st != FKA_OK) return st;
+    REQUIRE(n_rows >= 0 && len >= 0, "n_rows (%d) and len (%d) must be >= 0", n_rows, len);
+    REQUIRE(k_cap >= len && weights_cap >= len, "k_cap (%d) and weights_cap (%d) must be at least len (%d)", k_cap, weights_cap, len);
+    REQUIRE(std::isfinite(decay) && decay >= 0.f, "decay must be finite and >= 0");
+    REQUIRE(heads->n_kv_heads <= 65535, "n_kv_heads %d outside [1, 65535]", heads->n_kv_heads);
+    const int32_t G = heads->n_q_heads / heads->n_kv_heads;
+    if (len > kMaxTokens || (int64_t)n_rows * G > kMaxTokens)
+        return fail(FKA_ERR_UNSUPPORTED, "%d rows over %d keys are too many (limit %d)", n_rows, len, kMaxTokens);
+    if (len == 0) return ok();
+    if (n_rows > 0) {
+        REQUIRE_PTR16(q);
+        REQUIRE_PTR4(lse);
+    }
+    REQUIRE_PTR16(k);
+    REQUIRE_PTR4(weights);
+    fka::WeightsArgs a{};
+    a.q = static_cast<const uint16_t *>(q);
+    a.lse = lse;
+    a.k = static_cast<const uint16_t *>(k);
+    a.weights = weights;
+    a.n_rows = (int64_t)n_rows * G;
+    a.len = len;
+    a.k_cap = k_cap;
+    a.w_cap = weights_cap;
+    a.n_q_heads = heads->n_q_heads;
+    a.n_kv_heads = heads->n_kv_heads;
+    a.group = G;
+    a.by_group = fka::exact_div(G);
+    a.scale_log2 = (heads->softmax_scale > 0.f ? heads->softmax_scale : 1.0f / std::sqrt((float)heads->head_dim)) * 1.4426950408889634f;
+    a.decay = decay;
+    hipError_t e = fka::launch_key_weights(a, heads->head_dim, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "key weights kernel launch");
+    return ok();
+}
+
+size_t fka_evict_bytes(int32_t n_kv_heads, int32_t len)
+{
+    if (n_kv_heads < 1 || len < 0) return 0;
+    return (size_t)n_kv_heads * (3 * fka::kEvictBins * sizeof(uint32_t) + (size_t)ceil_div(len, fka::kEvictChunk) * 2 * sizeof(int32_t));
+}
+
+fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t keep, int32_t n_first, int32_t n_last,
+                     const void *k, const void *v, int32_t kv_cap, const float *weights, int32_t weights_cap, int32_t *index,
+                     void *k_out, void *v_out, float *weights_out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    REQUIRE(n_kv_heads >= 1 && n_kv_heads <= 65535, "n_kv_heads %d outside [1, 65535]", n_kv_heads);
+    if (head_dim != 64 && head_dim != 128)
+        return fail(FKA_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", head_dim);
+    REQUIRE(len >= 0 && keep >= 0 && keep <= len, "need 0 <= keep <= len (keep %d, len %d)", keep, len);
+    if (len > kMaxTokens) return fail(FKA_ERR_UNSUPPORTED, "%d tokens are too many (limit %d)", len, kMaxTokens);
+    REQUIRE(n_first >= 0 && n_last >= 0 && (int64_t)n_first + n_last <= keep,
+            "n_first (%d) and n_last (%d) must be >= 0 and together at most keep (%d)", n_first, n_last, keep);
+    REQUIRE(kv_cap >= len && weights_cap >= len, "kv_cap (%d) and weights_cap (%d) must be at least len (%d)", kv_cap, weights_cap, len);
+    if (keep == 0) return ok();
+    REQUIRE_PTR16(k);
+    REQUIRE_PTR16(v);
+    REQUIRE_PTR4(weights);
+    REQUIRE_PTR4(index);
+    REQUIRE_PTR16(k_out);
+    REQUIRE_PTR16(v_out);
+    REQUIRE_OPT4(weights_out);
+    REQUIRE_PTR4(workspace);
+    const size_t need = fka_evict_bytes(n_kv_heads, len);
+    REQUIRE(workspace_bytes >= need, "workspace of %zu bytes, %zu are needed", workspace_bytes, need);
+    fka::EvictArgs a{};
+    a.k = static_cast<const uint16_t *>(k);
+    a.v = static_cast<const uint16_t *>(v);
+    a.weights = weights;
+    a.index = index;
+    a.k_out = static_cast<uint16_t *>(k_out);
+    a.v_out = static_cast<uint16_t *>(v_out);
+    a.weights_out = weights_out;
+    a.hist = static_cast<uint32_t *>(workspace);
+    a.counts = reinterpret_cast<int32_t *>(a.hist + (size_t)3 * n_kv_heads * fka::kEvictBins);
+    a.len = len;
+    a.kv_cap = kv_cap;
+    a.w_cap = weights_cap;
+    a.keep = keep;
+    a.n_first = n_first;
+    a.n_last = n_last;
+    a.n_kv_heads = n_kv_heads;
+    a.head_dim = head_dim;
+    a.chunks = ceil_div(len, fka::kEvictChunk);
+    hipError_t e = fka::launch_evict(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "evict kernel launch");
     return ok();
 }
 

@@ -361,6 +361,104 @@ struct PrefillArgs {
     TileSplit split;
 };
 
+// New tokens' norm, rotation and store (rotate.h).
+struct RotateArgs {
+    const uint16_t *q, *k, *v;       // [tokens] rows of heads x d, q_stride / k_stride / v_stride elements apart
+    int64_t q_stride, k_stride, v_stride;
+    const uint16_t *q_weight, *k_weight;  // bf16 [d] or null
+    const double *freq;              // [rotary_dim / 2], radians per position
+    const int32_t *positions;        // [tokens]
+    uint16_t *q_out;                 // [tokens][Hq][d]
+    uint16_t *k_dst, *v_dst;         // contiguous [N][Hkv][cap][d] or pools [pages][Hkv][16][d]
+    int32_t *suffix_len;             // [N] or null (rows from 0)
+    const int32_t *page_table;       // paged: [N][max_pages]
+    const int32_t *seq_prefix_len;   // paged: [N]
+    int32_t n_seqs, n_tokens;        // N, n
+    ExactDiv by_tokens;
+    int32_t n_q_heads, n_kv_heads;
+    int32_t rotary_dim;
+    int32_t max_len, suffix_cap, max_pages, n_pool_pages;
+    int32_t advance;
+    float eps;
+    int32_t *err;                    // nullable
+};
+
+// 4-bit tiles (mx_tiles.h): tokens of a tile, values sharing a scale; packing and unpacking.
+constexpr int kMxTile = 128;
+constexpr int kMxBlock = 32;
+
+struct MxCopyArgs {
+    const uint16_t *k_src, *v_src;  // pack: [Hkv][cap][d], position from at row 0
+    uint16_t *k_dst, *v_dst;        // unpack: the same
+    uint8_t *tiles;                 // pool [n_pool_tiles][Hkv][136 d]
+    const int32_t *tile_row;        // tile ids of positions 0, 128, ...; null: 0, 1, ...
+    int32_t from, len;              // positions [from, len)
+    int32_t cap;
+    int32_t n_kv_heads, n_pool_tiles;
+    int32_t *err;                   // nullable
+};
+
+// Decode over a prefix in 4-bit tiles (mx_attend.h): a block's job, fixed by the plan.
+struct MxJob {  // 12 int32
+    int32_t suffix;     // 0: prefix tiles [begin, end) of the group; 1: share begin of end of a suffix
+    int32_t group;
+    int32_t head;
+    int32_t slot;       // partial-result slot
+    int32_t row0;       // first row of the slot it writes
+    int32_t seq0;       // its first sequence; a suffix: the sequence
+    int32_t first, rows; // its rows, from the first of seq0's on (a suffix: at most 16)
+    int32_t begin, end;
+    int32_t prefix_len;
+    int32_t tile0;      // first tile of the group where there is no tile table
+};
+
+struct MxArgs {
+    const MxJob *jobs;
+    const uint16_t *q;            // [S][Hq][d]
+    const uint8_t *tiles;         // [n_pool_tiles][Hkv][136 d]
+    const int32_t *tile_table;    // [groups][max_tiles] or null
+    const uint16_t *suffix_k, *suffix_v;  // [S][Hkv][cap][d]
+    const int32_t *suffix_len;    // [S]
+    int32_t *lens;                // [S] clamped lengths of this launch, for the merge
+    float *part_o, *part_lse;
+    int32_t *err;
+    int32_t max_tiles, n_pool_tiles;
+    int32_t suffix_cap, max_suffix_len;
+    int32_t n_seqs, n_q_heads, n_kv_heads, group;
+    uint32_t group_magic;
+    int32_t slot_rows;
+    float scale_log2;
+};
+
+// The attention weight of each key (evict.h).
+struct WeightsArgs {
+    const uint16_t *q;     // [R][Hq][d]
+    const float *lse;      // [R][Hq]
+    const uint16_t *k;     // [Hkv][k_cap][d]
+    float *weights;        // [Hkv][w_cap]
+    int64_t n_rows;        // R G per KV head
+    int32_t len, k_cap, w_cap;
+    int32_t n_q_heads, n_kv_heads, group;
+    ExactDiv by_group;
+    float scale_log2, decay;
+};
+
+// A prefix shortened to its heaviest keys (evict.h): histogram bins of a digit, positions per block.
+constexpr int kEvictBins = 2048;
+constexpr int kEvictChunk = 2048;
+
+struct EvictArgs {
+    const uint16_t *k, *v;   // [Hkv][kv_cap][d]
+    const float *weights;    // [Hkv][w_cap]
+    int32_t *index;          // [Hkv][keep]
+    uint16_t *k_out, *v_out; // [Hkv][keep][d]
+    float *weights_out;      // [Hkv][keep] or null
+    uint32_t *hist;          // [3][Hkv][2048]
+    int32_t *counts;         // [Hkv][chunks][2]: above the threshold, at it
+    int32_t len, kv_cap, w_cap, keep, n_first, n_last;
+    int32_t n_kv_heads, head_dim, chunks;
+};
+
 // error-flag bits (device)
 constexpr int32_t kErrSuffixClamped = 1;
 constexpr int32_t kErrAppendNoRoom = 2;
@@ -391,6 +489,14 @@ hipError_t launch_prefill_tiles(const PrefillArgs &a, int n_blocks, int head_dim
 hipError_t launch_append(const AppendArgs &a, int n_seqs, hipStream_t s);
 hipError_t launch_gather(const GatherArgs &a, hipStream_t s);
 hipError_t launch_scatter(const ScatterArgs &a, hipStream_t s);
+hipError_t launch_rotate(const RotateArgs &a, int head_dim, bool interleaved, hipStream_t s);
+hipError_t launch_mx_pack(const MxCopyArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_mx_unpack(const MxCopyArgs &a, int head_dim, hipStream_t s);
+// Decode over 4-bit tiles: resident blocks per compute unit (0 on error), and the launch.
+int mx_blocks_per_cu(int head_dim, int row_tiles);
+hipError_t launch_mx_partials(const MxArgs &a, int n_jobs, int head_dim, int row_tiles, hipStream_t s);
+hipError_t launch_key_weights(const WeightsArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
 hipError_t launch_read_probe(const void *buf, size_t bytes, int blocks, int threads, int unroll, uint32_t *sink,
                              hipStream_t s);
 

@@ -3,8 +3,14 @@
 // (the partial-attention kernel over key ranges lives in partials.hip)
 // merge_kernel: log-sum-exp combination of the partials of each (sequence, head).
 // append_kernel / gather_kernel: suffix append and paged gather (data movement).
+// The operators around a snapshot's cache are in headers of their own: rotate.h (norm, rotation and store of new
+// tokens), mx_tiles.h (4-bit tiles), mx_attend.h (decode over them), evict.h (key weights, shortening).
+#include "evict.h"
 #include "internal.h"
 #include "merge_row.h"
+#include "mx_attend.h"
+#include "mx_tiles.h"
+#include "rotate.h"
 
 namespace fka {
 namespace {
@@ -389,5 +395,28 @@ hipError_t launch_gather(const GatherArgs &a, hipStream_t s)
     gather_kernel<<<dim3((a.out_len - a.begin + kPageSize - 1) / kPageSize, a.n_kv_heads), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
+
+hipError_t launch_rotate(const RotateArgs &a, int head_dim, bool interleaved, hipStream_t s)
+{
+    return launch_rotate_kernels(a, head_dim, interleaved, s);
+}
+
+hipError_t launch_mx_pack(const MxCopyArgs &a, int head_dim, hipStream_t s) { return launch_mx_pack_kernel(a, head_dim, s); }
+
+hipError_t launch_mx_unpack(const MxCopyArgs &a, int head_dim, hipStream_t s) { return launch_mx_unpack_kernel(a, head_dim, s); }
+
+int mx_blocks_per_cu(int head_dim, int row_tiles) { return mx_blocks_per_cu_of(head_dim, row_tiles); }
+
+hipError_t launch_mx_partials(const MxArgs &a, int n_jobs, int head_dim, int row_tiles, hipStream_t s)
+{
+    if (n_jobs <= 0) return hipSuccess;
+    if (head_dim == 128) return launch_mx_hd<128>(a, n_jobs, row_tiles, s);
+    if (head_dim == 64) return launch_mx_hd<64>(a, n_jobs, row_tiles, s);
+    return hipErrorInvalidValue;
+}
+
+hipError_t launch_key_weights(const WeightsArgs &a, int head_dim, hipStream_t s) { return launch_key_weights_kernel(a, head_dim, s); }
+
+hipError_t launch_evict(const EvictArgs &a, hipStream_t s) { return launch_evict_kernels(a, s); }
 
 }  // namespace fka

@@ -66,6 +66,20 @@ class Slot(C.Structure):
                 ("suffix_begin", C.c_int32), ("suffix_end", C.c_int32), ("prefix_len", C.c_int32)]
 
 
+class RotateDesc(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("max_len", C.c_int32),
+                ("advance", C.c_int32), ("eps", C.c_float), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64)]
+
+
+class MxDesc(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_groups", C.c_int32), ("max_tiles_per_group", C.c_int32),
+                ("n_pool_tiles", C.c_int32), ("suffix_cap", C.c_int32), ("max_suffix_len", C.c_int32), ("blocks", C.c_int32)]
+
+
+MX_TILE = 128  # tokens of a 4-bit tile
+
 _vp = C.c_void_p
 _sig = {
     "fka_version": ([], C.c_int),
@@ -107,6 +121,18 @@ _sig = {
                          C.c_int),
     "fka_scatter_pages": ([_vp, _vp, C.c_int32, C.c_int32, _vp, C.c_int32, C.c_int32, C.c_int32, _vp, _vp, _vp, _vp],
                           C.c_int),
+    "fka_rotate_append": ([C.POINTER(RotateDesc)] + [_vp] * 10 + [C.c_int32, _vp, _vp, _vp], C.c_int),
+    "fka_rotate_append_paged": ([C.POINTER(RotateDesc)] + [_vp] * 12 + [C.c_int32, C.c_int32, _vp, _vp, _vp], C.c_int),
+    "fka_mx_tile_bytes": ([C.c_int32, C.c_int32], C.c_size_t),
+    "fka_mx_pack": ([C.c_int32] * 4 + [_vp, _vp, C.c_int32, _vp, _vp, C.c_int32, _vp, _vp], C.c_int),
+    "fka_mx_unpack": ([C.c_int32] * 4 + [_vp, _vp, C.c_int32, _vp, _vp, C.c_int32, _vp, _vp], C.c_int),
+    "fka_plan_create_mx": ([C.POINTER(Heads), C.POINTER(MxDesc), _vp, _vp, C.POINTER(_vp)], C.c_int),
+    "fka_fork_decode_mx": ([_vp] * 10, C.c_int),
+    "fka_fork_step_mx": ([_vp] * 12, C.c_int),
+    "fka_key_weights": ([C.POINTER(Heads), C.c_int32, C.c_int32, _vp, _vp, _vp, C.c_int32, _vp, C.c_int32, C.c_float, _vp],
+                        C.c_int),
+    "fka_evict_bytes": ([C.c_int32, C.c_int32], C.c_size_t),
+    "fka_evict": ([C.c_int32] * 6 + [_vp, _vp, C.c_int32, _vp, C.c_int32] + [_vp] * 5 + [C.c_size_t, _vp], C.c_int),
 }
 for _name, (_args, _res) in _sig.items():
     _f = getattr(_lib, _name)
@@ -135,7 +161,7 @@ def version() -> int:
     return _lib.fka_version()
 
 
-_KIND_DTYPES = {"bf16": torch.bfloat16, "i32": torch.int32, "f32": torch.float32}
+_KIND_DTYPES = {"bf16": torch.bfloat16, "i32": torch.int32, "f32": torch.float32, "f64": torch.float64, "u8": torch.uint8}
 
 
 def _p(t: Optional[torch.Tensor], kind: Optional[str] = None, device: Optional[int] = None):
@@ -243,6 +269,37 @@ class Plan:
         _check(_lib.fka_prefill(self._h, _p(q, "bf16", d), _p(prefix_k, "bf16", d), _p(prefix_v, "bf16", d),
                                 _p(suffix_k, "bf16", d), _p(suffix_v, "bf16", d), _p(suffix_len, "i32", d),
                                 _p(out, "f32", d), _p(out_lse, "f32", d), _stream(stream)))
+
+    @classmethod
+    def mx_plan(cls, n_q_heads, n_kv_heads, head_dim, group_start, group_prefix_len, suffix_cap, max_suffix_len, *, n_pool_tiles,
+                max_tiles=None, softmax_scale=0.0, blocks=0) -> "Plan":
+        """A decode plan over 4-bit prefix tiles and contiguous suffixes (fka_plan_create_mx); max_tiles is the
+        tile table's width (default: the longest prefix's tiles)."""
+        gs = np.ascontiguousarray(group_start, np.int32)
+        gl = np.ascontiguousarray(group_prefix_len, np.int32)
+        if gs.ndim != 1 or gl.shape != (len(gs) - 1,):
+            raise ValueError("group_start must have one entry more than group_prefix_len")
+        if max_tiles is None:
+            max_tiles = max(1, -(-int(gl.max(initial=0)) // MX_TILE))
+        h = Heads(n_q_heads, n_kv_heads, head_dim, softmax_scale)
+        d = MxDesc(int(gs[-1]), len(gl), max_tiles, n_pool_tiles, suffix_cap, max_suffix_len, blocks)
+        out = _vp()
+        _check(_lib.fka_plan_create_mx(C.byref(h), C.byref(d), gs.ctypes.data_as(_vp), gl.ctypes.data_as(_vp), C.byref(out)))
+        return cls(out.value, False, h, int(gs[-1]))
+
+    def decode_mx(self, q, tiles, suffix_k, suffix_v, suffix_len, out, out_lse=None, tile_table=None, stream=None):
+        """fka_fork_decode_mx: tiles uint8 [pool][Hkv][136 d], tile_table int32 [groups][max_tiles] or None."""
+        d = self.device
+        _check(_lib.fka_fork_decode_mx(self._h, _p(q, "bf16", d), _p(tiles, "u8", d), _p(tile_table, "i32", d),
+                                       _p(suffix_k, "bf16", d), _p(suffix_v, "bf16", d), _p(suffix_len, "i32", d),
+                                       _p(out, "f32", d), _p(out_lse, "f32", d), _stream(stream)))
+
+    def step_mx(self, q, k_new, v_new, tiles, suffix_k, suffix_v, suffix_len, out, out_lse=None, tile_table=None, stream=None):
+        """fka_fork_step_mx: append and decode."""
+        d = self.device
+        _check(_lib.fka_fork_step_mx(self._h, _p(q, "bf16", d), _p(k_new, "bf16", d), _p(v_new, "bf16", d), _p(tiles, "u8", d),
+                                     _p(tile_table, "i32", d), _p(suffix_k, "bf16", d), _p(suffix_v, "bf16", d),
+                                     _p(suffix_len, "i32", d), _p(out, "f32", d), _p(out_lse, "f32", d), _stream(stream)))
 
     def close(self):
         if self._h is not None and self._h.value:
@@ -446,6 +503,163 @@ def lse_merge(part_o, part_lse, out, out_lse=None, stream=None):
     """part_o fp32 [P][R][d], part_lse fp32 [P][R] -> out fp32 [R][d], out_lse fp32 [R]."""
     P, R, d = part_o.shape
     _check(_lib.fka_lse_merge(R, P, d, _p(part_o, "f32"), _p(part_lse, "f32"), _p(out, "f32"), _p(out_lse, "f32"), _stream(stream)))
+
+
+def _token_rows(t, what):
+    """Token stride (elements) of q, k or v [N][n][heads][d]: any view whose tokens lie evenly apart."""
+    if t.dim() != 4 or t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != t.shape[3]):
+        raise ValueError(f"{what} must be [N][n][heads][d] with the heads of a token dense")
+    N, n, heads, d = t.shape
+    step = t.stride(1) if n > 1 else t.stride(0) if N > 1 else heads * d
+    if N > 1 and n > 1 and t.stride(0) != n * step:
+        raise ValueError(f"the tokens of {what} must lie evenly apart")
+    return step
+
+
+def _on_current(t):
+    """The device of t, which has to be the current one: a call without a plan launches on the current device's stream."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("tensor must be on the GPU (the library reads device memory)")
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"tensor is on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+    return dev
+
+
+def _strided(t, dev):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.bfloat16:
+        raise ValueError("expected a bf16 tensor on the GPU")
+    if t.get_device() != dev:
+        raise ValueError(f"tensor is on cuda:{t.get_device()}, q is on cuda:{dev}")
+    return t.data_ptr()
+
+
+def _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, max_len, advance):
+    if any(not isinstance(t, torch.Tensor) for t in (q, k, v, positions, q_out)):
+        raise ValueError("expected a torch tensor")
+    steps = [_token_rows(t, what) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
+    N, n, Hq, d = q.shape
+    Hkv = k.shape[2]
+    if k.shape != (N, n, Hkv, d) or v.shape != (N, n, Hkv, d):
+        raise ValueError("k and v must be [N][n][Hkv][d] with q's N, n and d")
+    if q_out.shape != q.shape or positions.numel() != N * n:
+        raise ValueError("q_out must have q's shape, positions N n entries")
+    if any(w is not None and w.shape != (d,) for w in (q_weight, k_weight)):
+        raise ValueError("a norm weight must be [d]")
+    rot = 0 if freq is None else 2 * freq.numel()
+    return RotateDesc(N, n, Hq, Hkv, d, rot, int(bool(interleaved)), max_len, int(bool(advance)), eps, *steps)
+
+
+def _check_lens(suffix_len, N):
+    if suffix_len is not None and suffix_len.numel() != N:
+        raise ValueError("suffix_len must have an entry per sequence")
+
+
+def rotate_append(q, k, v, positions, freq, q_out, suffix_k, suffix_v, suffix_len=None, *, q_weight=None, k_weight=None,
+                  eps=1e-6, interleaved=False, max_len=None, advance=False, err=None, stream=None):
+    """fka_rotate_append: q, k, v bf16 [N][n][heads][d] (views of a joint projection output allowed), positions int32 [N][n],
+    freq fp64 [rotary_dim / 2] or None -> q_out, and rows of suffix_k / suffix_v bf16 [N][Hkv][cap][d]."""
+    desc = _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, 0, advance)
+    N, Hkv, d = desc.n_seqs, desc.n_kv_heads, desc.head_dim
+    cap = suffix_k.shape[2] if suffix_k.dim() == 4 else -1
+    if suffix_k.shape != (N, Hkv, cap, d) or suffix_v.shape != suffix_k.shape:
+        raise ValueError("suffix_k and suffix_v must be [N][Hkv][cap][d]")
+    _check_lens(suffix_len, N)
+    desc.max_len = cap if max_len is None else max_len
+    dev = _on_current(q)
+    _check(_lib.fka_rotate_append(C.byref(desc), _strided(q, dev), _strided(k, dev), _strided(v, dev), _p(q_weight, "bf16", dev),
+                                  _p(k_weight, "bf16", dev), _p(freq, "f64", dev), _p(positions, "i32", dev),
+                                  _p(q_out, "bf16", dev), _p(suffix_k, "bf16", dev), _p(suffix_v, "bf16", dev), cap,
+                                  _p(suffix_len, "i32", dev), _p(err, "i32", dev), _stream(stream)))
+
+
+def rotate_append_paged(q, k, v, positions, freq, q_out, k_pool, v_pool, page_table, prefix_len, suffix_len=None, *,
+                        q_weight=None, k_weight=None, eps=1e-6, interleaved=False, max_len=None, advance=False, err=None,
+                        stream=None):
+    """fka_rotate_append_paged: as rotate_append, into the pages of page_table int32 [N][max_pages] behind prefix_len int32 [N]."""
+    desc = _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, 0, advance)
+    N, Hkv, d = desc.n_seqs, desc.n_kv_heads, desc.head_dim
+    if k_pool.dim() != 4 or k_pool.shape[1:] != (Hkv, 16, d) or v_pool.shape != k_pool.shape:
+        raise ValueError("k_pool and v_pool must be [pages][Hkv][16][d]")
+    if page_table.dim() != 2 or page_table.shape[0] != N or prefix_len.numel() != N:
+        raise ValueError("page_table must have a row, prefix_len an entry per sequence")
+    _check_lens(suffix_len, N)
+    desc.max_len = 16 * page_table.shape[1] if max_len is None else max_len
+    dev = _on_current(q)
+    _check(_lib.fka_rotate_append_paged(C.byref(desc), _strided(q, dev), _strided(k, dev), _strided(v, dev),
+                                        _p(q_weight, "bf16", dev), _p(k_weight, "bf16", dev), _p(freq, "f64", dev),
+                                        _p(positions, "i32", dev), _p(q_out, "bf16", dev), _p(k_pool, "bf16", dev),
+                                        _p(v_pool, "bf16", dev), _p(page_table, "i32", dev), _p(prefix_len, "i32", dev),
+                                        page_table.shape[1], k_pool.shape[0], _p(suffix_len, "i32", dev), _p(err, "i32", dev),
+                                        _stream(stream)))
+
+
+def mx_tile_bytes(n_kv_heads, head_dim) -> int:
+    """Bytes of one 4-bit tile (128 tokens) of all KV heads."""
+    return _lib.fka_mx_tile_bytes(n_kv_heads, head_dim)
+
+
+def _mx_sizes(k, v, tiles, tile_row, frm, length):
+    if k.dim() != 3 or v.shape != k.shape:
+        raise ValueError("k and v must be [Hkv][cap][d]")
+    Hkv, cap, d = k.shape
+    if tiles.dim() != 3 or tiles.shape[1:] != (Hkv, 136 * d):
+        raise ValueError("tiles must be uint8 [pool][Hkv][136 d]")
+    length = int(frm) + cap if length is None else int(length)
+    if tile_row is not None and tile_row.numel() < -(-length // MX_TILE):
+        raise ValueError("tile_row is shorter than the prefix's tiles")
+    return Hkv, cap, d, length
+
+
+def mx_pack(k, v, tiles, *, tile_row=None, frm=0, length=None, err=None, stream=None):
+    """fka_mx_pack: positions [frm, length) held in k, v bf16 [Hkv][cap][d] -> tiles uint8 [pool][Hkv][136 d]."""
+    Hkv, cap, d, length = _mx_sizes(k, v, tiles, tile_row, frm, length)
+    dev = _on_current(tiles)
+    _check(_lib.fka_mx_pack(Hkv, d, int(frm), length, _p(k, "bf16", dev), _p(v, "bf16", dev), cap, _p(tiles, "u8", dev),
+                            _p(tile_row, "i32", dev), tiles.shape[0], _p(err, "i32", dev), _stream(stream)))
+
+
+def mx_unpack(tiles, k, v, *, tile_row=None, frm=0, length=None, err=None, stream=None):
+    """fka_mx_unpack: the values of positions [frm, length) -> k, v bf16 [Hkv][cap][d]."""
+    Hkv, cap, d, length = _mx_sizes(k, v, tiles, tile_row, frm, length)
+    dev = _on_current(tiles)
+    _check(_lib.fka_mx_unpack(Hkv, d, int(frm), length, _p(tiles, "u8", dev), _p(tile_row, "i32", dev), tiles.shape[0],
+                              _p(k, "bf16", dev), _p(v, "bf16", dev), cap, _p(err, "i32", dev), _stream(stream)))
+
+
+def key_weights(q, lse, k, weights, *, length=None, decay=0.0, softmax_scale=0.0, stream=None):
+    """fka_key_weights: q bf16 [R][Hq][d], lse fp32 [R][Hq], k bf16 [Hkv][cap][d] -> weights fp32 [Hkv][cap']."""
+    R, Hq, d = q.shape
+    Hkv, cap = k.shape[0], k.shape[1]
+    if k.shape != (Hkv, cap, d) or lse.shape != (R, Hq) or weights.dim() != 2 or weights.shape[0] != Hkv:
+        raise ValueError("lse must be [R][Hq], k [Hkv][cap][d] and weights [Hkv][cap']")
+    h = Heads(Hq, Hkv, d, softmax_scale)
+    dev = _on_current(weights)
+    _check(_lib.fka_key_weights(C.byref(h), R, min(cap, weights.shape[1]) if length is None else int(length), _p(q, "bf16", dev),
+                                _p(lse, "f32", dev), _p(k, "bf16", dev), cap, _p(weights, "f32", dev), weights.shape[1],
+                                float(decay), _stream(stream)))
+
+
+def evict_workspace(n_kv_heads, length, device="cuda"):
+    """A workspace for evict over up to `length` positions."""
+    return torch.empty(_lib.fka_evict_bytes(n_kv_heads, length), dtype=torch.uint8, device=device)
+
+
+def evict(k, v, weights, index, k_out, v_out, weights_out=None, *, n_first=0, n_last=0, length=None, workspace, stream=None):
+    """fka_evict: keeps index.shape[1] of each KV head's positions (k, v bf16 [Hkv][cap][d], weights fp32 [Hkv][cap'])."""
+    if k.dim() != 3 or v.shape != k.shape or weights.dim() != 2 or weights.shape[0] != k.shape[0] or index.dim() != 2:
+        raise ValueError("k and v must be [Hkv][cap][d], weights [Hkv][cap'], index [Hkv][keep]")
+    Hkv, cap, d = k.shape
+    keep = index.shape[1]
+    if index.shape != (Hkv, keep) or k_out.shape != (Hkv, keep, d) or v_out.shape != k_out.shape:
+        raise ValueError("k_out and v_out must be [Hkv][keep][d]")
+    if weights_out is not None and weights_out.shape != (Hkv, keep):
+        raise ValueError("weights_out must be [Hkv][keep]")
+    dev = _on_current(k)
+    _check(_lib.fka_evict(Hkv, d, min(cap, weights.shape[1]) if length is None else int(length), keep, int(n_first), int(n_last),
+                          _p(k, "bf16", dev), _p(v, "bf16", dev), cap, _p(weights, "f32", dev), weights.shape[1],
+                          _p(index, "i32", dev), _p(k_out, "bf16", dev), _p(v_out, "bf16", dev), _p(weights_out, "f32", dev),
+                          _p(workspace, "u8", dev), workspace.numel(), _stream(stream)))
 
 
 def raw_call(name: str, *args) -> int:

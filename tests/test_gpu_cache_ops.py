@@ -1,0 +1,885 @@
+"""The operators around a snapshot's cache on the GPU: new tokens' norm, rotation and store, the 4-bit prefix tiles and the
+decode over them, the keys' attention weights and the shortening of a prefix, each against its definition in 64 bits
+(numpy here, oracle.decode_contig for the attention over the unpacked values).
+
+Tolerances, from the arithmetic (u = 2^-24 is the fp32 half step):
+  a rounding to bf16 is off by at most 2^-8 of the value;
+  a score, an fp32 sum of d exact products, is off by at most (d + 4) u S, S = scale sum |q_c k_c| + |lse| (the largest of the
+  case), and so is the exponent of a weight, which is then off by that relative amount;
+  an attention output is a weighted mean of values whose weights are off by twice that (numerator and denominator), by 2^-20 for
+  the two terms of p (each cut to 11 bits), and by 2^-19 for the hardware's exponentials, reciprocal and the merge;
+  the rotation: the angle is off by less than 2^-21 and each fp32 step by u, in all 2^-18 of the pair's length.
+"""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from tests.gpu_util import dev_bf16, dev_i32
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def fa():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2608_13667_amd import forkattn
+    return forkattn
+
+
+def bits_of(x) -> np.ndarray:
+    """fp64 values -> bf16 bits, to nearest even."""
+    return torch.from_numpy(np.asarray(x, np.float32)).bfloat16().view(torch.int16).numpy().view(np.uint16)
+
+
+def value(bits) -> np.ndarray:
+    return (np.asarray(bits).astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+
+
+def host(t) -> np.ndarray:
+    return t.cpu().view(torch.int16).numpy().view(np.uint16)
+
+
+def normal(rng, *shape, scale=1.0) -> np.ndarray:
+    return bits_of(rng.standard_normal(shape) * scale)
+
+
+# ------------------------------------------------------------------ norm, rotation, store
+
+def ref_rotate(x, w, pos, freq, rot, interleaved, eps):
+    """x fp64 [N][n][H][d], pos [N][n] -> (z, length of each channel's pair)."""
+    y = x if w is None else x * w / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    z, size = y.copy(), np.abs(y)
+    if rot:
+        ang = pos[..., None, None] * freq
+        c, s = np.cos(ang), np.sin(ang)
+        a = np.arange(rot // 2)
+        i, j = (2 * a, 2 * a + 1) if interleaved else (a, a + rot // 2)
+        z[..., i] = y[..., i] * c - y[..., j] * s
+        z[..., j] = y[..., j] * c + y[..., i] * s
+        size[..., i] = size[..., j] = np.hypot(y[..., i], y[..., j])
+    return z, size
+
+
+def close_rotated(got, want, what):
+    z, size = want
+    bad = np.abs(value(got) - z) > 2.0 ** -8 * np.abs(z) + 2.0 ** -18 * size + 1e-37
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size} off"
+
+
+ROTATE = [
+    # N, n, Hq, Hkv, d, rot, interleaved, norm, lengths, far
+    (5, 1, 40, 8, 128, 128, False, True, [0, 7, 300, 31, 512], 131000),
+    (1, 1, 1, 1, 64, 64, False, True, [3], 0),
+    (3, 1, 9, 3, 64, 32, True, True, [1, 0, 2], 70000),
+    (2, 1, 7, 1, 128, 0, False, True, [1, 5], 0),
+    (2, 5, 10, 2, 128, 64, False, False, [0, 17], 999983),
+    (3, 17, 17, 17, 64, 64, True, False, [4, 15, 16], 12345),
+    (1, 2300, 12, 3, 128, 128, False, True, [0], 0),          # past the rule's many tokens
+    (2, 1100, 5, 1, 64, 48, True, True, [9, 33], 2 ** 20),
+    (2100, 1, 2, 1, 64, 64, False, True, None, 5),
+]
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("case", range(len(ROTATE)))
+def test_rotate_append(fa, case, paged):
+    N, n, Hq, Hkv, d, rot, inter, norm, lens, far = ROTATE[case]
+    rng = np.random.default_rng(100 + case)
+    lens = rng.integers(0, 20, N) if lens is None else np.array(lens)
+    width = (Hq + 2 * Hkv) * d + 8  # a joint projection's row, with a gap
+    rows = normal(rng, N, n, width)
+    w = [bits_of(1 + 0.3 * rng.standard_normal(d)) if norm else None for _ in "qk"]
+    pos = (far + lens[:, None] + np.arange(n)[None]).astype(np.int32)
+    freq = 1e6 ** (-np.arange(0, rot, 2) / rot) if rot else None
+    cap = int(lens.max()) + n + 2
+    t = dev_bf16(rows)
+    q, k, v = (t[..., a * d: b * d].unflatten(-1, (-1, d)) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    q_out = torch.full((N, n, Hq, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    kw = dict(q_weight=dev_bf16(w[0]) if norm else None, k_weight=dev_bf16(w[1]) if norm else None, eps=1e-5, interleaved=inter)
+    dl, err = dev_i32(lens), torch.zeros(1, dtype=torch.int32, device="cuda")
+    fr = torch.from_numpy(freq).cuda() if rot else None
+    for advance in (False, True):
+        print(f"[rotate] {ROTATE[case]} paged {paged} advance {advance}", flush=True)
+        if paged:
+            lp = rng.integers(0, 40, N).astype(np.int32)
+            wide = (40 + 15) // 16 + (cap + 15) // 16
+            table = rng.permutation(N * wide + 2)[: N * wide].reshape(N, wide).astype(np.int32)
+            pools = [torch.full((N * wide + 2, Hkv, 16, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+            fa.rotate_append_paged(q, k, v, dev_i32(pos), fr, q_out, *pools, dev_i32(table), dev_i32(lp), dl, advance=advance,
+                                   err=err, **kw)
+        else:
+            pools = [torch.full((N, Hkv, cap, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+            fa.rotate_append(q, k, v, dev_i32(pos), fr, q_out, *pools, dl, advance=advance, err=err, **kw)
+        torch.cuda.synchronize()
+        assert int(err.item()) == 0
+        assert np.array_equal(dl.cpu().numpy(), lens + (n if advance else 0))
+        x = value(rows)
+        f64 = lambda b: None if b is None else value(b)  # noqa: E731
+        part = lambda a, b: x[..., a * d: b * d].reshape(N, n, b - a, d)  # noqa: E731
+        close_rotated(host(q_out), ref_rotate(part(0, Hq), f64(w[0]), pos.astype(np.float64), freq, rot, inter, 1e-5), "q")
+        want_k = ref_rotate(part(Hq, Hq + Hkv), f64(w[1]), pos.astype(np.float64), freq, rot, inter, 1e-5)
+        got = [host(p) for p in pools]
+        # the written rows, and nothing else
+        row = lens[:, None] + np.arange(n)[None]
+        if paged:
+            page = np.take_along_axis(table, (lp[:, None] + 15) // 16 + row // 16, 1)
+            at = (page, slice(None), row % 16)
+        else:
+            at = (np.arange(N)[:, None], slice(None), row)
+        close_rotated(got[0][at], want_k, "k")
+        raw_v = rows[..., (Hq + Hkv) * d: (Hq + 2 * Hkv) * d].reshape(N, n, Hkv, d)
+        assert np.array_equal(got[1][at], raw_v), "v is copied"
+        for g in got:
+            g[at] = bits_of(7.0)
+            assert (g == bits_of(7.0)).all(), "rows outside the new tokens were written"
+
+
+def test_rotate_without_norm_or_rotation_copies_bits(fa):
+    rng = np.random.default_rng(3)
+    rows = rng.integers(0, 2 ** 16, (2, 3, 6, 64)).astype(np.uint16)  # NaN payloads, infinities, subnormals
+    t = dev_bf16(rows)
+    q_out = torch.zeros(2, 3, 4, 64, dtype=torch.bfloat16, device="cuda")
+    kc, vc = (torch.zeros(2, 1, 3, 64, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    fa.rotate_append(t[:, :, :4], t[:, :, 4:5], t[:, :, 5:], dev_i32(np.zeros((2, 3))), None, q_out, kc, vc)
+    assert np.array_equal(host(q_out), rows[:, :, :4])
+    assert np.array_equal(host(kc)[:, 0], rows[:, :, 4]) and np.array_equal(host(vc)[:, 0], rows[:, :, 5])
+
+
+def test_rotate_in_place_and_zero_row(fa):
+    """q_out may be q; a head of zeros stays zero (eps keeps the norm finite), a NaN stays in its head."""
+    rng = np.random.default_rng(4)
+    rows = normal(rng, 4, 1, 5, 128)
+    rows[1, 0, 2] = 0
+    rows[2, 0, 3, 17] = 0x7FC0
+    q, k = dev_bf16(rows), dev_bf16(normal(rng, 4, 1, 1, 128))
+    w, freq, pos = dev_bf16(bits_of(np.ones(128))), torch.full((64,), 0.01, dtype=torch.float64, device="cuda"), dev_i32(np.arange(4))
+    out = torch.empty_like(q)
+    kc, vc = (torch.zeros(4, 1, 1, 128, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    fa.rotate_append(q, k, k, pos, freq, out, kc, vc, q_weight=w)
+    fa.rotate_append(q, k, k, pos, freq, q, kc, vc, q_weight=w)
+    a, b = host(out), host(q)
+    assert np.array_equal(a, b)
+    assert (value(a[1, 0, 2]) == 0).all()
+    nan = np.isnan(value(a)).any(-1)
+    assert nan[2, 0, 3] and nan.sum() == 1
+
+
+def test_rotate_refuses_rows_without_room(fa):
+    rng = np.random.default_rng(5)
+    for n in (1, 3):
+        lens = np.array([0, 8 - n, 9 - n, -1, 2 ** 31 - 1], np.int32)
+        t = dev_bf16(normal(rng, 5, n, 3, 64))
+        kc, vc = (torch.zeros(5, 1, 9, 64, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+        q_out, dl = torch.zeros(5, n, 1, 64, dtype=torch.bfloat16, device="cuda"), dev_i32(lens)
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        fa.rotate_append(t[:, :, :1], t[:, :, 1:2], t[:, :, 2:], dev_i32(np.zeros((5, n))), None, q_out, kc, vc, dl, max_len=8,
+                         advance=True, err=err)
+        assert int(err.item()) == fa.ERR_APPEND_NO_ROOM
+        assert np.array_equal(dl.cpu().numpy(), [n, 8, 9 - n, -1, 2 ** 31 - 1])
+        assert (host(q_out) != 0).any(axis=(1, 2, 3)).all()
+        assert [int((host(c)[b] != 0).any()) for c in (kc, vc) for b in range(5)] == [1, 1, 0, 0, 0] * 2
+
+
+def test_rotate_paged_missing_pages(fa):
+    """A page id outside the pool or past the table: its tokens are left out and flagged, the length stays."""
+    rng = np.random.default_rng(6)
+    table = np.array([[0, 1, 2], [3, -1, 4], [5, 6, 99], [7, 8, 9]], np.int32)
+    lens, n = np.array([14, 14, 14, 30], np.int32), 4
+    t = dev_bf16(normal(rng, 4, n, 3, 64))
+    kp, vp = (torch.zeros(10, 1, 16, 64, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    q_out, dl, err = torch.zeros(4, n, 1, 64, dtype=torch.bfloat16, device="cuda"), dev_i32(lens), dev_i32([0])
+    fa.rotate_append_paged(t[:, :, :1], t[:, :, 1:2], t[:, :, 2:], dev_i32(np.zeros((4, n))), None, q_out, kp, vp, dev_i32(table),
+                           dev_i32([0, 0, 16, 16]), dl, advance=True, err=err, max_len=64)
+    assert int(err.item()) == fa.ERR_APPEND_NO_ROOM
+    assert np.array_equal(dl.cpu().numpy(), [18, 14, 14, 30])
+    used = {(p, s) for p, s in zip(*np.nonzero((host(vp) != 0).any(axis=(1, 3))))}
+    assert used == {(0, 14), (0, 15), (1, 0), (1, 1), (3, 14), (3, 15), (6, 14), (6, 15), (9, 14), (9, 15)}
+
+
+# ------------------------------------------------------------------ 4-bit tiles
+
+GRID = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+
+
+def ref_block(x):
+    """fp64 [..., 32] -> the values that the block's 4-bit form stands for."""
+    amax = np.abs(x).max(-1, keepdims=True)
+    fine = np.isfinite(x).all(-1, keepdims=True)
+    e = np.floor(np.log2(np.where(fine & (amax > 0), amax, 1.0))) - 2
+    e = np.where(amax > 7 * 2.0 ** e, e + 1, e)
+    e = np.clip(np.where(amax > 0, e, -125), -125, 125)
+    y = np.abs(np.where(fine, x, 0.0)) / 2.0 ** e
+    d = np.abs(y[..., None] - GRID)
+    near = d == d.min(-1, keepdims=True)
+    even = near & (np.arange(8) % 2 == 0)
+    code = np.where(near.sum(-1) > 1, even.argmax(-1), near.argmax(-1))
+    z = np.copysign(GRID[code] * 2.0 ** e, x)
+    return np.where(fine, z, np.nan)
+
+
+def ref_pack(k, v):
+    """k, v fp64 [Hkv][L][d] -> the packed values."""
+    h, n, d = k.shape
+    kq = ref_block(k.reshape(h, n, d // 32, 32)).reshape(h, n, d)
+    pad = -n % 32
+    vp = np.concatenate([v, np.zeros((h, pad, d))], 1).transpose(0, 2, 1).reshape(h, d, -1, 32)
+    return kq, ref_block(vp).reshape(h, d, -1).transpose(0, 2, 1)[:, :n]
+
+
+def pack(fa, k, v, pool=None, row=None, **kw):
+    """bf16 bits [Hkv][L][d] -> tiles."""
+    n = -(-k.shape[1] // 128)
+    pool = n if pool is None else pool
+    tiles = torch.full((pool, k.shape[0], 136 * k.shape[2]), 0xA5, dtype=torch.uint8, device="cuda")
+    fa.mx_pack(dev_bf16(k), dev_bf16(v), tiles, tile_row=None if row is None else dev_i32(row), **kw)
+    return tiles
+
+
+def unpack(fa, tiles, L, d, row=None, frm=0, **kw):
+    out = [torch.full((tiles.shape[1], L - frm, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    fa.mx_unpack(tiles, *out, tile_row=None if row is None else dev_i32(row), frm=frm, length=L, **kw)
+    return [host(o) for o in out]
+
+
+@pytest.mark.parametrize("L", [1, 2, 31, 32, 33, 127, 128, 129, 255, 700])
+@pytest.mark.parametrize("hkv,d", [(1, 128), (3, 64), (8, 128)])
+def test_mx_pack_values(fa, hkv, d, L):
+    rng = np.random.default_rng(L * 7 + d)
+    k, v = normal(rng, hkv, L, d), normal(rng, hkv, L, d, scale=3e-3)
+    row = rng.permutation(-(-L // 128) + 2)[: -(-L // 128)]
+    tiles = pack(fa, k, v, pool=len(row) + 2, row=row)
+    for got, want in zip(unpack(fa, tiles, L, d, row=row), ref_pack(value(k), value(v))):
+        assert np.array_equal(value(got), want)
+    left = sorted(set(range(len(row) + 2)) - set(row.tolist()))
+    assert (tiles[left] == 0xA5).all(), "a tile of another prefix was written"
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_mx_pack_of_every_magnitude(fa, d):
+    """Blocks from zeros and subnormals to the largest numbers, ties, signed zeros, infinities and NaN."""
+    rng = np.random.default_rng(d)
+    L, hkv = 640, 2
+    x = rng.standard_normal((2, hkv, L, d)) * 2.0 ** rng.integers(-140, 128, (2, hkv, L // 32, 1, d // 32, 1)).repeat(32, 3).repeat(
+        32, 5).reshape(2, hkv, L, d)
+    x = np.clip(x, -3.38e38, 3.38e38)
+    x[:, 0, :32] = 0
+    x[:, 0, 32:64] = np.resize([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6, -0.25, -0.75, -5, 6.5, -6.5, 0, 7, -7], (32, d))
+    x[:, 0, 64:96] = np.resize([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 6, -0.25, -0.75, -5, 6], (d, 32)).T
+    bits = bits_of(x)
+    bits[:, 1, 5, 3], bits[:, 1, 70, 40], bits[:, 1, 140, 0] = 0x7F80, 0x7FC1, 0xFF80
+    bits[:, 1, 200:232, :] = rng.integers(0, 0x81, (2, 32, d))  # subnormals
+    got = unpack(fa, pack(fa, *bits), L, d)
+    for g, want, name in zip(got, ref_pack(value(bits[0]), value(bits[1])), "kv"):
+        same = (value(g) == want) | (np.isnan(value(g)) & np.isnan(want))
+        assert same.all(), (name, np.argwhere(~same)[:4], value(g)[~same][:4], want[~same][:4])
+
+
+def test_mx_pack_in_parts_and_unpack_of_ranges(fa):
+    rng = np.random.default_rng(8)
+    L, hkv, d = 500, 2, 64
+    k, v = normal(rng, hkv, L, d), normal(rng, hkv, L, d)
+    whole = pack(fa, k, v, pool=5)
+    tiles = torch.full_like(whole, 0xA5)
+    fa.mx_pack(dev_bf16(k[:, :300]), dev_bf16(v[:, :300]), tiles)
+    fa.mx_pack(dev_bf16(k[:, 256:]), dev_bf16(v[:, 256:]), tiles, frm=256)  # the last tile again, and the new ones
+    assert torch.equal(tiles, whole)
+    fa.mx_pack(dev_bf16(k[:, 256:]), dev_bf16(v[:, 256:]), tiles, frm=256, length=400)  # a source with more rows
+    kw, vw = unpack(fa, tiles, 400, d)
+    for frm, to in ((0, 1), (1, 400), (127, 129), (128, 256), (399, 400), (130, 140), (5, 5)):
+        gk, gv = unpack(fa, tiles, to, d, frm=frm)
+        assert np.array_equal(gk, kw[:, frm:to]) and np.array_equal(gv, vw[:, frm:to]), (frm, to)
+
+
+def test_mx_tile_ids_outside_the_pool(fa):
+    rng = np.random.default_rng(9)
+    k, v = normal(rng, 2, 500, 128), normal(rng, 2, 500, 128)
+    good = pack(fa, k, v)
+    err = dev_i32([0])
+    tiles = pack(fa, k, v, pool=4, row=[0, -1, 4, 3], err=err)
+    assert int(err.item()) == fa.ERR_BAD_PAGE
+    assert torch.equal(tiles[0], good[0]) and torch.equal(tiles[3], good[3]) and (tiles[1:3] == 0xA5).all()
+    err.zero_()
+    got = unpack(fa, good, 500, 128, row=[0, 1, 2 ** 31 - 1, 3], err=err)
+    want = unpack(fa, good, 500, 128)
+    assert int(err.item()) == fa.ERR_BAD_PAGE
+    for g, w in zip(got, want):
+        w[:, 256:384] = 0
+        assert np.array_equal(g, w)
+
+
+# ------------------------------------------------------------------ decode over 4-bit tiles
+
+class Mx:
+    """A decode over several groups: inputs, device tensors and the oracle's answer over the unpacked values."""
+
+    def __init__(self, fa, seed, hq, hkv, d, groups, prefixes, lens, cap=None, table=False, scale=0.0, blocks=0, max_suffix=None,
+                 kscale=1.0):
+        rng = np.random.default_rng(seed)
+        self.fa, self.hq, self.hkv, self.d = fa, hq, hkv, d
+        self.start = np.concatenate([[0], np.cumsum(groups)])
+        S = int(self.start[-1])
+        self.prefixes, self.lens = prefixes, np.array(lens, np.int32)
+        self.cap = max(1, int(self.lens.max(initial=0))) if cap is None else cap
+        self.scale = scale or 1 / np.sqrt(d)
+        self.q = normal(rng, S, hq, d)
+        self.sk, self.sv = normal(rng, S, hkv, self.cap, d, scale=kscale), normal(rng, S, hkv, self.cap, d)
+        for s in range(S):  # what lies behind a suffix is never read
+            self.sk[s, :, self.lens[s]:] = self.sv[s, :, self.lens[s]:] = 0x7FC0
+        counts = [-(-n // 128) for n in prefixes]
+        total, ids = sum(counts), np.arange(sum(counts))
+        self.table = None
+        if table:
+            ids = rng.permutation(total + 3)[:total]
+            self.table = np.full((len(prefixes), max(counts) + 1), -5, np.int32)
+        pool = total + (3 if table else 0)
+        self.tiles = torch.full((max(pool, 1), hkv, 136 * d), 0xFF, dtype=torch.uint8, device="cuda")
+        self.pk, self.pv, at = [], [], 0
+        for t, n in enumerate(prefixes):
+            row = ids[at: at + counts[t]]
+            at += counts[t]
+            if table:
+                self.table[t, : counts[t]] = row
+            if n:
+                fa.mx_pack(dev_bf16(normal(rng, hkv, n, d, scale=kscale)), dev_bf16(normal(rng, hkv, n, d)), self.tiles,
+                           tile_row=dev_i32(row))
+                kk, vv = unpack(fa, self.tiles, n, d, row=row)
+            else:
+                kk = vv = np.zeros((hkv, 0, d), np.uint16)
+            self.pk.append(kk)
+            self.pv.append(vv)
+        self.plan = fa.Plan.mx_plan(hq, hkv, d, self.start, prefixes, self.cap, self.cap if max_suffix is None else max_suffix,
+                                    n_pool_tiles=pool, max_tiles=None if self.table is None else self.table.shape[1],
+                                    softmax_scale=scale, blocks=blocks)
+        self.dev = dict(q=dev_bf16(self.q), tiles=self.tiles, suffix_k=dev_bf16(self.sk), suffix_v=dev_bf16(self.sv),
+                        suffix_len=dev_i32(self.lens))
+        self.dev_table = None if self.table is None else dev_i32(self.table)
+
+    def outs(self):
+        S = len(self.lens)
+        return (torch.full((S, self.hq, self.d), float("nan"), device="cuda"), torch.full((S, self.hq), float("nan"), device="cuda"))
+
+    def decode(self, stream=None):
+        out, lse = self.outs()
+        self.plan.decode_mx(out=out, out_lse=lse, tile_table=self.dev_table, stream=stream, **self.dev)
+        torch.cuda.synchronize()
+        return out.cpu().numpy(), lse.cpu().numpy()
+
+    def reference(self, sk=None, sv=None, lens=None):
+        sk, sv, lens = self.sk if sk is None else sk, self.sv if sv is None else sv, self.lens if lens is None else lens
+        outs = []
+        for t, n in enumerate(self.prefixes):
+            a, b = self.start[t], self.start[t + 1]
+            outs.append(oracle.decode_contig(self.q[a:b], self.pk[t], self.pv[t], sk[a:b], sv[a:b], lens[a:b].astype(np.int32), self.scale))
+        return [np.concatenate(x) for x in zip(*outs)]
+
+    def bounds(self, ref_lse, sk=None, sv=None, lens=None):
+        """Tolerances of out and lse from the largest score terms and values of the case."""
+        sk, sv, lens = self.sk if sk is None else sk, self.sv if sv is None else sv, self.lens if lens is None else lens
+        qa, G = np.abs(value(self.q)), self.hq // self.hkv
+        S, vmax = 0.0, 0.0
+        for t in range(len(self.prefixes)):
+            for s in range(self.start[t], self.start[t + 1]):
+                ka = np.abs(np.concatenate([value(self.pk[t]), value(sk[s, :, : lens[s]])], 1))
+                for h in range(self.hq):
+                    S = max(S, (ka[h // G] @ qa[s, h]).max(initial=0.0) * self.scale)
+                vmax = max(vmax, np.abs(value(self.pv[t])).max(initial=0.0), np.abs(value(sv[s, :, : lens[s]])).max(initial=0.0))
+        S += np.abs(np.where(np.isfinite(ref_lse), ref_lse, 0)).max()
+        rel = (self.d + 4) * U * S
+        return vmax * (2 * rel + 2.0 ** -20 + 2.0 ** -19), rel + 2.0 ** -19
+
+    def check(self, out, lse, what="", **over):
+        o, l = self.reference(**over)
+        tol, tol_l = self.bounds(l, **over)
+        assert np.array_equal(np.isneginf(lse), np.isneginf(l)), what
+        e, el = np.abs(out - o).max(), np.abs(np.where(np.isneginf(l), 0, lse - np.where(np.isneginf(l), 0, l))).max()
+        print(f"[mx] {what} out {e:.2e} of {tol:.2e}, lse {el:.2e} of {tol_l:.2e}", flush=True)
+        assert e <= tol and el <= tol_l, (what, e, tol, el, tol_l)
+
+
+MX = [
+    # hq, hkv, d, groups, prefixes, lens, more
+    (1, 1, 128, [1], [1], [0], {}),
+    (1, 1, 64, [1], [1], [1], {}),
+    (8, 2, 64, [5], [512], [0, 64, 31, 32, 33], {}),
+    (8, 2, 128, [5], [127], [1, 0, 65, 32, 200], {}),
+    (5, 1, 128, [3], [129], [4, 5, 6], dict(blocks=1)),
+    (40, 8, 128, [5], [2000], [513, 0, 77, 1000, 3], {}),
+    (40, 8, 128, [5], [4096 + 17], [100, 200, 300, 0, 1], dict(blocks=3000)),
+    (24, 3, 64, [6], [1000], [9, 8, 7, 0, 40, 640], dict(table=True)),
+    (64, 8, 128, [5], [900], [50, 60, 0, 10, 11], dict(scale=0.05)),
+    (8, 1, 128, [8], [300], [0, 1, 2, 3, 31, 32, 33, 100], {}),
+    (64, 1, 64, [1], [300], [70], {}),
+    (64, 1, 128, [1], [0], [70], {}),
+    (48, 1, 128, [1], [400], [33], {}),
+    (7, 7, 128, [2, 1, 3], [300, 0, 5], [0, 9, 40, 3, 0, 2], dict(table=True)),
+    (32, 8, 128, [5, 2, 1, 5], [3000, 128, 1, 640], [1, 2, 3, 4, 5, 0, 0, 400, 31, 32, 33, 34, 35], dict(table=True)),
+    (16, 2, 64, [3, 3], [200, 2000], [0, 0, 0, 0, 0, 0], dict(max_suffix=0)),
+    (10, 2, 128, [5], [23017], [100, 900, 450, 33, 0], dict(cap=3000, kscale=2.0)),
+]
+
+
+@pytest.mark.parametrize("case", range(len(MX)))
+def test_mx_decode(fa, case):
+    hq, hkv, d, groups, prefixes, lens, more = MX[case]
+    print(f"[mx] case {case}: {MX[case]}", flush=True)
+    m = Mx(fa, 200 + case, hq, hkv, d, groups, prefixes, lens, **more)
+    out, lse = m.decode()
+    m.check(out, lse, f"case {case}")
+    again, lse2 = m.decode()
+    assert np.array_equal(out, again) and np.array_equal(lse, lse2), "not repeatable"
+    assert m.plan.device_error() == 0
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_mx_decode_random(fa, seed):
+    rng = np.random.default_rng(900 + seed)
+    hkv, d, G = int(rng.choice([1, 2, 3, 8])), int(rng.choice([64, 128])), int(rng.choice([1, 2, 4, 5, 7, 8, 16]))
+    groups = [int(rng.integers(1, 64 // G + 1)) for _ in range(rng.integers(1, 4))]
+    groups = [min(g, 8) for g in groups]
+    prefixes = [int(2 ** rng.uniform(0, 12)) for _ in groups]
+    lens = rng.integers(0, int(rng.choice([2, 40, 700])), sum(groups))
+    m = Mx(fa, seed, hkv * G, hkv, d, groups, prefixes, lens, table=bool(rng.integers(2)), blocks=int(rng.choice([0, 0, 1, 37, 999])),
+           cap=int(lens.max()) + int(rng.integers(1, 900)))
+    m.check(*m.decode(), f"seed {seed} G {G} hkv {hkv} d {d} groups {groups} prefixes {prefixes}")
+
+
+@pytest.mark.parametrize("d,hkv,G", [(128, 8, 5), (64, 2, 4)])
+def test_mx_step_appends_and_decodes(fa, d, hkv, G):
+    lens = [0, 31, 32, 100, 7]
+    m = Mx(fa, 31, hkv * G, hkv, d, [3, 2], [700, 260], lens, cap=105)
+    rng = np.random.default_rng(32)
+    for step in range(3):
+        kn, vn = normal(rng, 5, hkv, d), normal(rng, 5, hkv, d)
+        out, lse = m.outs()
+        m.plan.step_mx(m.dev["q"], dev_bf16(kn), dev_bf16(vn), m.tiles, m.dev["suffix_k"], m.dev["suffix_v"], m.dev["suffix_len"],
+                       out, lse)
+        for s in range(5):
+            m.sk[s, :, m.lens[s]], m.sv[s, :, m.lens[s]] = kn[s], vn[s]
+        m.lens = m.lens + 1
+        assert np.array_equal(m.dev["suffix_len"].cpu().numpy(), m.lens)
+        assert np.array_equal(host(m.dev["suffix_k"]), m.sk) and np.array_equal(host(m.dev["suffix_v"]), m.sv)
+        m.check(out.cpu().numpy(), lse.cpu().numpy(), f"step {step}")
+    # append, then decode
+    kn, vn = normal(rng, 5, hkv, d), normal(rng, 5, hkv, d)
+    m.plan.append(dev_bf16(kn), dev_bf16(vn), m.dev["suffix_k"], m.dev["suffix_v"], m.dev["suffix_len"])
+    for s in range(5):
+        m.sk[s, :, m.lens[s]], m.sv[s, :, m.lens[s]] = kn[s], vn[s]
+    m.lens = m.lens + 1
+    m.check(*m.decode(), "append")
+    assert m.plan.device_error() == 0
+
+
+def test_mx_lengths_are_clamped_and_full_suffixes_flagged(fa):
+    m = Mx(fa, 33, 8, 2, 128, [5], [200], [5, 6, 7, 8, 10], cap=10)
+    m.dev["suffix_len"].copy_(dev_i32([5, -3, 7, 8, 10]))
+    out, lse = m.decode()
+    m.check(out, lse, "clamped", lens=np.array([5, 0, 7, 8, 10]))
+    assert m.plan.device_error() == fa.ERR_SUFFIX_CLAMPED
+    m.dev["suffix_len"].copy_(dev_i32([5, 6, 7, 8, 10]))
+    kn = dev_bf16(normal(np.random.default_rng(1), 5, 2, 128))
+    out, lse = m.outs()
+    m.plan.step_mx(m.dev["q"], kn, kn, m.tiles, m.dev["suffix_k"], m.dev["suffix_v"], m.dev["suffix_len"], out, lse)
+    assert m.plan.device_error() == fa.ERR_APPEND_NO_ROOM
+    assert np.array_equal(m.dev["suffix_len"].cpu().numpy(), [6, 7, 8, 9, 10])
+
+
+def test_mx_sequences_without_keys(fa):
+    m = Mx(fa, 34, 10, 2, 128, [2, 1], [0, 0], [0, 3, 0], cap=8)
+    out, lse = m.decode()
+    assert (out[[0, 2]] == 0).all() and np.isneginf(lse[[0, 2]]).all()
+    m.check(out, lse, "empty")
+
+
+def test_mx_bad_tile_ids_count_as_zeros(fa):
+    m = Mx(fa, 35, 8, 2, 128, [3], [500], [9, 0, 40], table=True)
+    m.table[0, 1], m.table[0, 3] = -1, 2 ** 31 - 1
+    m.dev_table = dev_i32(m.table)
+    for x in (m.pk, m.pv):
+        x[0] = x[0].copy()
+        x[0][:, 128:256] = x[0][:, 384:500] = 0
+    m.check(*m.decode(), "bad ids")
+    assert m.plan.device_error() == fa.ERR_BAD_PAGE
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_mx_non_finite_values(fa, d):
+    """A NaN in one sequence's suffix reaches only that sequence; a NaN block of V only its channel; of K every row."""
+    m = Mx(fa, 36, 10, 2, d, [5], [300], [40, 50, 60, 0, 33])
+    out, lse = m.decode()
+    for which in ("suffix_k", "suffix_v"):
+        good = m.dev[which].clone()
+        m.dev[which][2, 1, 45, 7] = float("nan")
+        o2, l2 = m.decode()
+        m.dev[which].copy_(good)
+        rows = np.zeros(out.shape[:2], bool)
+        rows[2, 5:] = True
+        assert np.array_equal(o2[~rows], out[~rows]) and np.array_equal(l2[~rows], lse[~rows])
+        assert np.isnan(o2[rows]).any(-1).all()
+        if which == "suffix_k":
+            assert np.isnan(o2[rows]).all()
+    rng = np.random.default_rng(37)
+    k, v = normal(rng, 2, 300, d), normal(rng, 2, 300, d)
+    v[1, 70, 9] = 0x7FC0
+    fa.mx_pack(dev_bf16(k), dev_bf16(v), m.tiles)
+    o3, _ = m.decode()
+    nan = np.isnan(o3)
+    assert nan[:, 5:, 9].all() and nan.sum() == 25
+    k[0, 299, 0] = 0x7F80
+    fa.mx_pack(dev_bf16(k), dev_bf16(v), m.tiles)
+    o4, _ = m.decode()
+    assert np.isnan(o4[:, :5]).all() and np.array_equal(o4[:, 5:], o3[:, 5:], equal_nan=True)
+
+
+@pytest.mark.parametrize("d,hkv,G,N", [(128, 2, 5, 5), (64, 2, 4, 3), (128, 1, 12, 4), (128, 1, 8, 8)])
+def test_mx_value_scales_of_every_size(fa, d, hkv, G, N):
+    """V blocks whose scales fp16 does not hold (tiles of them alone, mixed with others, behind others, in one channel only):
+    every channel is held to the bound of its own values."""
+    rng = np.random.default_rng(41)
+    L = 1300
+    m = Mx(fa, 42, G * hkv, hkv, d, [N], [L], rng.integers(0, 90, N))
+    k = normal(rng, hkv, L, d)
+    exps = np.zeros((L, d))
+    exps[128:256], exps[256:384] = 40, -40
+    exps[384:400, 5], exps[512:640] = 12, rng.integers(-100, 100, (1, d))
+    exps[700:, ::3] += rng.integers(-30, 30, (600, 1)) // 32 * 20
+    for flat in (False, True):
+        v = bits_of(rng.standard_normal((hkv, L, d)) * 2.0 ** (-50 if flat else exps))
+        fa.mx_pack(dev_bf16(k), dev_bf16(v), m.tiles)
+        m.pk[0], m.pv[0] = unpack(fa, m.tiles, L, d)
+        if flat:
+            m.lens[:] = 0
+            m.dev["suffix_len"].zero_()
+        out, lse = m.decode()
+        o, l = m.reference()
+        tol, tol_l = m.bounds(l)
+        tol /= np.abs(value(m.pv[0])).max(initial=0) if flat else max(np.abs(value(m.pv[0])).max(), np.nanmax(np.abs(value(m.sv))))
+        vmax = np.abs(value(m.pv[0])).max(1)  # per KV head and channel
+        if not flat:
+            vmax = np.maximum(vmax, np.nanmax(np.abs(value(m.sv)), axis=(0, 2)))
+        tol = tol * vmax.repeat(G, 0)[None]
+        assert (np.abs(out - o) <= tol).all(), (flat, np.max(np.abs(out - o) / tol))
+        assert np.abs(lse - l).max() <= tol_l
+
+
+def test_mx_scores_far_apart(fa):
+    """Keys whose scores grow along the prefix, so that the reference moves in every tile, and large negative ones."""
+    m = Mx(fa, 38, 4, 1, 128, [2], [900], [40, 3])
+    q = np.abs(value(m.q)) * 0.5
+    m.q = bits_of(q)
+    rng = np.random.default_rng(38)
+    ramp = np.linspace(-3, 3, 900)[None, :, None] * (0.5 + rng.random((1, 900, 128)))
+    fa.mx_pack(dev_bf16(bits_of(ramp)), dev_bf16(normal(rng, 1, 900, 128)), m.tiles)
+    m.pk[0], m.pv[0] = unpack(fa, m.tiles, 900, 128)
+    m.dev["q"] = dev_bf16(m.q)
+    m.check(*m.decode(), "ramp")
+
+
+def test_mx_tiles_past_4_gib(fa):
+    """Tile ids and suffix rows whose byte offsets pass 32 bits."""
+    hkv, d, n = 8, 128, 33000
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    m = Mx(fa, 39, 16, hkv, d, [2], [300], [40, 30], table=True)
+    big = torch.zeros(n, hkv, 136 * d, dtype=torch.uint8, device="cuda")
+    row = [n - 1, 0, n - 2]
+    for i, r in enumerate(row):
+        big[r] = m.tiles[int(m.table[0, i])]
+    cap = 1_100_000
+    plan = fa.Plan.mx_plan(16, hkv, d, [0, 2], [300], cap, 64, n_pool_tiles=n)
+    sk, sv = (torch.zeros(2, hkv, cap, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    sk[:, :, :40], sv[:, :, :40] = m.dev["suffix_k"], m.dev["suffix_v"]
+    out, lse = m.outs()
+    plan.decode_mx(m.dev["q"], big, sk, sv, m.dev["suffix_len"], out, lse, tile_table=dev_i32([row]))
+    m.check(out.cpu().numpy(), lse.cpu().numpy(), "far")
+    assert plan.device_error() == 0
+    del sk, sv
+    kk, vv = (torch.full((hkv, 130, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    fa.mx_unpack(big, kk, vv, tile_row=dev_i32(row), length=130)
+    assert np.array_equal(host(kk), m.pk[0][:, :130]) and np.array_equal(host(vv), m.pv[0][:, :130])
+
+
+def test_mx_plans_refuse_other_calls(fa):
+    m = Mx(fa, 40, 8, 2, 64, [2], [100], [3, 4])
+    out, lse = m.outs()
+    d = m.dev
+    pk = torch.zeros(2, 100, 64, dtype=torch.bfloat16, device="cuda")
+    for call in (lambda: m.plan.decode(d["q"], pk, pk, d["suffix_k"], d["suffix_v"], d["suffix_len"], out, lse),
+                 lambda: m.plan.partials(d["q"], pk, pk, d["suffix_k"], d["suffix_v"], d["suffix_len"], out, lse),
+                 lambda: m.plan.step(d["q"], d["q"], d["q"], pk, pk, d["suffix_k"], d["suffix_v"], d["suffix_len"], out, lse),
+                 lambda: m.plan.slots(m.lens)):
+        with pytest.raises(fa.FkaError, match="4-bit"):
+            call()
+    with pytest.raises(fa.FkaError, match="paged|contiguous"):
+        m.plan.decode_paged(d["q"], pk, pk, d["suffix_len"], d["suffix_len"], out, lse)
+    with pytest.raises(fa.FkaError, match="prefill"):
+        m.plan.prefill(d["q"], pk, pk, d["suffix_k"], d["suffix_v"], d["suffix_len"], out, lse)
+    plain = fa.Plan.contig(8, 2, 64, 2, 100, 4, 4)
+    with pytest.raises(fa.FkaError, match="4-bit"):
+        plain.decode_mx(d["q"], m.tiles, d["suffix_k"], d["suffix_v"], d["suffix_len"], out, lse)
+    assert m.plan.info().n_blocks >= 1 and m.plan.info().workspace_bytes > 0
+
+
+# ------------------------------------------------------------------ key weights
+
+def ref_weights(q, lse, k, scale):
+    """fp64: (sum of weights [Hkv][L], largest score term sum)."""
+    R, hq, d = q.shape
+    hkv = k.shape[0]
+    G, S = hq // hkv, 0.0
+    w = np.zeros(k.shape[:2])
+    for g in range(hkv):
+        for r in range(R):
+            for h in range(g * G, (g + 1) * G):
+                if np.isneginf(lse[r, h]):
+                    continue
+                w[g] += np.exp(scale * (k[g] @ q[r, h]) - lse[r, h])
+                S = max(S, scale * (np.abs(k[g]) @ np.abs(q[r, h])).max() + abs(lse[r, h]))
+    return w, S
+
+
+@pytest.mark.parametrize("hq,hkv,d,R,L,decay", [
+    (1, 1, 128, 1, 1, 0.0), (8, 2, 64, 5, 63, 0.5), (40, 8, 128, 5, 1000, 0.9), (5, 1, 128, 1, 257, 1.0), (8, 8, 64, 33, 64, 0.0),
+    (6, 3, 128, 0, 100, 0.25), (16, 1, 128, 64, 700, 0.0), (14, 2, 64, 17, 4097, 2.0)])
+def test_key_weights(fa, hq, hkv, d, R, L, decay):
+    rng = np.random.default_rng(hq * 1000 + L)
+    q, k = normal(rng, R, hq, d), normal(rng, hkv, L + 3, d)
+    k[:, L:] = 0x7FC0  # rows behind the prefix
+    scale = 1 / np.sqrt(d)
+    x = np.einsum("rghd,gld->rghl", value(q).reshape(R, hkv, hq // hkv, d), value(k[:, :L])) * scale
+    lse = (np.log(np.exp(x).sum(-1)) + 0.1).reshape(R, hq).astype(np.float32)
+    if R > 4:
+        lse[3, 0] = -np.inf  # a row without keys
+    old = rng.random((hkv, L + 5)).astype(np.float32)
+    if decay == 0:
+        old[:, :L] = np.nan  # not read
+    w = torch.from_numpy(old.copy()).cuda()
+    fa.key_weights(dev_bf16(q), torch.from_numpy(lse).cuda(), dev_bf16(k), w, length=L, decay=decay)
+    got = w.cpu().numpy()
+    assert np.array_equal(got[:, L:], old[:, L:])
+    new, S = ref_weights(value(q), lse.astype(np.float64), value(k[:, :L]), scale)
+    want = new + (decay * old[:, :L].astype(np.float64) if decay else 0)
+    # each weight's exponent, the exponential (2^-21), the sum of R G terms, the decay
+    tol = new * ((d + 4) * U * S + 2.0 ** -21 + (R * hq / hkv + 2) * 2 * U) + 4 * U * want + 1e-36
+    err = np.abs(got[:, :L] - want)
+    print(f"[weights] worst {np.max(err / tol):.3f} of the bound", flush=True)
+    assert (err <= tol).all()
+    w2 = torch.from_numpy(old.copy()).cuda()
+    fa.key_weights(dev_bf16(q), torch.from_numpy(lse).cuda(), dev_bf16(k), w2, length=L, decay=decay)
+    assert np.array_equal(w2.cpu().numpy(), got, equal_nan=True)
+
+
+def test_key_weights_non_finite(fa):
+    rng = np.random.default_rng(50)
+    q, k = normal(rng, 3, 4, 64), normal(rng, 2, 200, 64)
+    lse = np.full((3, 4), 8.0, np.float32)
+    base = torch.zeros(2, 200, device="cuda")
+    fa.key_weights(dev_bf16(q), torch.from_numpy(lse).cuda(), dev_bf16(k), base)
+    k[1, 77, 5] = 0x7FC0
+    w = torch.zeros(2, 200, device="cuda")
+    fa.key_weights(dev_bf16(q), torch.from_numpy(lse).cuda(), dev_bf16(k), w)
+    got, want = w.cpu().numpy(), base.cpu().numpy()
+    assert np.isnan(got[1, 77]) and np.isnan(got).sum() == 1
+    assert np.array_equal(np.delete(got[1], 77), np.delete(want[1], 77)) and np.array_equal(got[0], want[0])
+    lse[:, 2:] = -np.inf  # no row of the second KV head has keys
+    w.fill_(3.0)
+    fa.key_weights(dev_bf16(q), torch.from_numpy(lse).cuda(), dev_bf16(normal(rng, 2, 200, 64)), w)
+    assert (w[1] == 0).all() and (w[0] > 0).all()
+
+
+def test_key_weights_past_4_gib(fa):
+    if torch.cuda.mem_get_info()[0] < 20 << 30:
+        pytest.skip("needs 20 GiB")
+    rng = np.random.default_rng(51)
+    k = torch.zeros(8, 2_300_000, 128, dtype=torch.bfloat16, device="cuda")
+    few = dev_bf16(normal(rng, 8, 100, 128))
+    k[:, :100] = few
+    q, lse = dev_bf16(normal(rng, 2, 16, 128)), torch.full((2, 16), 9.0, device="cuda")
+    a, b = torch.zeros(8, 100, device="cuda"), torch.zeros(8, 100, device="cuda")
+    fa.key_weights(q, lse, k, a, length=100)
+    fa.key_weights(q, lse, few, b)
+    assert torch.equal(a, b) and (a > 0).all()
+
+
+# ------------------------------------------------------------------ shortening
+
+def ref_evict(w, keep, first, last):
+    L = w.shape[1]
+    out = []
+    for row in w:
+        mid = np.arange(first, L - last)
+        key = np.where(np.isnan(row[mid]), np.inf, row[mid].astype(np.float64))
+        nan = np.isnan(row[mid])
+        order = np.lexsort((mid, -key, ~nan))  # NaN first, then the largest, then the lowest position
+        out.append(np.sort(np.concatenate([np.arange(first), np.arange(L - last, L), mid[order[: keep - first - last]]])))
+    return np.array(out)
+
+
+def run_evict(fa, w, keep, first, last, d=64, cap=None, seed=0):
+    rng = np.random.default_rng(seed)
+    hkv, L = w.shape
+    cap = L if cap is None else cap
+    k, v = (rng.integers(0, 2 ** 16, (hkv, cap, d)).astype(np.uint16) for _ in "kv")
+    index = torch.full((hkv, keep), -9, dtype=torch.int32, device="cuda")
+    ko, vo = (torch.zeros(hkv, keep, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    wo = torch.zeros(hkv, keep, device="cuda")
+    work = torch.full((fa._lib.fka_evict_bytes(hkv, L),), 0xEE, dtype=torch.uint8, device="cuda")
+    fa.evict(dev_bf16(k), dev_bf16(v), torch.from_numpy(w).cuda(), index, ko, vo, wo, n_first=first, n_last=last, length=L,
+             workspace=work)
+    want = ref_evict(w, keep, first, last)
+    got = index.cpu().numpy()
+    assert np.array_equal(got, want), (np.argwhere(got != want)[:3], got[got != want][:3], want[got != want][:3])
+    head = np.arange(hkv)[:, None]
+    assert np.array_equal(host(ko), k[head, want]) and np.array_equal(host(vo), v[head, want])
+    assert np.array_equal(wo.cpu().numpy().view(np.uint32), w[head, want].view(np.uint32))
+
+
+@pytest.mark.parametrize("L,keep,first,last", [(1, 1, 0, 0), (1, 0, 0, 0), (2, 1, 0, 0), (5, 5, 2, 3), (300, 100, 4, 30), (300, 34, 4, 30),
+                                               (2047, 1, 0, 0), (2048, 2047, 0, 0), (2049, 1024, 1, 0), (4097, 2050, 0, 2049),
+                                               (4500, 3000, 2500, 100), (9001, 700, 3, 5)])
+@pytest.mark.parametrize("hkv,d", [(1, 64), (3, 128)])
+def test_evict(fa, hkv, d, L, keep, first, last):
+    rng = np.random.default_rng(L + keep)
+    run_evict(fa, np.exp(2 * rng.standard_normal((hkv, L))).astype(np.float32), keep, first, last, d=d, cap=L + 3)
+
+
+@pytest.mark.parametrize("kind", ["zeros", "few values", "signs", "close", "special", "equal at the border"])
+def test_evict_ties_and_orders(fa, kind):
+    rng = np.random.default_rng(60)
+    hkv, L = 2, 5000
+    w = {"zeros": lambda: np.zeros((hkv, L)), "few values": lambda: rng.integers(0, 4, (hkv, L)) * 0.25,
+         "signs": lambda: rng.standard_normal((hkv, L)), "close": lambda: 1 + rng.integers(0, 40, (hkv, L)) * 2.0 ** -23,
+         "special": lambda: rng.choice([0.0, -0.0, np.inf, -np.inf, np.nan, 1e-45, -1e-45, 3e38], (hkv, L)),
+         "equal at the border": lambda: np.where(np.arange(L) % 3 == 0, 2.0, 1.0)[None].repeat(hkv, 0)}[kind]().astype(np.float32)
+    if kind == "special":
+        w.view(np.uint32)[0, 7] = 0xFFC00001  # a NaN with its sign set
+    for keep in (1, 1666, 1667, 1668, 2500, 4999):
+        run_evict(fa, w, keep, 0, 0)
+    run_evict(fa, w, 3000, 100, 900)
+
+
+def test_evict_long(fa):
+    rng = np.random.default_rng(61)
+    run_evict(fa, np.exp(1.5 * rng.standard_normal((2, 131072))).astype(np.float32), 32768, 4, 512)
+
+
+# ------------------------------------------------------------------ together
+
+def test_a_turn_from_prompt_to_step(fa):
+    """A context is written as a prefix (norm and rotation), scored by an instruction's queries, shortened, packed, and read by
+    decode steps whose new tokens are rotated and stored: every stage against its definition in 64 bits over what the stage before
+    it left, the last one over the values that the tiles stand for."""
+    rng = np.random.default_rng(70)
+    N, hq, hkv, d, L, keep, cap = 5, 20, 4, 128, 1500, 700, 40
+    freq = 1e6 ** (-np.arange(0, d, 2) / d)
+    fr = torch.from_numpy(freq).cuda()
+    w = bits_of(1 + 0.1 * rng.standard_normal(d))
+    wd = dev_bf16(w)
+    # the prefix
+    rows = dev_bf16(normal(rng, 1, L, (hq + 2 * hkv) * d))
+    cut = lambda t: [t[..., a * d: b * d].unflatten(-1, (-1, d)) for a, b in ((0, hq), (hq, hq + hkv), (hq + hkv, hq + 2 * hkv))]  # noqa: E731
+    q, k, v = cut(rows)
+    pk, pv = (torch.zeros(1, hkv, L, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    q_all = torch.empty(1, L, hq, d, dtype=torch.bfloat16, device="cuda")
+    fa.rotate_append(q, k, v, dev_i32(np.arange(L)[None]), fr, q_all, pk, pv, q_weight=wd, k_weight=wd)
+    x = value(host(rows))
+    kx = x[..., hq * d: (hq + hkv) * d].reshape(1, L, hkv, d)
+    close_rotated(host(pk).transpose(0, 2, 1, 3), ref_rotate(kx, value(w), np.arange(L)[None].astype(float), freq, d, False, 1e-6), "k")
+    # the last 16 tokens' queries over the prefix: a prefill of one sequence gives their lse
+    R = 16
+    win = q_all[:, -R:].contiguous()
+    pre = fa.Plan.prefill_plan(hq, hkv, d, 1, R, L - R, R, R)
+    out, lse = torch.empty(1, R, hq, d, device="cuda"), torch.empty(1, R, hq, device="cuda")
+    body = [t[0, :, : L - R].contiguous() for t in (pk, pv)]
+    tail = [t[:, :, L - R:].contiguous() for t in (pk, pv)]
+    pre.prefill(win, *body, *tail, dev_i32([0]), out, lse)
+    weights = torch.empty(hkv, L - R, device="cuda")
+    fa.key_weights(win[0], lse[0], body[0], weights)
+    want, S = ref_weights(value(host(win))[0], lse[0].cpu().numpy().astype(np.float64), value(host(body[0])), d ** -0.5)
+    assert (np.abs(weights.cpu().numpy() - want) <= want * ((d + 4) * U * S + 2.0 ** -20 + R * hq / hkv * 2 * U)).all()
+    # shortened (the window itself stays) and packed
+    index = torch.empty(hkv, keep, dtype=torch.int32, device="cuda")
+    ko, vo = (torch.empty(hkv, keep, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    fa.evict(*body, weights, index, ko, vo, n_first=4, n_last=64, workspace=fa.evict_workspace(hkv, L))
+    at = ref_evict(weights.cpu().numpy(), keep, 4, 64)
+    assert np.array_equal(index.cpu().numpy(), at)
+    assert np.array_equal(host(ko), host(body[0])[np.arange(hkv)[:, None], at])
+    tiles = torch.empty(6, hkv, 136 * d, dtype=torch.uint8, device="cuda")
+    fa.mx_pack(ko, vo, tiles)
+    kk, vv = unpack(fa, tiles, keep, d)
+    for got, ref in zip((kk, vv), ref_pack(value(host(ko)), value(host(vo)))):
+        assert np.array_equal(value(got), ref)
+    # decode steps of five branches: every one rotates its token, stores it and decodes
+    plan = fa.Plan.mx_plan(hq, hkv, d, [0, N], [keep], cap, cap, n_pool_tiles=6)
+    sk, sv = (torch.zeros(N, hkv, cap, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    lens = dev_i32([0] * N)
+    m = Mx.__new__(Mx)
+    m.fa, m.hq, m.hkv, m.d, m.scale, m.prefixes, m.start, m.pk, m.pv = fa, hq, hkv, d, d ** -0.5, [keep], np.array([0, N]), [kk], [vv]
+    for step in range(3):
+        q, k, v = cut(dev_bf16(normal(rng, N, 1, (hq + 2 * hkv) * d)))
+        qr = torch.empty(N, 1, hq, d, dtype=torch.bfloat16, device="cuda")
+        fa.rotate_append(q, k, v, dev_i32(np.full((N, 1), L + step)), fr, qr, sk, sv, lens, q_weight=wd, k_weight=wd, advance=True)
+        out, lse = torch.empty(N, hq, d, device="cuda"), torch.empty(N, hq, device="cuda")
+        plan.decode_mx(qr[:, 0], tiles, sk, sv, lens, out, lse)
+        assert np.array_equal(lens.cpu().numpy(), [step + 1] * N)
+        m.q, m.sk, m.sv, m.lens = host(qr)[:, 0], host(sk), host(sv), lens.cpu().numpy()
+        m.check(out.cpu().numpy(), lse.cpu().numpy(), f"turn, step {step}")
+    assert plan.device_error() == 0
+
+
+def test_captured_and_replayed_on_another_stream(fa):
+    """A decode step (rotation, store, decode over tiles, weights, shortening) captured into a graph on a side stream and replayed,
+    with eager work between the replays: every replay gives the eager calls' bits."""
+    rng = np.random.default_rng(71)
+    N, hq, hkv, d, cap = 3, 8, 2, 64, 60
+    m = Mx(fa, 72, hq, hkv, d, [N], [400], [10, 20, 30], cap=cap)
+    t = dev_bf16(normal(rng, N, 1, hq + 2 * hkv, d))
+    freq, pos = torch.full((32,), 0.3, dtype=torch.float64, device="cuda"), dev_i32(np.full((N, 1), 421))
+    pk = dev_bf16(m.pk[0])
+    pv = dev_bf16(m.pv[0])
+    qr = torch.empty(N, 1, hq, d, dtype=torch.bfloat16, device="cuda")
+    out, lse = m.outs()
+    weights = torch.zeros(hkv, 400, device="cuda")
+    index = torch.empty(hkv, 100, dtype=torch.int32, device="cuda")
+    ko, vo = (torch.empty(hkv, 100, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    tiles2, work = torch.zeros(1, hkv, 136 * d, dtype=torch.uint8, device="cuda"), fa.evict_workspace(hkv, 400)
+    k_back, v_back = torch.empty_like(ko), torch.empty_like(vo)
+    lens = m.dev["suffix_len"]
+
+    def step():
+        fa.rotate_append(t[:, :, :hq], t[:, :, hq: hq + hkv], t[:, :, hq + hkv:], pos, freq, qr, m.dev["suffix_k"], m.dev["suffix_v"],
+                         lens, advance=True)
+        m.plan.decode_mx(qr[:, 0], m.tiles, m.dev["suffix_k"], m.dev["suffix_v"], lens, out, lse)
+        fa.key_weights(qr[:, 0], lse, pk, weights, decay=0.5)
+        fa.evict(pk, pv, weights, index, ko, vo, n_last=8, workspace=work)
+        fa.mx_pack(ko, vo, tiles2)
+        fa.mx_unpack(tiles2, k_back, v_back)
+
+    held = (out, lse, weights, index, ko, vo, tiles2, k_back, v_back, lens)
+    lens0 = lens.clone()
+    want = []
+    for _ in range(4):
+        step()
+        torch.cuda.synchronize()
+        want.append([x.clone() for x in held])
+    lens.copy_(lens0)
+    weights.zero_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    torch.cuda.synchronize()
+    assert torch.equal(lens, lens0), "capture runs nothing"
+    for i in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, got, ref in zip(("out", "lse", "weights", "index", "k", "v", "tiles", "k back", "v back", "lens"), held, want[i]):
+            assert torch.equal(got, ref), (i, name)
+        junk = torch.randn(1 << 20, device="cuda").sum()  # eager work between the replays
+        for x in held[:2] + held[3:9]:
+            x.zero_()
+        torch.cuda.synchronize()
+        del junk
