@@ -549,7 +549,7 @@ size_t fka_evict_bytes(int32_t n_kv_heads, int32_t len);
  *   k, v         bf16 [Hkv][kv_cap][d];  weights fp32 [Hkv][weights_cap]
  *   index        int32 [Hkv][keep]: the kept positions, ascending
  *   k_out, v_out bf16 [Hkv][keep][d];  weights_out fp32 [Hkv][keep] or NULL; none may overlap an input
- *   workspace    fka_evict_bytes(Hkv, len) device bytes, used by one call at a time; its contents before and after do not matter
+ *   workspace    fka_evict_bytes(Hkv, len) device bytes (16-byte aligned), used by one call at a time; its contents before and after do not matter
  */
 fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t keep, int32_t n_first, int32_t n_last,
                      const void *k, const void *v, int32_t kv_cap, const float *weights, int32_t weights_cap, int32_t *index,

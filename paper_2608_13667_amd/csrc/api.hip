@@ -2102,7 +2102,8 @@ fka_status fka_key_weights(const fka_heads *heads, int32_t n_rows, int32_t len, 
 size_t fka_evict_bytes(int32_t n_kv_heads, int32_t len)
 {
     if (n_kv_heads < 1 || len < 0) return 0;
-    return (size_t)n_kv_heads * (3 * fka::kEvictBins * sizeof(uint32_t) + (size_t)ceil_div(len, fka::kEvictChunk) * 2 * sizeof(int32_t));
+    const size_t chunks = std::min(ceil_div(len, fka::kEvictGroup), fka::kEvictChunks);
+    return (size_t)n_kv_heads * (chunks * (3 * fka::kEvictBins * sizeof(uint32_t) + 2 * sizeof(int32_t)) + 4 * sizeof(int32_t));
 }
 
 fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t keep, int32_t n_first, int32_t n_last,
@@ -2125,7 +2126,7 @@ fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t 
     REQUIRE_PTR16(k_out);
     REQUIRE_PTR16(v_out);
     REQUIRE_OPT4(weights_out);
-    REQUIRE_PTR4(workspace);
+    REQUIRE_PTR16(workspace);
     const size_t need = fka_evict_bytes(n_kv_heads, len);
     REQUIRE(workspace_bytes >= need, "workspace of %zu bytes, %zu are needed", workspace_bytes, need);
     fka::EvictArgs a{};
@@ -2137,7 +2138,11 @@ fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t 
     a.v_out = static_cast<uint16_t *>(v_out);
     a.weights_out = weights_out;
     a.hist = static_cast<uint32_t *>(workspace);
-    a.counts = reinterpret_cast<int32_t *>(a.hist + (size_t)3 * n_kv_heads * fka::kEvictBins);
+    const int32_t groups = ceil_div(len, fka::kEvictGroup);
+    a.chunk_blocks = ceil_div(groups, fka::kEvictChunks);
+    a.chunks = ceil_div(groups, a.chunk_blocks);
+    a.counts = reinterpret_cast<int32_t *>(a.hist + (size_t)3 * n_kv_heads * a.chunks * fka::kEvictBins);
+    a.state = a.counts + (size_t)n_kv_heads * a.chunks * 2;
     a.len = len;
     a.kv_cap = kv_cap;
     a.w_cap = weights_cap;
@@ -2146,7 +2151,6 @@ fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t 
     a.n_last = n_last;
     a.n_kv_heads = n_kv_heads;
     a.head_dim = head_dim;
-    a.chunks = ceil_div(len, fka::kEvictChunk);
     hipError_t e = fka::launch_evict(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "evict kernel launch");
     return ok();

@@ -7,24 +7,58 @@
 // evict: of the positions [0, len) of each KV head, the first n_first and the last n_last, and of those between
 // the ones with the largest weights (equal ones: the lowest positions), `keep` in all; their K and V rows and
 // weights are copied in order.  The threshold is found digit by digit (11, 11 and 10 bits of an order-preserving
-// integer of the weight) from histograms, so the choice is exact and does not depend on the order of the atomics.
+// integer of the weight) from histograms, so the choice is exact and does not depend on the order of the atomics;
+// a kept position's place is the count of kept ones in front of it.
 #pragma once
 
 #include "internal.h"
 #include "mx_attend.h"
+#include "scan64.h"
 
 namespace fka {
 
-// grid (ceil(len / 256), Hkv), four waves of 64 keys: K on M, query rows on N, so a lane sums its rows'
-// weights of 16 keys over all row tiles and the 16 lanes of a key are summed once at the end.
+// grid (ceil(len / 256), Hkv), four waves of 64 keys, which a wave holds as the products' A operands (keys on M), so
+// a lane sums its rows' weights of 16 keys over all row tiles and the 16 lanes of a key are summed once at the end.  The query
+// rows (N) pass through LDS, 32 at a time and the next ones loading, for the four waves together: read from L2 by each
+// wave, they were what bounded many rows (512 rows over 128k keys 289 us).
 template <int HD>
-__global__ __launch_bounds__(256, 2) void key_weights_kernel(WeightsArgs a)
+__global__ __launch_bounds__(256, 3) void key_weights_kernel(WeightsArgs a)
 {
-    constexpr int NC = HD / 32, KT = 4;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int NC = HD / 32, KT = 4, CPR = HD / 8, QR = 32, QL = QR * CPR / 256;
+    __shared__ uint4 qs[2][QR * CPR];  // chunk c of row r at r CPR + (c ^ r mod CPR): a read of 16 rows touches every bank
+    __shared__ float nls[2][QR];       // -lse log2(e); -inf: a row past the end or without keys, weight 0
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, q4 = lane >> 4, head = blockIdx.y;
     const int key0 = (blockIdx.x * 4 + wave) * 16 * KT;
-    if (key0 >= a.len) return;
+    uint4 qr[QL];
+    float nl_next = 0.f;
+    auto fetch = [&](int64_t r0) {
+        auto row_of = [&](int64_t r) {
+            const int32_t seq = (int32_t)r / a.by_group;
+            return (size_t)seq * a.n_q_heads + head * a.group + ((int32_t)r - seq * a.group);
+        };
+#pragma unroll
+        for (int i = 0; i < QL; ++i) {
+            const int64_t r = r0 + (tid + 256 * i) / CPR;
+            qr[i] = uint4{0, 0, 0, 0};
+            if (r < a.n_rows) qr[i] = *reinterpret_cast<const uint4 *>(a.q + row_of(r) * HD + (tid % CPR) * 8);
+        }
+        nl_next = -INFINITY;
+        if (tid < QR && r0 + tid < a.n_rows) {
+            const float l = a.lse[row_of(r0 + tid)];
+            if (l != -INFINITY) nl_next = -l * 1.44269504088896341f;
+        }
+    };
+    auto put = [&](int buf) {
+#pragma unroll
+        for (int i = 0; i < QL; ++i) {
+            const int r = (tid + 256 * i) / CPR, c = tid % CPR;
+            qs[buf][r * CPR + (c ^ (r & (CPR - 1)))] = qr[i];
+        }
+        if (tid < QR) nls[buf][tid] = nl_next;
+    };
+    float w[KT][4] = {};
+    fetch(0);  // in front of the keys, so that they are still on their way while the rows pass into LDS
     const uint16_t *k = a.k + ((size_t)head * a.k_cap + key0) * HD;
     mx_bf16x8 kb[KT][NC];
 #pragma unroll
@@ -33,39 +67,46 @@ __global__ __launch_bounds__(256, 2) void key_weights_kernel(WeightsArgs a)
         for (int c = 0; c < NC; ++c) {
             kb[u][c] = mx_bf16x8{};
             if (key0 + 16 * u + l16 < a.len)
-                kb[u][c] = *reinterpret_cast<const mx_bf16x8 *>(k + (size_t)(16 * u + l16) * HD + 32 * c + 8 * q4);
+                kb[u][c] = __builtin_nontemporal_load(reinterpret_cast<const mx_bf16x8 *>(k + (size_t)(16 * u + l16) * HD + 32 * c + 8 * q4));
         }
-    float w[KT][4] = {};
-    for (int64_t r0 = 0; r0 < a.n_rows; r0 += 16) {
-        const int64_t r = r0 + l16;
-        mx_bf16x8 qb[NC];
-        float nl = -INFINITY;  // a row past the end, or one without keys: weight 0
+    put(0);
+    __syncthreads();
+    for (int64_t r0 = 0; r0 < a.n_rows; r0 += QR) {
+        const int buf = (int)(r0 / QR) & 1, tiles = (int)(min(a.n_rows - r0, (int64_t)QR) + 15) / 16;
+        if (r0 + QR < a.n_rows) fetch(r0 + QR);
+        for (int t = 0; t < tiles; ++t) {
+            const int r = 16 * t + l16;
+            mx_bf16x8 qb[NC];
 #pragma unroll
-        for (int c = 0; c < NC; ++c) qb[c] = mx_bf16x8{};
-        if (r < a.n_rows) {
-            const int64_t seq = (int32_t)r / a.by_group;
-            const size_t row = (size_t)seq * a.n_q_heads + head * a.group + (r - seq * a.group);
+            for (int c = 0; c < NC; ++c)
+                qb[c] = __builtin_bit_cast(mx_bf16x8, qs[buf][r * CPR + ((4 * c + q4) ^ (r & (CPR - 1)))]);
+            const float nl = nls[buf][r];
+            mx_f32x4 s[KT];
 #pragma unroll
-            for (int c = 0; c < NC; ++c) qb[c] = *reinterpret_cast<const mx_bf16x8 *>(a.q + row * HD + 32 * c + 8 * q4);
-            const float l = a.lse[row];
-            if (l != -INFINITY) nl = -l * 1.44269504088896341f;
-        }
-        mx_f32x4 s[KT];
+            for (int u = 0; u < KT; ++u) {
+                s[u] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int u = 0; u < KT; ++u) {
-            s[u] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < NC; ++c) s[u] = mx_mfma(kb[u][c], qb[c], s[u]);
-        }
-        mx_result_wait();
-        const bool live = nl != -INFINITY;
-#pragma unroll
-        for (int u = 0; u < KT; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.scale_log2, nl));
-                w[u][i] += live ? p : 0.f;
+                for (int c = 0; c < NC; ++c) s[u] = mx_mfma(kb[u][c], qb[c], s[u]);
             }
+            mx_result_wait();
+            const bool live = nl != -INFINITY;
+            if (__builtin_amdgcn_ballot_w64(!live) == 0) {
+#pragma unroll
+                for (int u = 0; u < KT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[u][i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.scale_log2, nl));
+            } else {
+#pragma unroll
+                for (int u = 0; u < KT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[u][i], a.scale_log2, nl));
+                        w[u][i] += live ? p : 0.f;
+                    }
+            }
+        }
+        if (r0 + QR < a.n_rows) put(buf ^ 1);  // its readers are a barrier behind
+        __syncthreads();
     }
     auto ror = [](float v, auto n) {
         return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x120 + decltype(n)::value, 0xf, 0xf, false));
@@ -99,181 +140,265 @@ __device__ inline uint32_t evict_key(float w)
 __device__ inline int evict_shift(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
 __device__ inline uint32_t evict_mask(int digit) { return digit == 2 ? 1023u : 2047u; }
 
-// The threshold's first `digits` digits, from their histograms, by a block of 256 threads: the `want`-th largest key has
-// the prefix `key` (in its place), and `want` counts on among those that share it.
-__device__ inline void evict_threshold(const EvictArgs &a, int head, int digits, uint32_t &key, int &want)
+constexpr int kEvictThreads = 1024;
+
+struct EvictLds {
+    uint32_t bins[kEvictBins];
+    int32_t wave[kEvictThreads / 64];
+    int32_t bin, want;
+    int32_t sums[3];
+    uint32_t ranks[32 * kEvictThreads / 64];  // per (load, wave): keys above the threshold << 16, keys at it
+};
+
+// The bin that holds the want-th largest key: thread t has the counts of bins 2047 - 2 t and 2046 - 2 t.
+// want goes on among the keys of that bin.
+__device__ inline void evict_find(EvictLds &l, int c0, int c1, int &bin, int &want)
 {
-    __shared__ int32_t s_sum[256], s_bin, s_want;
-    key = 0;
-    want = a.keep - a.n_first - a.n_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int sum = scan64(c0 + c1);
+    if (lane == 63) l.wave[wave] = sum;
+    __syncthreads();
+    int before = sum - c0 - c1;
+    for (int w = 0; w < kEvictThreads / 64; ++w) before += w < wave ? l.wave[w] : 0;
+    if (before < want && want <= before + c0) {
+        l.bin = kEvictBins - 1 - 2 * tid;
+        l.want = want - before;
+    } else if (before + c0 < want && want <= before + c0 + c1) {
+        l.bin = kEvictBins - 2 - 2 * tid;
+        l.want = want - before - c0;
+    }
+    __syncthreads();
+    bin = l.bin;
+    want = l.want;
+}
+
+// The histogram of a digit among this block's keys that share the digits before it (key), in LDS.  Keys out of the
+// choice are 0 with `in` unset.
+template <int E>
+__device__ inline void evict_hist(EvictLds &l, const uint32_t (&k)[E], uint32_t in, int digit, uint32_t key)
+{
     const int tid = threadIdx.x;
-    for (int d = 0; d < digits; ++d) {
-        const uint32_t *h = a.hist + ((size_t)d * a.n_kv_heads + head) * kEvictBins;
-        // thread t has bins [2048 - 8 (t + 1), 2048 - 8 t), from the top
-        uint32_t c[8];
-        int32_t sum = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            c[i] = h[kEvictBins - 1 - 8 * tid - i];
-            sum += c[i];
-        }
-        __syncthreads();
-        s_sum[tid] = sum;
-        if (tid == 0) s_bin = 0, s_want = 0;
-        __syncthreads();
-        for (int o = 1; o < 256; o *= 2) {
-            const int32_t x = tid >= o ? s_sum[tid - o] : 0;
-            __syncthreads();
-            s_sum[tid] += x;
-            __syncthreads();
-        }
-        int32_t before = s_sum[tid] - sum;  // keys above this thread's bins
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (before < want && want <= before + (int32_t)c[i]) {
-                s_bin = kEvictBins - 1 - 8 * tid - i;
-                s_want = want - before;
-            }
-            before += c[i];
-        }
-        __syncthreads();
-        if (want == 0) {  // nothing to take: above every key
-            key = 0xffffffffu;
-            return;
-        }
-        key |= (uint32_t)s_bin << evict_shift(d);
-        want = s_want;
-    }
-}
-
-__global__ __launch_bounds__(256) void evict_clear_kernel(uint32_t *hist, int n)
-{
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < n) hist[i] = 0;
-}
-
-// grid (chunks, Hkv): the histogram of one digit among the keys that share the digits before it.
-__global__ __launch_bounds__(256) void evict_hist_kernel(EvictArgs a, int digit)
-{
-    __shared__ uint32_t bins[kEvictBins];
-    const int tid = threadIdx.x, head = blockIdx.y;
-    uint32_t key;
-    int want;
-    evict_threshold(a, head, digit, key, want);
-    if (want == 0) return;
-    for (int i = tid; i < kEvictBins; i += 256) bins[i] = 0;
+    l.bins[2 * tid] = l.bins[2 * tid + 1] = 0;
     __syncthreads();
-    const float *w = a.weights + (size_t)head * a.w_cap;
-    const int p0 = blockIdx.x * kEvictChunk, p1 = min(p0 + kEvictChunk, a.len - a.n_last);
-    const int above = digit == 0 ? 32 : evict_shift(digit - 1);  // the digits before it start here
-    for (int p = max(p0, a.n_first) + tid; p < p1; p += 256) {
-        const uint32_t k = evict_key(w[p]);
-        if (digit == 0 || (k >> above) == (key >> above)) atomicAdd(&bins[(k >> evict_shift(digit)) & evict_mask(digit)], 1u);
-    }
-    __syncthreads();
-    uint32_t *h = a.hist + ((size_t)digit * a.n_kv_heads + head) * kEvictBins;
-    for (int i = tid; i < kEvictBins; i += 256)
-        if (bins[i]) atomicAdd(&h[i], bins[i]);
-}
-
-// grid (chunks, Hkv): how many of the chunk's keys are above the threshold and at it.
-__global__ __launch_bounds__(256) void evict_count_kernel(EvictArgs a)
-{
-    __shared__ int32_t n[2];
-    const int tid = threadIdx.x, head = blockIdx.y;
-    uint32_t key;
-    int want;
-    evict_threshold(a, head, 3, key, want);
-    if (tid < 2) n[tid] = 0;
-    __syncthreads();
-    const float *w = a.weights + (size_t)head * a.w_cap;
-    const int p0 = blockIdx.x * kEvictChunk, p1 = min(p0 + kEvictChunk, a.len - a.n_last);
-    int above = 0, at = 0;
-    for (int p = max(p0, a.n_first) + tid; p < p1; p += 256) {
-        const uint32_t k = evict_key(w[p]);
-        above += k > key;
-        at += k == key;
-    }
-    atomicAdd(&n[0], above);
-    atomicAdd(&n[1], at);
-    __syncthreads();
-    if (tid < 2) a.counts[((size_t)head * a.chunks + blockIdx.x) * 2 + tid] = n[tid];
-}
-
-// grid (chunks, Hkv): the chunk's kept positions, in order, to their places in the index.
-__global__ __launch_bounds__(256) void evict_index_kernel(EvictArgs a)
-{
-    __shared__ int32_t s_before[2], s_at[256], s_kept[256];
-    const int tid = threadIdx.x, head = blockIdx.y, chunk = blockIdx.x;
-    uint32_t key;
-    int want;
-    evict_threshold(a, head, 3, key, want);
-    const int m = a.keep - a.n_first - a.n_last;
-    if (tid < 2) s_before[tid] = 0;
-    __syncthreads();
-    int above = 0, at = 0;
-    for (int c = tid; c < chunk; c += 256) {
-        above += a.counts[((size_t)head * a.chunks + c) * 2];
-        at += a.counts[((size_t)head * a.chunks + c) * 2 + 1];
-    }
-    atomicAdd(&s_before[0], above);
-    atomicAdd(&s_before[1], at);
-    __syncthreads();
-    const int at_before = s_before[1];
-    const int p0 = chunk * kEvictChunk, mid1 = a.len - a.n_last;
-    // kept before the chunk: the first n_first, the middle's, the last n_last
-    int out = min(p0, a.n_first) + s_before[0] + min(at_before, want) + max(p0 - mid1, 0);
-    // eight consecutive positions per thread, so that the order is kept
-    constexpr int E = kEvictChunk / 256;
-    const float *w = a.weights + (size_t)head * a.w_cap;
-    uint32_t k[E];
-    int n_at = 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-        const int p = p0 + E * tid + i;
-        const bool mid = p >= a.n_first && p < mid1;
-        k[i] = mid ? evict_key(w[p]) : 0;
-        n_at += mid && m > 0 && k[i] == key;
-    }
-    s_at[tid] = n_at;
-    __syncthreads();
-    for (int o = 1; o < 256; o *= 2) {
-        const int32_t x = tid >= o ? s_at[tid - o] : 0;
-        __syncthreads();
-        s_at[tid] += x;
-        __syncthreads();
-    }
-    int rank = at_before + s_at[tid] - n_at;  // keys at the threshold before this thread's
-    bool take[E];
-    int n_take = 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-        const int p = p0 + E * tid + i;
-        const bool mid = p >= a.n_first && p < mid1;
-        take[i] = p < a.len && !mid;
-        if (mid && m > 0) {
-            if (k[i] == key)
-                take[i] = rank++ < want;
-            else
-                take[i] = k[i] > key;
-        }
-        n_take += take[i];
-    }
-    s_kept[tid] = n_take;
-    __syncthreads();
-    for (int o = 1; o < 256; o *= 2) {
-        const int32_t x = tid >= o ? s_kept[tid - o] : 0;
-        __syncthreads();
-        s_kept[tid] += x;
-        __syncthreads();
-    }
-    out += s_kept[tid] - n_take;
+    const int above = digit == 0 ? 31 : evict_shift(digit - 1);  // the digits before it start here
 #pragma unroll
     for (int i = 0; i < E; ++i)
-        if (take[i]) {
-            if (out < a.keep) a.index[(size_t)head * a.keep + out] = p0 + E * tid + i;
-            ++out;
+        if ((in >> i & 1) && (digit == 0 || (k[i] >> above) == (key >> above)))
+            atomicAdd(&l.bins[(k[i] >> evict_shift(digit)) & evict_mask(digit)], 1u);
+    __syncthreads();
+}
+
+// The block's keys: position p0 + i 1024 + tid; returns which lie between the first n_first and the last n_last.
+template <int E>
+__device__ inline uint32_t evict_load(const EvictArgs &a, int head, int p0, uint32_t (&k)[E])
+{
+    const float *w = a.weights + (size_t)head * a.w_cap;
+    float x[E];
+    uint32_t in = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int p = p0 + i * kEvictThreads + (int)threadIdx.x;
+        const bool mid = p >= a.n_first && p < a.len - a.n_last;
+        x[i] = mid ? w[p] : 0.f;
+        in |= mid ? 1u << i : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) k[i] = evict_key(x[i]);
+    return in;
+}
+
+// The block's kept positions to their places in the index.  above0 and at0: keys above the threshold `key` and at it in the
+// blocks in front; of those at it the first `want` are kept (want = 0: none, and none above).
+template <int E>
+__device__ inline void evict_write(EvictLds &l, const EvictArgs &a, int head, int p0, const uint32_t (&k)[E], uint32_t in, uint32_t key,
+                                   int want, int above0, int at0)
+{
+    constexpr int NW = kEvictThreads / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint64_t above[E], at[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const bool mid = (in >> i & 1) && want > 0;
+        above[i] = __builtin_amdgcn_ballot_w64(mid && k[i] > key);
+        at[i] = __builtin_amdgcn_ballot_w64(mid && k[i] == key);
+        if (lane == 0) l.ranks[i * NW + wave] = (uint32_t)__builtin_popcountll(above[i]) << 16 | (uint32_t)__builtin_popcountll(at[i]);
+    }
+    __syncthreads();
+    // exclusive sums in the order of the positions, by the first wave
+    if (wave == 0) {
+        constexpr int PER = E * NW / 64;
+        uint32_t c[PER], sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            c[i] = l.ranks[lane * PER + i];
+            sum += c[i];
         }
+        uint32_t run = (uint32_t)scan64((int)sum) - sum;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            l.ranks[lane * PER + i] = run;
+            run += c[i];
+        }
+    }
+    __syncthreads();
+    const uint64_t below = lane == 0 ? 0 : ~0ull >> (64 - lane);
+    int32_t *index = a.index + (size_t)head * a.keep;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const int p = p0 + i * kEvictThreads + tid;
+        if (p >= a.len) continue;
+        const uint32_t r = l.ranks[i * NW + wave];
+        const int ab = above0 + (int)(r >> 16) + __builtin_popcountll(above[i] & below);
+        const int eq = at0 + (int)(r & 0xffff) + __builtin_popcountll(at[i] & below);
+        int out = -1;
+        if (p < a.n_first)
+            out = p;
+        else if (p >= a.len - a.n_last)
+            out = a.keep - (a.len - p);
+        else if ((above[i] >> lane & 1) || ((at[i] >> lane & 1) && eq < want))
+            out = a.n_first + ab + min(eq, want);
+        if (out >= 0 && out < a.keep) index[out] = p;
+    }
+}
+
+// grid (Hkv): a head's positions all in one block's registers (len <= 1024 E).
+template <int E>
+__global__ __launch_bounds__(kEvictThreads) void evict_one_kernel(EvictArgs a)
+{
+    __shared__ EvictLds l;
+    const int head = blockIdx.x, tid = threadIdx.x;
+    uint32_t k[E], key = 0;
+    const uint32_t in = evict_load<E>(a, head, 0, k);
+    int want = a.keep - a.n_first - a.n_last;
+    if (want > 0)
+        for (int d = 0; d < 3; ++d) {
+            int bin;
+            evict_hist<E>(l, k, in, d, key);
+            evict_find(l, l.bins[kEvictBins - 1 - 2 * tid], l.bins[kEvictBins - 2 - 2 * tid], bin, want);
+            key |= (uint32_t)bin << evict_shift(d);
+            __syncthreads();
+        }
+    evict_write<E>(l, a, head, 0, k, in, key, want, 0, 0);
+}
+
+// Longer prefixes: a kernel per digit, grid (chunks, Hkv).  Each leaves its chunk's histogram; the next finds
+// the digit in their sum, and what the chunk has above it.
+//
+// The sums over the chunks of this thread's two bins of a digit: all, this chunk's own and those in front.
+__device__ inline void evict_sum(const EvictArgs &a, int head, int digit, int (&all)[2], int (&own)[2], int (&front)[2])
+{
+    const uint2 *h = reinterpret_cast<const uint2 *>(a.hist) +
+                     ((size_t)digit * a.n_kv_heads + head) * a.chunks * (kEvictBins / 2) + (kEvictBins / 2 - 1 - threadIdx.x);
+    all[0] = all[1] = own[0] = own[1] = front[0] = front[1] = 0;
+#pragma unroll 8
+    for (int c = 0; c < a.chunks; ++c) {
+        const uint2 v = h[(size_t)c * (kEvictBins / 2)];  // the higher bin is y
+        all[0] += v.y;
+        all[1] += v.x;
+        if (c < (int)blockIdx.x) front[0] += v.y, front[1] += v.x;
+        if (c == (int)blockIdx.x) own[0] = v.y, own[1] = v.x;
+    }
+}
+
+// Adds x over the block into l.sums[i] (cleared before, read behind a barrier).
+__device__ inline void evict_add(EvictLds &l, int i, int x)
+{
+    const int s = scan64(x);
+    if ((threadIdx.x & 63) == 63 && s) atomicAdd(&l.sums[i], s);
+}
+
+// Digit DIGIT's histogram; behind the first, the digit before it is found first.
+template <int E, int DIGIT>
+__global__ __launch_bounds__(kEvictThreads) void evict_hist_kernel(EvictArgs a)
+{
+    __shared__ EvictLds l;
+    const int tid = threadIdx.x, head = blockIdx.y, chunk = blockIdx.x;
+    const int per = a.chunk_blocks;  // groups of 1024 E positions to a chunk
+    uint32_t key = 0, k[E];
+    uint32_t in = evict_load<E>(a, head, chunk * per * E * kEvictThreads, k);
+    if constexpr (DIGIT > 0) {
+        int want = a.keep - a.n_first - a.n_last, bin, all[2], own[2], front[2];
+        int32_t *state = a.state + (size_t)head * 4;
+        if (DIGIT > 1) {
+            key = state[0];
+            want = state[1];
+        }
+        if (tid < 3) l.sums[tid] = 0;
+        evict_sum(a, head, DIGIT - 1, all, own, front);
+        evict_find(l, all[0], all[1], bin, want);
+        key |= (uint32_t)bin << evict_shift(DIGIT - 1);
+        // each digit's state in a place of its own: other blocks may still read the one before
+        if (chunk == 0 && tid == 0) {
+            state[2 * (DIGIT - 1)] = (int32_t)key;
+            state[2 * (DIGIT - 1) + 1] = want;
+        }
+        const int b0 = kEvictBins - 1 - 2 * tid;
+        evict_add(l, 0, (b0 > bin ? own[0] : 0) + (b0 - 1 > bin ? own[1] : 0));
+        __syncthreads();
+        if (tid == 0) a.counts[((size_t)head * a.chunks + chunk) * 2 + DIGIT - 1] = l.sums[0];
+    }
+    uint32_t mine[2] = {0, 0};
+    for (int g = 0;;) {
+        evict_hist<E>(l, k, in, DIGIT, key);
+        mine[0] += l.bins[2 * tid];
+        mine[1] += l.bins[2 * tid + 1];
+        if (++g == per) break;
+        in = evict_load<E>(a, head, (chunk * per + g) * E * kEvictThreads, k);
+        __syncthreads();
+    }
+    reinterpret_cast<uint2 *>(a.hist)[(((size_t)DIGIT * a.n_kv_heads + head) * a.chunks + chunk) * (kEvictBins / 2) + tid] =
+        uint2{mine[0], mine[1]};
+}
+
+// The last digit, the chunk's place among the kept, and its part of the index.
+template <int E>
+__global__ __launch_bounds__(kEvictThreads) void evict_index_kernel(EvictArgs a)
+{
+    __shared__ EvictLds l;
+    const int tid = threadIdx.x, head = blockIdx.y, chunk = blockIdx.x;
+    const int per = a.chunk_blocks;
+    uint32_t k[E], key = 0;
+    uint32_t in = evict_load<E>(a, head, chunk * per * E * kEvictThreads, k);
+    int want = a.keep - a.n_first - a.n_last, above0 = 0, at0 = 0;
+    if (want > 0) {
+        int bin, all[2], own[2], front[2];
+        const int32_t *state = a.state + (size_t)head * 4;
+        key = state[2];
+        want = state[3];
+        if (tid < 3) l.sums[tid] = 0;
+        evict_sum(a, head, 2, all, own, front);
+        evict_find(l, all[0], all[1], bin, want);
+        key |= (uint32_t)bin;
+        const int b0 = kEvictBins - 1 - 2 * tid;
+        int above = (b0 > bin ? front[0] : 0) + (b0 - 1 > bin ? front[1] : 0);
+        for (int c = tid; c < 2 * chunk; c += kEvictThreads) above += a.counts[(size_t)head * a.chunks * 2 + c];
+        evict_add(l, 0, above);
+        evict_add(l, 1, (b0 == bin ? front[0] : 0) + (b0 - 1 == bin ? front[1] : 0));
+        __syncthreads();
+        above0 = l.sums[0];
+        at0 = l.sums[1];
+    }
+    for (int g = 0;;) {
+        const int p0 = (chunk * per + g) * E * kEvictThreads;
+        evict_write<E>(l, a, head, p0, k, in, key, want, above0, at0);
+        if (++g == per) break;
+        // the group's own keys above the threshold and at it, for the next group
+        int above = 0, at = 0;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            above += (in >> i & 1) && want > 0 && k[i] > key;
+            at += (in >> i & 1) && want > 0 && k[i] == key;
+        }
+        __syncthreads();
+        if (tid < 3) l.sums[tid] = 0;
+        __syncthreads();
+        evict_add(l, 0, above);
+        evict_add(l, 1, at);
+        in = evict_load<E>(a, head, p0 + E * kEvictThreads, k);
+        __syncthreads();
+        above0 += l.sums[0];
+        at0 += l.sums[1];
+    }
 }
 
 // grid (ceil(keep / rows per block), Hkv): the kept rows and weights.
@@ -310,14 +435,21 @@ inline hipError_t launch_key_weights_kernel(const WeightsArgs &a, int head_dim, 
 inline hipError_t launch_evict_kernels(const EvictArgs &a, hipStream_t s)
 {
     if (a.keep <= 0) return hipSuccess;
-    const dim3 chunks(a.chunks, a.n_kv_heads), block(256);
-    const int n = 3 * a.n_kv_heads * kEvictBins;
-    evict_clear_kernel<<<dim3((n + 255) / 256), block, 0, s>>>(a.hist, n);
-    for (int d = 0; d < 3; ++d) evict_hist_kernel<<<chunks, block, 0, s>>>(a, d);
-    evict_count_kernel<<<chunks, block, 0, s>>>(a);
-    evict_index_kernel<<<chunks, block, 0, s>>>(a);
+    const dim3 block(kEvictThreads), chunks(a.chunks, a.n_kv_heads), heads(a.n_kv_heads);
+    if (a.len <= 8 * kEvictThreads) {
+        evict_one_kernel<8><<<heads, block, 0, s>>>(a);
+    } else if (a.len <= 32 * kEvictThreads) {
+        evict_one_kernel<32><<<heads, block, 0, s>>>(a);
+    } else {
+        if (a.keep > a.n_first + a.n_last) {
+            evict_hist_kernel<8, 0><<<chunks, block, 0, s>>>(a);
+            evict_hist_kernel<8, 1><<<chunks, block, 0, s>>>(a);
+            evict_hist_kernel<8, 2><<<chunks, block, 0, s>>>(a);
+        }
+        evict_index_kernel<8><<<chunks, block, 0, s>>>(a);
+    }
     const int per = 256 / (a.head_dim / 8) * 4;
-    evict_gather_kernel<<<dim3((a.keep + per - 1) / per, a.n_kv_heads), block, 0, s>>>(a);
+    evict_gather_kernel<<<dim3((a.keep + per - 1) / per, a.n_kv_heads), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 

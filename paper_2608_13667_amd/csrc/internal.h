@@ -443,9 +443,11 @@ struct WeightsArgs {
     float scale_log2, decay;
 };
 
-// A prefix shortened to its heaviest keys (evict.h): histogram bins of a digit, positions per block.
+// A prefix shortened to its heaviest keys (evict.h): histogram bins of a digit; the positions a block takes at a time, a
+// multiple of which is a chunk, so that there are at most kEvictChunks of them (every block sums them all).
 constexpr int kEvictBins = 2048;
-constexpr int kEvictChunk = 2048;
+constexpr int kEvictGroup = 8192;
+constexpr int kEvictChunks = 64;
 
 struct EvictArgs {
     const uint16_t *k, *v;   // [Hkv][kv_cap][d]
@@ -453,10 +455,12 @@ struct EvictArgs {
     int32_t *index;          // [Hkv][keep]
     uint16_t *k_out, *v_out; // [Hkv][keep][d]
     float *weights_out;      // [Hkv][keep] or null
-    uint32_t *hist;          // [3][Hkv][2048]
-    int32_t *counts;         // [Hkv][chunks][2]: above the threshold, at it
+    // longer prefixes only
+    uint32_t *hist;          // [3][Hkv][chunks][2048]: the chunks' histograms of each digit
+    int32_t *counts;         // [Hkv][chunks][2]: keys above the threshold by its first digit, by its second
+    int32_t *state;          // [Hkv][4]: the threshold's digits and what is wanted on, behind one digit and behind two
     int32_t len, kv_cap, w_cap, keep, n_first, n_last;
-    int32_t n_kv_heads, head_dim, chunks;
+    int32_t n_kv_heads, head_dim, chunks, chunk_blocks;
 };
 
 // error-flag bits (device)

@@ -62,9 +62,11 @@ __device__ inline __amdgpu_buffer_rsrc_t mx_rsrc(const void *base, int bytes)
                                              0x00020000);
 }
 
+// 16 bytes per lane, non-temporal where they are read once (POLICY 2), else kept for the pair's other wave (0).
+template <int POLICY = 2>
 __device__ inline uint4 mx_load16(__amdgpu_buffer_rsrc_t r, uint32_t off)
 {
-    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 2));  // non-temporal: read once
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, POLICY));
 }
 
 // Sixteen wait states between products and the first vector read of their results: what the compiler counts
@@ -76,16 +78,9 @@ __device__ inline void mx_result_wait()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// A product's result, read behind mx_result_wait: held where the product left it (ACC: an accumulation register, which the
-// compiler takes in kernels of one wave per SIMD), so that no copy is made in front of the wait.
-template <bool ACC>
-__device__ __attribute__((always_inline)) inline void mx_result(mx_f32x4 &x)
-{
-    if constexpr (ACC)
-        asm volatile("" : "+a"(x));
-    else
-        asm volatile("" : "+v"(x));
-}
+// A product's result, read behind mx_result_wait: held in the registers where the product left it, so that no copy is made
+// in front of the wait.
+__device__ __attribute__((always_inline)) inline void mx_result(mx_f32x4 &x) { asm volatile("" : "+v"(x)); }
 
 // The four lanes that hold one query row: l, l ^ 16, l ^ 32, l ^ 48.
 __device__ inline float mx_row_max(float x)
@@ -152,16 +147,26 @@ __device__ __attribute__((always_inline)) inline void mx_exp(float (&x)[N], floa
     l_run += sum;
 }
 
+// p less one half of a word of two fp16 values, in one instruction.
+template <int HALF>
+__device__ __attribute__((always_inline)) inline float mx_rest(uint32_t h, float p)
+{
+    float r;
+    if constexpr (HALF == 0)
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+    else
+        asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(h), "v"(p));
+    return r;
+}
+
 // Eight p as two fp16 terms, each cut (not rounded: one instruction for two values), 2^-21 of p together.
 __device__ __attribute__((always_inline)) inline void mx_split16(const float *p, mx_f16x8 &hi, mx_f16x8 &lo)
 {
     uint32_t h[4], l[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const auto w = __builtin_amdgcn_cvt_pkrtz(p[2 * i], p[2 * i + 1]);
-        h[i] = __builtin_bit_cast(uint32_t, w);
-        l[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(__builtin_fmaf((float)w[0], -1.f, p[2 * i]),
-                                                                       __builtin_fmaf((float)w[1], -1.f, p[2 * i + 1])));
+        h[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p[2 * i], p[2 * i + 1]));
+        l[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(mx_rest<0>(h[i], p[2 * i]), mx_rest<1>(h[i], p[2 * i + 1])));
     }
     hi = __builtin_bit_cast(mx_f16x8, h);
     lo = __builtin_bit_cast(mx_f16x8, l);
@@ -179,23 +184,26 @@ __device__ __attribute__((always_inline)) inline void mx_split3(const float *p, 
     }
 }
 
-// 16-row tiles NT: one wave per SIMD where the accumulators of three or four need the registers, else two.
-template <int HD, int NT>
-__global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void mx_partials_kernel(MxArgs a)
+// A wave takes NT 16-row tiles, one or two: with three or four, its registers would leave one wave to a SIMD, and a
+// lone wave issues a vector instruction every 8 cycles at best (two together every 4; measured with chains of eight).  So
+// with more than 32 rows the waves of a block work in pairs (RS = 2), each pair on one tile, half of the rows each.
+template <int HD, int NT, int RS>
+__global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
 {
-    constexpr int NW = 4, NC = HD / 32, NE = HD / 16, CPR = HD / 8, ROWB = 2 * HD;
+    constexpr int NW = 4, NG = NW / RS, NC = HD / 32, NE = HD / 16, CPR = HD / 8, ROWB = 2 * HD;
     constexpr int kTileB = mx_tile_bytes<HD>();
-    constexpr bool kAcc = NT > 2;  // one wave per SIMD
-    // the waves' V slices of a suffix, then their accumulators, one 16-row tile at a time
-    __shared__ __attribute__((aligned(16))) float stage[NW][16 * HD];
-    __shared__ float red_m[NT * 16][NW], red_l[NT * 16][NW];
-    static_assert(sizeof(stage[0]) == (size_t)kSlice * ROWB, "a V slice fits");
+    // the waves' V slices of a suffix, then their accumulators
+    __shared__ __attribute__((aligned(16))) float stage[NW][NT * 16 * HD];
+    __shared__ __attribute__((aligned(16))) float red_m[NT * 16][NW], red_l[NT * 16][NW];
+    static_assert(sizeof(stage[0]) >= (size_t)kSlice * ROWB, "a V slice fits");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, q4 = lane >> 4;
     const MxJob job = a.jobs[blockIdx.x];
-    const int G = a.group, rows = job.rows, nt_act = (rows + 15) / 16;
     const bool suffix = job.suffix != 0;
+    // a prefix job's waves: wave group wg takes every NG-th tile, row half rh of it (rows from 16 NT rh on)
+    const int wg = suffix ? wave : wave / RS, rh = suffix ? 0 : wave % RS, row_lo = 16 * NT * rh;
+    const int G = a.group, rows = job.rows, nt_act = (rows - row_lo + 15) / 16;
 
     if (blockIdx.x == 0) {  // what the merge appends at
         for (int s = tid; s < a.n_seqs; s += 256) {
@@ -209,7 +217,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void mx_partials_kernel(MxArg
     mx_bf16x8 qb[NT][NC];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-        const int r = 16 * t + l16;
+        const int r = row_lo + 16 * t + l16;
 #pragma unroll
         for (int c = 0; c < NC; ++c) qb[t][c] = mx_bf16x8{};
         if (r < rows) {
@@ -247,13 +255,13 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void mx_partials_kernel(MxArg
         };
         auto load_k = [&](__amdgpu_buffer_rsrc_t rs) {
 #pragma unroll
-            for (int i = 0; i < KL; ++i) kr[i] = mx_load16(rs, i * 1024 + lane * 16);
+            for (int i = 0; i < KL; ++i) kr[i] = mx_load16<RS == 1 ? 2 : 0>(rs, i * 1024 + lane * 16);
             const auto w = __builtin_amdgcn_raw_buffer_load_b64(rs, 128 * HD + ((HD == 128 ? q4 : q4 >> 1) * 16 + l16) * 8, 0, 2);
             ks[0] = w[0], ks[1] = w[1];
         };
         auto load_v = [&](__amdgpu_buffer_rsrc_t rs) {
 #pragma unroll
-            for (int e = 0; e < NE; ++e) vr[e] = mx_load16(rs, 64 * HD + e * 1024 + lane * 16);
+            for (int e = 0; e < NE; ++e) vr[e] = mx_load16<RS == 1 ? 2 : 0>(rs, 64 * HD + e * 1024 + lane * 16);
             if constexpr (HD == 128) {
                 const auto w = __builtin_amdgcn_raw_buffer_load_b64(rs, 132 * HD + lane * 8, 0, 2);
                 vs[0] = w[0], vs[1] = w[1];
@@ -261,81 +269,110 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void mx_partials_kernel(MxArg
                 vs[0] = __builtin_amdgcn_raw_buffer_load_b32(rs, 132 * HD + lane * 4, 0, 2);
             }
         };
-        int tile = job.begin + wave;
+        int tile = job.begin + wg;
         const __amdgpu_buffer_rsrc_t rs = tile_rsrc(tile);
         load_k(rs);
         load_v(rs);
-        for (; tile < job.end; tile += NW) {
+        for (; tile < job.end; tile += NG) {
             const int valid = job.prefix_len - tile * kMxTile;
-            const __amdgpu_buffer_rsrc_t next = tile_rsrc(tile + NW);
+            const __amdgpu_buffer_rsrc_t next = tile_rsrc(tile + NG);
             // V scales 2^-23 .. 2^8, as bytes 104 .. 135: exact in fp16 (a byte below 104 borrows, and shows so itself)
             uint32_t odd = (vs[0] - 0x68686868u) & 0xe0e0e0e0u;
             if constexpr (HD == 128) odd |= (vs[1] - 0x68686868u) & 0xe0e0e0e0u;
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0) != 0, 0)) break;  // the loop behind takes the rest
-            // 32 keys at a time (eight of a lane's row): scores and p of more would not leave the registers that the
-            // next tile's loads need
+            // All scores of the tile, then its softmax, then p.v: the first two need K only, so V arrives behind them.
+            // Product (j, x) has keys 32 a + 8 j + 4 x + b in M row 4 a + b.
+            constexpr int J = 4;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                // S^T: product x has keys 32 a + 8 j + 4 x + b in M row 4 a + b
-                mx_f32x4 s[NT][2];
+            for (int j0 = 0; j0 < 4; j0 += J) {
+                mx_f32x4 s[NT][2 * J];
+                // two products' chains (x = 0, 1) of each row tile side by side: a product of a chain waits for the one before
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const float ksc = __uint_as_float(((ks[j >> 1] >> (8 * (2 * (j & 1) + u))) & 0xff) << 23);
-                    mx_bf16x8 kb[NC];
+                for (int i = 0; i < 2 * J; i += 2) {
+                    const int jx = 2 * j0 + i;
+                    float ksc[2];
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        const uint4 w = HD == 128 ? kr[2 * j + u] : kr[j];
-                        const int n = HD == 128 ? c : 2 * u + c;
-                        kb[c] = __builtin_bit_cast(mx_bf16x8, mx_value8(n == 0 ? w.x : n == 1 ? w.y : n == 2 ? w.z : w.w, ksc));
+                    for (int u = 0; u < 2; ++u) {
+                        ksc[u] = __uint_as_float(((ks[jx >> 2] >> (8 * ((jx & 3) + u))) & 0xff) << 23);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) s[t][i + u] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
                     }
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        s[t][u] = mx_f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int c = 0; c < NC; ++c)
 #pragma unroll
-                        for (int c = 0; c < NC; ++c) s[t][u] = mx_mfma(kb[c], qb[t][c], s[t][u]);
-                    }
+                        for (int u = 0; u < 2; ++u) {
+                            const uint4 w = HD == 128 ? kr[jx + u] : kr[jx >> 1];
+                            const int n = HD == 128 ? c : 2 * u + c;
+                            const mx_bf16x8 kb =
+                                __builtin_bit_cast(mx_bf16x8, mx_value8(n == 0 ? w.x : n == 1 ? w.y : n == 2 ? w.z : w.w, ksc[u]));
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) s[t][i + u] = mx_mfma(kb, qb[t][c], s[t][i + u]);
+                        }
+                    __builtin_amdgcn_sched_barrier(0);  // (conversions far ahead would leave the registers)
                 }
                 mx_result_wait();
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mx_result<kAcc>(s[t][0]), mx_result<kAcc>(s[t][1]);
-                if (j == 3) load_k(next);  // its time: the rest of this tile
-                float x[NT][8], mx[NT];
-#pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) x[t][i] = s[t][i / 4][i % 4];
+                    for (int i = 0; i < 2 * J; ++i) mx_result(s[t][i]);
+                if (j0 + J == 4) load_k(next);  // its time: the softmax and p.v
                 if (__builtin_expect(valid < kMxTile, 0)) {
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) x[t][i] = 32 * q4 + 8 * j + i < valid ? x[t][i] : -INFINITY;
+                        for (int i = 0; i < 8 * J; ++i)
+                            s[t][i / 4][i % 4] = 32 * q4 + 8 * j0 + i < valid ? s[t][i / 4][i % 4] : -INFINITY;
                 }
+                float mx[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mx[t] = mx_max(x[t]);
+                for (int t = 0; t < NT; ++t) {
+                    mx[t] = s[t][0][0];
+#pragma unroll
+                    for (int i = 1; i < 8 * J; ++i) mx[t] = fmaxf(mx[t], s[t][i / 4][i % 4]);
+                }
                 mx_move(mx, a.scale_log2, m_ref, l_run, acc);
+                mx_f16x8 ph[NT][J], pl[NT][J];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mx_exp(x[t], a.scale_log2, m_ref[t], l_run[t]);
-                auto vscale = [&](int e) { return __uint_as_float(((vs[e >> 2] >> (8 * (e & 3))) & 0xff) << 23); };
-                auto vword = [&](int e) { return j == 0 ? vr[e].x : j == 1 ? vr[e].y : j == 2 ? vr[e].z : vr[e].w; };
-                mx_f16x8 ph[NT], pl[NT];
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mx_split16(x[t], ph[t], pl[t]);
+                    for (int j = 0; j < J; ++j) {
+                        float x[8];
 #pragma unroll
-                for (int e = 0; e < NE; ++e) {
-                    const mx_f16x8 vb = mx_value8h(vword(e), vscale(e));
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        acc[t][e] = mx_mfma(vb, ph[t], acc[t][e]);
-                        acc[t][e] = mx_mfma(vb, pl[t], acc[t][e]);
+                        for (int i = 0; i < 8; ++i) x[i] = s[t][2 * j + i / 4][i % 4];
+                        mx_exp(x, a.scale_log2, m_ref[t], l_run[t]);
+                        mx_split16(x, ph[t][j], pl[t][j]);
                     }
-                }
                 __builtin_amdgcn_sched_barrier(0);
+                // two channel tiles side by side, the first terms of p in front of the second
+#pragma unroll
+                for (int e = 0; e < NE; e += 2) {
+                    float vsc[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) vsc[u] = __uint_as_float(((vs[e >> 2] >> (8 * ((e & 3) + u))) & 0xff) << 23);
+#pragma unroll
+                    for (int i = 0; i < J; ++i) {
+                        const int j = j0 + i;
+                        mx_f16x8 vb[2];
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+                            vb[u] = mx_value8h(j == 0 ? vr[e + u].x : j == 1 ? vr[e + u].y : j == 2 ? vr[e + u].z : vr[e + u].w, vsc[u]);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) acc[t][e + u] = mx_mfma(vb[u], ph[t][i], acc[t][e + u]);
+#pragma unroll
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) acc[t][e + u] = mx_mfma(vb[u], pl[t][i], acc[t][e + u]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
             load_v(next);  // its time: the next tile's scores and first softmax
         }
         // the same with V in bf16 and three terms of p, from the first tile with another scale on: 32 keys at
         // a time straight from memory, since such values are not what a cache is made of
-        for (; tile < job.end; tile += NW) {
+        for (; tile < job.end; tile += NG) {
             const int valid = job.prefix_len - tile * kMxTile;
             const __amdgpu_buffer_rsrc_t rt = tile_rsrc(tile);
 #pragma unroll 1
@@ -367,7 +404,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void mx_partials_kernel(MxArg
                 float x[NT][8], mx[NT];
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    mx_result<kAcc>(s[t][0]), mx_result<kAcc>(s[t][1]);
+                    mx_result(s[t][0]), mx_result(s[t][1]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) x[t][i] = 32 * q4 + 8 * j + i < valid ? s[t][i / 4][i % 4] : -INFINITY;
                     mx[t] = mx_max(x[t]);
@@ -419,7 +456,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void mx_partials_kernel(MxArg
                 for (int c = 0; c < NC; ++c) s[u] = mx_mfma(__builtin_bit_cast(mx_bf16x8, kr[u][c]), qb[0][c], s[u]);
             }
             mx_result_wait();
-            mx_result<kAcc>(s[0]), mx_result<kAcc>(s[1]);
+            mx_result(s[0]), mx_result(s[1]);
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -459,6 +496,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void mx_partials_kernel(MxArg
         for (int r = tid; r < rows; r += 256) a.part_lse[row_out + r] = -INFINITY;
         return;
     }
+    mx_result_wait();
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const float sum = mx_row_sum(l_run[t]);
@@ -466,70 +504,69 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void mx_partials_kernel(MxArg
             red_m[16 * t + l16][wave] = m_ref[t];
             red_l[16 * t + l16][wave] = sum;
         }
-    }
-    mx_result_wait();
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        if (t >= nt_act) break;
-        __syncthreads();  // the stage is free
-        // chunk c of row r at c ^ r: a store covers 16 rows at one chunk
+        // chunk c of row r at c ^ r mod 16: a store covers 16 rows at one chunk (a suffix's slices in the ring are read)
 #pragma unroll
         for (int e = 0; e < NE; ++e)
-            *reinterpret_cast<mx_f32x4 *>(&stage[wave][l16 * HD + 4 * ((4 * e + q4) ^ l16)]) = acc[t][e];
-        __syncthreads();
-        for (int u = tid; u < 16 * (HD / 4); u += 256) {
-            const int r = u / (HD / 4), c = u % (HD / 4);
-            if (16 * t + r >= rows) break;
-            float M = -INFINITY, W = 0.f;
+            if (t < nt_act) *reinterpret_cast<mx_f32x4 *>(&stage[wave][(16 * t + l16) * HD + 4 * ((4 * e + q4) ^ l16)]) = acc[t][e];
+    }
+    __syncthreads();
+    // a thread takes one chunk of 4 channels of every 256 / (HD / 4)-th row
+    constexpr int CH = HD / 4;
+    const int c = tid % CH;
+    for (int row = tid / CH; row < rows; row += 256 / CH) {
+        // the row in its half, whose waves are every RS-th (a suffix: all four have all rows)
+        const int half = row / (16 * NT), r = row - 16 * NT * half;
+        float m[NW], w[NW], M = -INFINITY, W = 0.f;
+        mx_f32x4 v[NW], o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < NW; ++w) M = fmaxf(M, red_m[16 * t + r][w]);
-            const float Mu = M == -INFINITY ? 0.f : M;
-            mx_f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                // a wave without keys has max -inf, sum 0 and a zero accumulator
-                const float e = __builtin_amdgcn_exp2f(red_m[16 * t + r][w] - Mu);
-                W = __builtin_fmaf(e, red_l[16 * t + r][w], W);
-                o += e * *reinterpret_cast<const mx_f32x4 *>(&stage[w][r * HD + 4 * (c ^ r)]);
-            }
-            const size_t at = row_out + 16 * t + r;
-            *reinterpret_cast<mx_f32x4 *>(a.part_o + at * HD + 4 * c) = o * (W == 0.f ? 0.f : 1.f / W);
-            if (c == 0) a.part_lse[at] = W == 0.f ? -INFINITY : (Mu - kMxShift + log2f(W)) * 0.693147180559945309f;
+        for (int i = 0; i < NW; ++i) {
+            const bool has = RS == 1 || suffix || i % RS == half;
+            m[i] = has ? red_m[r][i] : -INFINITY;
+            w[i] = has ? red_l[r][i] : 0.f;
+            v[i] = *reinterpret_cast<const mx_f32x4 *>(&stage[i][r * HD + 4 * (c ^ (r & 15))]);
         }
+#pragma unroll
+        for (int i = 0; i < NW; ++i) M = fmaxf(M, m[i]);
+        const float Mu = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const float e = __builtin_amdgcn_exp2f(m[i] - Mu);  // a wave without keys: 0
+            W = __builtin_fmaf(e, w[i], W);
+            if (RS == 1 || suffix || i % RS == half) o += e * v[i];  // (the other half's may be NaN)
+        }
+        *reinterpret_cast<mx_f32x4 *>(a.part_o + (row_out + row) * HD + 4 * c) = o * (W == 0.f ? 0.f : 1.f / W);
+        if (c == 0) a.part_lse[row_out + row] = W == 0.f ? -INFINITY : (Mu - kMxShift + log2f(W)) * 0.693147180559945309f;
     }
 }
 
 template <int HD>
 const void *mx_kernel_of(int row_tiles)
 {
-    switch (row_tiles) {
-    case 1: return reinterpret_cast<const void *>(&mx_partials_kernel<HD, 1>);
-    case 2: return reinterpret_cast<const void *>(&mx_partials_kernel<HD, 2>);
-    case 3: return reinterpret_cast<const void *>(&mx_partials_kernel<HD, 3>);
-    case 4: return reinterpret_cast<const void *>(&mx_partials_kernel<HD, 4>);
-    default: return nullptr;
-    }
+    if (row_tiles == 1) return reinterpret_cast<const void *>(&mx_partials_kernel<HD, 1, 1>);
+    if (row_tiles == 2) return reinterpret_cast<const void *>(&mx_partials_kernel<HD, 2, 1>);
+    return reinterpret_cast<const void *>(&mx_partials_kernel<HD, 2, 2>);
 }
 
 // Resident blocks per compute unit (0 on error).
 inline int mx_blocks_per_cu_of(int head_dim, int row_tiles)
 {
-    const void *f = head_dim == 128 ? mx_kernel_of<128>(row_tiles) : head_dim == 64 ? mx_kernel_of<64>(row_tiles) : nullptr;
+    if ((head_dim != 64 && head_dim != 128) || row_tiles < 1 || row_tiles > 4) return 0;
     int n = 0;
-    if (!f || hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, f, 256, 0) != hipSuccess) return 0;
+    const void *f = head_dim == 128 ? mx_kernel_of<128>(row_tiles) : mx_kernel_of<64>(row_tiles);
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, f, 256, 0) != hipSuccess) return 0;
     return n;
 }
 
 template <int HD>
 hipError_t launch_mx_hd(const MxArgs &a, int n_jobs, int row_tiles, hipStream_t s)
 {
-    switch (row_tiles) {
-    case 1: mx_partials_kernel<HD, 1><<<dim3(n_jobs), dim3(256), 0, s>>>(a); break;
-    case 2: mx_partials_kernel<HD, 2><<<dim3(n_jobs), dim3(256), 0, s>>>(a); break;
-    case 3: mx_partials_kernel<HD, 3><<<dim3(n_jobs), dim3(256), 0, s>>>(a); break;
-    case 4: mx_partials_kernel<HD, 4><<<dim3(n_jobs), dim3(256), 0, s>>>(a); break;
-    default: return hipErrorInvalidValue;
-    }
+    if (row_tiles < 1 || row_tiles > 4) return hipErrorInvalidValue;
+    if (row_tiles == 1)
+        mx_partials_kernel<HD, 1, 1><<<dim3(n_jobs), dim3(256), 0, s>>>(a);
+    else if (row_tiles == 2)
+        mx_partials_kernel<HD, 2, 1><<<dim3(n_jobs), dim3(256), 0, s>>>(a);
+    else
+        mx_partials_kernel<HD, 2, 2><<<dim3(n_jobs), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -21,7 +21,7 @@ def test_every_xdl_result_read_is_padded_around_the_cache():
         asm = X.compile_asm(hipcc, os.path.join(ROOT, "paper_2608_13667_amd", "csrc", "kernels.hip"),
                             os.path.join(ROOT, "include"), os.path.join(d, "kernels.s"))
     mx, weights = X.kernels(asm, "mx_partials_kernel"), X.kernels(asm, "key_weights_kernel")
-    assert len(mx) == 8 and len(weights) == 2
+    assert len(mx) == 6 and len(weights) == 2
     for k in mx + weights:
         pairs = X.scan(asm, k)
         assert pairs, k

@@ -765,6 +765,17 @@ def test_evict_long(fa):
     run_evict(fa, np.exp(1.5 * rng.standard_normal((2, 131072))).astype(np.float32), 32768, 4, 512)
 
 
+@pytest.mark.parametrize("L", [8191, 8192, 8193, 32767, 32768, 32769, 40000, 73729, 600001])
+def test_evict_at_the_kernels_sizes(fa, L):
+    """Around the lengths where a block, several blocks, and several groups of positions per block take a head; values that differ
+    in each of the three digits, many equal ones, and the choice's border at every place."""
+    rng = np.random.default_rng(L)
+    w = np.stack([np.exp(rng.standard_normal(L)), 1 + rng.integers(0, 9, L) * 2.0 ** -12, 1 + rng.integers(0, 3, L) * 2.0 ** -23,
+                  np.where(rng.random(L) < 0.999, 0.0, rng.random(L))]).astype(np.float32)
+    for keep, first, last in ((L // 3, 0, 0), (L - 1, 9000 if L > 20000 else 10, 7), (900, 400, 500), (901, 400, 500), (L, 0, 0)):
+        run_evict(fa, w, keep, first, last)
+
+
 # ------------------------------------------------------------------ together
 
 def test_a_turn_from_prompt_to_step(fa):
