@@ -728,22 +728,26 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
 // Largest device id range of the copies below: a launch's threads stay below 2^32.
 constexpr int32_t kMaxRotateTokens = 1 << 25;
 
-// The jobs of a decode over 4-bit tiles.  A job's unit of work is a prefix tile (17 KiB at d = 128) or a
-// suffix slice of 32 keys (16 KiB); every job gets about the same number, so that the jobs fill the resident
-// blocks once with every suffix at max_suffix_len, and at least one unit for each of a block's four waves.
+// The jobs of a decode over 4-bit tiles: ranges of prefix tiles and shares of the suffixes.  Two blocks are resident on a
+// compute unit, and each unit is to have one of either kind: a prefix job is bound by the vector units, a suffix job by its
+// loads.  So each kind is cut into about as many jobs as there are units, whatever the suffixes' lengths turn out to be up to
+// max_suffix_len; twice as many where the suffixes are short beside the prefixes (fewer than a slice to four tiles), and with
+// several groups, whose lengths do not come out even.  Measured (us a step or call, prefix tiles x suffix slices per job): 32k
+// prefix, 40 / 8 heads, 8 x 12 (256 + 200 jobs) 21.7, 4 x 8 29.3, 8 x 24 25.4, 16 x 8 25.0; 128k, 64 / 8 heads, 32 x 16 (256 + 280) 69,
+// 16 x 16 75, 48 x 16 90; without suffixes 512k, 40 / 8 heads, 512 jobs 120, 256 jobs 131.
 fka_status build_mx_jobs(fka_plan *p, int32_t blocks)
 {
     const int n_groups = p->n_groups;
-    int64_t units = 0;
+    int64_t prefix_tiles = 0;
     int32_t max_nseq = 1;
     for (int t = 0; t < n_groups; ++t) {
-        units += ceil_div(p->group_prefix_len[t], fka::kMxTile);
+        prefix_tiles += ceil_div(p->group_prefix_len[t], fka::kMxTile);
         max_nseq = std::max(max_nseq, p->group_start[t + 1] - p->group_start[t]);
     }
     const int32_t slices = fka::slices_of(p->max_suffix_len);
-    units += (int64_t)p->n_seqs * slices;
-    if (units * p->Hkv > (int64_t)1 << 30)
-        return fail(FKA_ERR_UNSUPPORTED, "prefix and suffixes of %lld tiles are too long", (long long)(units * p->Hkv));
+    const int64_t suffix_slices = (int64_t)p->n_seqs * slices;
+    if ((prefix_tiles + suffix_slices) * p->Hkv > (int64_t)1 << 30)
+        return fail(FKA_ERR_UNSUPPORTED, "prefix and suffixes of %lld tiles are too long", (long long)((prefix_tiles + suffix_slices) * p->Hkv));
     p->slot_rows = max_nseq * p->G;
     p->row_tiles = ceil_div(p->slot_rows, 16);
     hipError_t e = hipGetDevice(&p->device);
@@ -754,17 +758,20 @@ fka_status build_mx_jobs(fka_plan *p, int32_t blocks)
     const int per_cu = fka::mx_blocks_per_cu(p->d, p->row_tiles);
     if (per_cu <= 0) return fail(FKA_ERR_HIP, "occupancy query of the 4-bit decode kernel failed");
     p->waves = 4;
-    const int64_t resident = (int64_t)cus * per_cu;
-    const int64_t want = blocks > 0 ? std::min<int64_t>(blocks, 16 * resident) : resident;
-    const int64_t per = std::max<int64_t>(p->waves, (units * p->Hkv + want - 1) / want);
-    const int32_t shares = ceil_div(slices, per);  // of every suffix
+    // jobs of each kind; a prefix job has a whole number of tiles for each wave (each pair of waves past 32 rows)
+    const int64_t each = blocks > 0 ? std::max<int64_t>(1, std::min<int64_t>(blocks, 16 * (int64_t)cus * per_cu) / 2)
+                                    : (int64_t)cus * (n_groups > 1 || 4 * suffix_slices < prefix_tiles ? 2 : 1);
+    const int64_t step = p->slot_rows > 32 ? p->waves / 2 : p->waves;
+    const int64_t job_tiles = std::max<int64_t>(1, ((prefix_tiles * p->Hkv + each - 1) / each + step - 1) / step) * step;
+    const int64_t job_slices = std::max<int64_t>(p->waves, (suffix_slices * p->Hkv + each - 1) / each);
+    const int32_t shares = ceil_div(slices, job_slices);  // of every suffix
     p->rowrec.assign((size_t)p->n_seqs * p->Hq * fka::kRowRec, 0);
     int64_t slot = 0;
     int32_t tile0 = 0;
-    std::vector<fka::MxJob> tail;  // the suffixes' jobs, behind the prefixes': short ones fill the end
+    std::vector<fka::MxJob> tail;  // the suffixes' jobs, behind the prefixes'
     for (int t = 0; t < n_groups; ++t) {
         const int32_t s0 = p->group_start[t], nseq = p->group_start[t + 1] - s0, lp = p->group_prefix_len[t];
-        const int32_t tiles = ceil_div(lp, fka::kMxTile), parts = ceil_div(tiles, per);
+        const int32_t tiles = ceil_div(lp, fka::kMxTile), parts = ceil_div(tiles, job_tiles);
         for (int32_t g = 0; g < p->Hkv; ++g) {
             fka::MxJob j{};
             j.group = t;
@@ -804,6 +811,8 @@ fka_status build_mx_jobs(fka_plan *p, int32_t blocks)
         }
         tile0 += tiles;
     }
+    // the longest first, so that short ones fill the end
+    std::stable_sort(p->jobs.begin(), p->jobs.end(), [](const fka::MxJob &x, const fka::MxJob &y) { return x.end - x.begin > y.end - y.begin; });
     p->jobs.insert(p->jobs.end(), tail.begin(), tail.end());
     p->n_slots = (int32_t)slot;
     p->n_items = n_groups * p->Hkv;

@@ -280,9 +280,9 @@ __global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
             uint32_t odd = (vs[0] - 0x68686868u) & 0xe0e0e0e0u;
             if constexpr (HD == 128) odd |= (vs[1] - 0x68686868u) & 0xe0e0e0e0u;
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0) != 0, 0)) break;  // the loop behind takes the rest
-            // All scores of the tile, then its softmax, then p.v: the first two need K only, so V arrives behind them.
-            // Product (j, x) has keys 32 a + 8 j + 4 x + b in M row 4 a + b.
-            constexpr int J = 4;
+            // J steps of 32 keys at a time: their scores, their softmax, their p.v.  With one row tile all four, whose first two
+            // parts need K only, so that V arrives behind them; with two, two and two, which the registers hold.  Product (j, x) has keys 32 a + 8 j + 4 x + b in M row 4 a + b.
+            constexpr int J = NT == 1 ? 4 : 2;
 #pragma unroll
             for (int j0 = 0; j0 < 4; j0 += J) {
                 mx_f32x4 s[NT][2 * J];
@@ -435,19 +435,22 @@ __global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
         uint4 *ring = reinterpret_cast<uint4 *>(&stage[wave][0]);
         constexpr int VL = kSlice * CPR / 64;  // V loads per lane of a slice
         const int jt = l16 >> 2, m4 = l16 & 3, T0 = 4 * q4 + jt;
-        for (int sl = begin + wave; sl < end; sl += NW) {
-            const int valid = L - sl * kSlice;
-            const int bytes = min(valid, kSlice) * ROWB;  // rows at or past L read as zeros
-            const size_t off = base + (size_t)sl * kSlice * ROWB;
+        uint4 kr[2][NC], vr[VL];
+        auto load = [&](int sl) {
+            const int bytes = sl < end ? min(L - sl * kSlice, kSlice) * ROWB : 0;  // rows at or past L read as zeros
+            const size_t off = base + (size_t)(sl < end ? sl : 0) * kSlice * ROWB;
             const __amdgpu_buffer_rsrc_t rk = mx_rsrc(reinterpret_cast<const char *>(a.suffix_k) + off, bytes);
             const __amdgpu_buffer_rsrc_t rv = mx_rsrc(reinterpret_cast<const char *>(a.suffix_v) + off, bytes);
-            uint4 kr[2][NC], vr[VL];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int c = 0; c < NC; ++c) kr[u][c] = mx_load16(rk, (16 * u + l16) * ROWB + 64 * c + 16 * q4);
 #pragma unroll
             for (int i = 0; i < VL; ++i) vr[i] = mx_load16(rv, (64 * i + lane) * 16);
+        };
+        load(begin + wave);
+        for (int sl = begin + wave; sl < end; sl += NW) {
+            const int valid = L - sl * kSlice;
             mx_f32x4 s[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
@@ -455,8 +458,16 @@ __global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
 #pragma unroll
                 for (int c = 0; c < NC; ++c) s[u] = mx_mfma(__builtin_bit_cast(mx_bf16x8, kr[u][c]), qb[0][c], s[u]);
             }
+            // V through the wave's own LDS, read back transposed: chunk c of token T at T CPR + (c ^ 2 T mod CPR),
+            // so that a column read touches every bank (a wave's LDS operations run in order: no barrier)
+#pragma unroll
+            for (int i = 0; i < VL; ++i) {
+                const int p = 64 * i + lane, T = p / CPR, c = p % CPR;
+                ring[T * CPR + (c ^ ((2 * T) & (CPR - 1)))] = vr[i];
+            }
             mx_result_wait();
             mx_result(s[0]), mx_result(s[1]);
+            load(sl + NW);  // its time: the softmax and p.v
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -469,13 +480,6 @@ __global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
             mx_exp(x, a.scale_log2, m_ref[0], l_run[0]);
             mx_bf16x8 p3[3];
             mx_split3(x, p3);
-            // V through the wave's own LDS, read back transposed: chunk c of token T at T CPR + (c ^ 2 T mod CPR),
-            // so that a column read touches every bank (a wave's LDS operations run in order: no barrier)
-#pragma unroll
-            for (int i = 0; i < VL; ++i) {
-                const int p = 64 * i + lane, T = p / CPR, c = p % CPR;
-                ring[T * CPR + (c ^ ((2 * T) & (CPR - 1)))] = vr[i];
-            }
 #pragma unroll
             for (int e = 0; e < NE; ++e) {
                 // lane (q4, 4 j + m): tokens 4 q4 + j and 16 + 4 q4 + j, channels 16 e + 4 m ..
