@@ -20,8 +20,8 @@ def test_every_xdl_result_read_is_padded_around_the_cache():
     with tempfile.TemporaryDirectory() as d:
         asm = X.compile_asm(hipcc, os.path.join(ROOT, "paper_2608_13667_amd", "csrc", "kernels.hip"),
                             os.path.join(ROOT, "include"), os.path.join(d, "kernels.s"))
-    mx, weights = X.kernels(asm, "mx_partials_kernel"), X.kernels(asm, "key_weights_kernel")
-    assert len(mx) == 6 and len(weights) == 2
+    mx, weights = X.kernels(asm, "mx_partials_kernel"), X.kernels(asm, "key_weights")
+    assert len(mx) == 6 and len(weights) == 6
     for k in mx + weights:
         pairs = X.scan(asm, k)
         assert pairs, k

@@ -642,7 +642,8 @@ def ref_weights(q, lse, k, scale):
 
 @pytest.mark.parametrize("hq,hkv,d,R,L,decay", [
     (1, 1, 128, 1, 1, 0.0), (8, 2, 64, 5, 63, 0.5), (40, 8, 128, 5, 1000, 0.9), (5, 1, 128, 1, 257, 1.0), (8, 8, 64, 33, 64, 0.0),
-    (6, 3, 128, 0, 100, 0.25), (16, 1, 128, 64, 700, 0.0), (14, 2, 64, 17, 4097, 2.0)])
+    (6, 3, 128, 0, 100, 0.25), (16, 1, 128, 64, 700, 0.0), (14, 2, 64, 17, 4097, 2.0),
+    (16, 8, 128, 19, 8130, 0.5), (16, 16, 64, 40, 4030, 0.0)])
 def test_key_weights(fa, hq, hkv, d, R, L, decay):
     rng = np.random.default_rng(hq * 1000 + L)
     q, k = normal(rng, R, hq, d), normal(rng, hkv, L + 3, d)
