@@ -505,13 +505,15 @@ def lse_merge(part_o, part_lse, out, out_lse=None, stream=None):
     _check(_lib.fka_lse_merge(R, P, d, _p(part_o, "f32"), _p(part_lse, "f32"), _p(out, "f32"), _p(out_lse, "f32"), _stream(stream)))
 
 
-def _token_rows(t, what):
+def _token_rows(t, shape, what):
     """Token stride (elements) of q, k or v [N][n][heads][d]: any view whose tokens lie evenly apart."""
-    if t.dim() != 4 or t.stride(3) != 1 or (t.shape[2] > 1 and t.stride(2) != t.shape[3]):
+    N, n, heads, d = shape
+    seq, step, head, elem = t.stride()
+    if elem != 1 or (head != d and heads > 1):
         raise ValueError(f"{what} must be [N][n][heads][d] with the heads of a token dense")
-    N, n, heads, d = t.shape
-    step = t.stride(1) if n > 1 else t.stride(0) if N > 1 else heads * d
-    if N > 1 and n > 1 and t.stride(0) != n * step:
+    if n == 1:
+        return seq if N > 1 else heads * d
+    if N > 1 and seq != n * step:
         raise ValueError(f"the tokens of {what} must lie evenly apart")
     return step
 
@@ -521,33 +523,37 @@ def _on_current(t):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError("tensor must be on the GPU (the library reads device memory)")
     dev = t.get_device()
-    if dev != torch.cuda.current_device():
-        raise ValueError(f"tensor is on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+    current = torch.cuda.current_device() if _current_device is None else _current_device()
+    if dev != current:
+        raise ValueError(f"tensor is on cuda:{dev}, the current device is cuda:{current}")
     return dev
 
 
 def _strided(t, dev):
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.bfloat16:
+    if t.dtype is torch.bfloat16 and t.get_device() == dev:  # -1 on the CPU
+        return t.data_ptr()
+    if not t.is_cuda or t.dtype is not torch.bfloat16:
         raise ValueError("expected a bf16 tensor on the GPU")
-    if t.get_device() != dev:
-        raise ValueError(f"tensor is on cuda:{t.get_device()}, q is on cuda:{dev}")
-    return t.data_ptr()
+    raise ValueError(f"tensor is on cuda:{t.get_device()}, q is on cuda:{dev}")
 
 
-def _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, max_len, advance):
-    if any(not isinstance(t, torch.Tensor) for t in (q, k, v, positions, q_out)):
-        raise ValueError("expected a torch tensor")
-    steps = [_token_rows(t, what) for t, what in ((q, "q"), (k, "k"), (v, "v"))]
-    N, n, Hq, d = q.shape
-    Hkv = k.shape[2]
-    if k.shape != (N, n, Hkv, d) or v.shape != (N, n, Hkv, d):
+def _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, advance):
+    for t in (q, k, v, positions, q_out):
+        if not isinstance(t, torch.Tensor):
+            raise ValueError("expected a torch tensor")
+    shape, kv = q.shape, k.shape
+    if len(shape) != 4 or len(kv) != 4 or v.dim() != 4:
+        raise ValueError("q, k and v must be [N][n][heads][d]")
+    steps = _token_rows(q, shape, "q"), _token_rows(k, kv, "k"), _token_rows(v, v.shape, "v")
+    N, n, Hq, d = shape
+    if (kv[0], kv[1], kv[3]) != (N, n, d) or v.shape != kv:
         raise ValueError("k and v must be [N][n][Hkv][d] with q's N, n and d")
-    if q_out.shape != q.shape or positions.numel() != N * n:
+    if q_out.shape != shape or positions.numel() != N * n:
         raise ValueError("q_out must have q's shape, positions N n entries")
-    if any(w is not None and w.shape != (d,) for w in (q_weight, k_weight)):
+    if (q_weight is not None and q_weight.shape != (d,)) or (k_weight is not None and k_weight.shape != (d,)):
         raise ValueError("a norm weight must be [d]")
-    rot = 0 if freq is None else 2 * freq.numel()
-    return RotateDesc(N, n, Hq, Hkv, d, rot, int(bool(interleaved)), max_len, int(bool(advance)), eps, *steps)
+    return RotateDesc(N, n, Hq, kv[2], d, 0 if freq is None else 2 * freq.numel(), 1 if interleaved else 0, 0,
+                      1 if advance else 0, eps, *steps)
 
 
 def _check_lens(suffix_len, N):
@@ -559,10 +565,11 @@ def rotate_append(q, k, v, positions, freq, q_out, suffix_k, suffix_v, suffix_le
                   eps=1e-6, interleaved=False, max_len=None, advance=False, err=None, stream=None):
     """fka_rotate_append: q, k, v bf16 [N][n][heads][d] (views of a joint projection output allowed), positions int32 [N][n],
     freq fp64 [rotary_dim / 2] or None -> q_out, and rows of suffix_k / suffix_v bf16 [N][Hkv][cap][d]."""
-    desc = _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, 0, advance)
-    N, Hkv, d = desc.n_seqs, desc.n_kv_heads, desc.head_dim
-    cap = suffix_k.shape[2] if suffix_k.dim() == 4 else -1
-    if suffix_k.shape != (N, Hkv, cap, d) or suffix_v.shape != suffix_k.shape:
+    desc = _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, advance)
+    N, _, Hkv, d = k.shape
+    rows = suffix_k.shape
+    cap = rows[2] if len(rows) == 4 else -1
+    if rows != (N, Hkv, cap, d) or suffix_v.shape != rows:
         raise ValueError("suffix_k and suffix_v must be [N][Hkv][cap][d]")
     _check_lens(suffix_len, N)
     desc.max_len = cap if max_len is None else max_len
@@ -577,8 +584,8 @@ def rotate_append_paged(q, k, v, positions, freq, q_out, k_pool, v_pool, page_ta
                         q_weight=None, k_weight=None, eps=1e-6, interleaved=False, max_len=None, advance=False, err=None,
                         stream=None):
     """fka_rotate_append_paged: as rotate_append, into the pages of page_table int32 [N][max_pages] behind prefix_len int32 [N]."""
-    desc = _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, 0, advance)
-    N, Hkv, d = desc.n_seqs, desc.n_kv_heads, desc.head_dim
+    desc = _rotate_desc(q, k, v, positions, freq, q_out, q_weight, k_weight, eps, interleaved, advance)
+    N, _, Hkv, d = k.shape
     if k_pool.dim() != 4 or k_pool.shape[1:] != (Hkv, 16, d) or v_pool.shape != k_pool.shape:
         raise ValueError("k_pool and v_pool must be [pages][Hkv][16][d]")
     if page_table.dim() != 2 or page_table.shape[0] != N or prefix_len.numel() != N:
