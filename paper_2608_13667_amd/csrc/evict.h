@@ -174,41 +174,47 @@ __global__ __launch_bounds__(256, 2) void key_weights_few_kernel(WeightsArgs a)
     }
 }
 
-// Many query rows.  They pass through LDS 32 at a time, the next ones loading: read from L2 by each wave they were what bounded it (512
-// rows over 128k keys 289 us).  grid (ceil(len / 256), Hkv); SPLIT, for few keys: (ceil(len / 64), Hkv), where the four waves
-// of a block have the same 64 keys and every fourth 16-row tile each, joined at the end.
+typedef __attribute__((address_space(3))) void weights_lds;
+typedef const __attribute__((address_space(1))) void weights_global;
+
+// 16 bytes per lane from global memory into LDS at dst + 16 lane, past the registers.
+__device__ inline void weights_dma16(const void *src, void *dst)
+{
+    __builtin_amdgcn_global_load_lds((weights_global *)src, (weights_lds *)dst, 16, 0, 0);
+}
+
+// Many query rows: bound by the products and the exponentials, which three waves of a SIMD overlap (one wave that computes a
+// tile's exponentials beside the next one's products, at two waves a SIMD, was slower: 190 us against 168).  The rows pass
+// through LDS 64 at a time, the next ones on their way meanwhile: 512 rows over 128k keys x 8 heads 165 us (832 TF/s; by way of
+// registers, 32 at a time, 176; read from L2 by each wave 289).  grid (ceil(len / 256), Hkv); SPLIT, for few keys:
+// (ceil(len / 64), Hkv), where the four waves of a block have the same 64 keys and every fourth 16-row tile each, joined at the end.
 template <int HD, bool SPLIT>
 __global__ __launch_bounds__(256, 3) void key_weights_kernel(WeightsArgs a)
 {
-    constexpr int CPR = HD / 8, QR = SPLIT ? 64 : 32, QL = QR * CPR / 256;
+    constexpr int CPR = HD / 8, QR = 64, QL = QR * CPR / 256;
     __shared__ uint4 qs[2][QR * CPR];  // chunk c of row r at r CPR + (c ^ r mod CPR): a read of 16 rows touches every bank
     __shared__ float nls[2][QR];
     __shared__ float part[SPLIT ? 4 : 1][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, q4 = lane >> 4, head = blockIdx.y;
     const int key0 = (SPLIT ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave) * kWeightsKeys;
-    uint4 qr[QL];
     float nl_next = 0.f;
-    auto fetch = [&](int64_t r0) {
+    auto fetch = [&](int64_t r0, int buf) {
 #pragma unroll
         for (int i = 0; i < QL; ++i) {
-            const int64_t r = r0 + (tid + 256 * i) / CPR;
-            qr[i] = uint4{0, 0, 0, 0};
-            if (r < a.n_rows) qr[i] = *reinterpret_cast<const uint4 *>(a.q + weights_row(a, head, (int32_t)r) * HD + (tid % CPR) * 8);
+            const int r = (tid + 256 * i) / CPR, c = tid % CPR;
+            const int64_t row = min(r0 + r, a.n_rows - 1);  // (rows past the end have weight 0)
+            weights_dma16(a.q + weights_row(a, head, (int32_t)row) * HD + (c ^ (r & (CPR - 1))) * 8, &qs[buf][256 * i + 64 * wave]);
         }
         nl_next = -INFINITY;
         if (tid < QR && r0 + tid < a.n_rows) nl_next = weights_offset(a.lse[weights_row(a, head, (int32_t)(r0 + tid))]);
     };
     auto put = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < QL; ++i) {
-            const int r = (tid + 256 * i) / CPR, c = tid % CPR;
-            qs[buf][r * CPR + (c ^ (r & (CPR - 1)))] = qr[i];
-        }
         if (tid < QR) nls[buf][tid] = nl_next;
+        __builtin_amdgcn_s_waitcnt(0xf70);  // vmcnt(0): this wave's rows are in LDS
     };
     float w[4][4] = {};
-    fetch(0);  // in front of the keys, so that they are still on their way while the rows pass into LDS
+    fetch(0, 0);
     mx_bf16x8 kb[4][HD / 32];
     weights_keys<HD>(a, head, key0, l16, q4, kb);
     const int key = key0 + weights_key(l16, q4);
@@ -217,7 +223,7 @@ __global__ __launch_bounds__(256, 3) void key_weights_kernel(WeightsArgs a)
     __syncthreads();
     for (int64_t r0 = 0; r0 < a.n_rows; r0 += QR) {
         const int buf = (int)(r0 / QR) & 1;
-        if (r0 + QR < a.n_rows) fetch(r0 + QR);
+        if (r0 + QR < a.n_rows) fetch(r0 + QR, buf ^ 1);  // whose readers are a barrier behind
         if constexpr (SPLIT) {
             weights_tile<HD>(qs[buf], nls[buf][16 * wave + l16], 16 * wave + l16, q4, kb, a.scale_log2, w);
         } else {
@@ -225,7 +231,7 @@ __global__ __launch_bounds__(256, 3) void key_weights_kernel(WeightsArgs a)
             for (int t = 0; t < QR / 16; ++t)
                 weights_tile<HD>(qs[buf], nls[buf][16 * t + l16], 16 * t + l16, q4, kb, a.scale_log2, w);
         }
-        if (r0 + QR < a.n_rows) put(buf ^ 1);  // its readers are a barrier behind
+        if (r0 + QR < a.n_rows) put(buf ^ 1);
         __syncthreads();
     }
     float sum = weights_sum(l16, w);
@@ -540,8 +546,8 @@ inline hipError_t launch_key_weights_kernel(const WeightsArgs &a, int head_dim, 
         const dim3 grid(groups < per_head ? groups : per_head, a.n_kv_heads);
         head_dim == 128 ? key_weights_few_kernel<128><<<grid, dim3(256), 0, s>>>(a) : key_weights_few_kernel<64><<<grid, dim3(256), 0, s>>>(a);
     } else {
-        // fewer blocks than CUs leave CUs idle: 512 rows, 4096 keys x 2 heads 20.9 us whole and 10.9 split, x 8 heads 22.3 and
-        // 15.7; 8192 x 8, as many blocks as CUs, 22.6 and 25.7
+        // fewer blocks than CUs leave CUs idle: 512 rows, 4096 keys x 2 heads 20.9 us whole and 10.4 split, x 8 heads 22.3 and
+        // 14.1; 8192 x 8, as many blocks as CUs, 22.6 and 25.7
         const bool split = (int64_t)groups * a.n_kv_heads < 256;
         const dim3 grid(split ? (a.len + kWeightsKeys - 1) / kWeightsKeys : groups, a.n_kv_heads), block(256);
         if (head_dim == 128)
@@ -556,10 +562,10 @@ inline hipError_t launch_evict_kernels(const EvictArgs &a, hipStream_t s)
 {
     if (a.keep <= 0) return hipSuccess;
     const dim3 block(kEvictThreads), chunks(a.chunks, a.n_kv_heads), heads(a.n_kv_heads);
+    // 8 heads, with 256 rows' copies: 8192 positions in one block's registers 12.8 us, a kernel per digit 22.1; past them, 32 to a
+    // thread, 16384 24.8 and 23.6, 32768 31.3 and 25.7
     if (a.len <= 8 * kEvictThreads) {
         evict_one_kernel<8><<<heads, block, 0, s>>>(a);
-    } else if (a.len <= 32 * kEvictThreads) {
-        evict_one_kernel<32><<<heads, block, 0, s>>>(a);
     } else {
         if (a.keep > a.n_first + a.n_last) {
             evict_hist_kernel<8, 0><<<chunks, block, 0, s>>>(a);

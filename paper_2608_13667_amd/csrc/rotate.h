@@ -186,6 +186,8 @@ void launch_rotate_hd(const RotateArgs &a, hipStream_t s)
 {
     const int tokens = a.n_seqs * a.n_tokens;
     const int per = 1024 / HD, units = (a.n_q_heads + per - 1) / per + 2 * ((a.n_kv_heads + per - 1) / per);
+    // a wave to a token computes its angles once, but only many tokens fill the GPU that way; 40 + 8 + 8 heads of 128: one
+    // token 6.6 us by wave and 3.6 by block, 1024 tokens 9.2 and 8.1, 2048 13.1 and 14.2, 8192 37.6 and 43.1
     if (tokens >= 2048)
         rotate_kernel<HD, INTERLEAVED, true><<<dim3((tokens + 3) / 4), dim3(256), 0, s>>>(a);
     else
