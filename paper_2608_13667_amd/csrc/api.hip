@@ -764,7 +764,8 @@ fka_status build_mx_jobs(fka_plan *p, int32_t blocks)
     const int64_t step = p->slot_rows > 32 ? p->waves / 2 : p->waves;
     const int64_t job_tiles = std::max<int64_t>(1, ((prefix_tiles * p->Hkv + each - 1) / each + step - 1) / step) * step;
     const int64_t job_slices = std::max<int64_t>(p->waves, (suffix_slices * p->Hkv + each - 1) / each);
-    const int32_t shares = ceil_div(slices, job_slices);  // of every suffix
+    // of every suffix; a plan without any keys keeps one, whose blocks find the lengths and leave empty parts
+    const int32_t shares = std::max<int32_t>(ceil_div(slices, job_slices), prefix_tiles == 0 ? 1 : 0);
     p->rowrec.assign((size_t)p->n_seqs * p->Hq * fka::kRowRec, 0);
     int64_t slot = 0;
     int32_t tile0 = 0;

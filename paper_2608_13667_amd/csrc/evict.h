@@ -263,7 +263,7 @@ struct EvictLds {
     int32_t wave[kEvictThreads / 64];
     int32_t bin, want;
     int32_t sums[3];
-    uint32_t ranks[32 * kEvictThreads / 64];  // per (load, wave): keys above the threshold << 16, keys at it
+    uint32_t ranks[8 * kEvictThreads / 64];  // per (load, wave): keys above the threshold << 16, keys at it
 };
 
 // The bin that holds the want-th largest key: thread t has the counts of bins 2047 - 2 t and 2046 - 2 t.
@@ -406,7 +406,7 @@ __device__ inline void evict_sum(const EvictArgs &a, int head, int digit, int (&
     const uint2 *h = reinterpret_cast<const uint2 *>(a.hist) +
                      ((size_t)digit * a.n_kv_heads + head) * a.chunks * (kEvictBins / 2) + (kEvictBins / 2 - 1 - threadIdx.x);
     all[0] = all[1] = own[0] = own[1] = front[0] = front[1] = 0;
-#pragma unroll 8
+#pragma unroll 16
     for (int c = 0; c < a.chunks; ++c) {
         const uint2 v = h[(size_t)c * (kEvictBins / 2)];  // the higher bin is y
         all[0] += v.y;

@@ -493,6 +493,24 @@ def test_mx_sequences_without_keys(fa):
     m.check(out, lse, "empty")
 
 
+def test_mx_plan_without_any_keys(fa):
+    """No prefix and no room for a suffix: the lengths on the device are looked at all the same."""
+    m = Mx(fa, 41, 10, 2, 64, [2, 1], [0, 0], [0, 0, 0], max_suffix=0)
+    out, lse = m.decode()
+    assert (out == 0).all() and np.isneginf(lse).all() and m.plan.device_error() == 0
+    m.dev["suffix_len"].copy_(dev_i32([0, 3, 0]))
+    out, lse = m.decode()
+    assert (out == 0).all() and np.isneginf(lse).all()
+    assert m.plan.device_error() == fa.ERR_SUFFIX_CLAMPED
+    before = m.dev["suffix_k"].clone()
+    kn = dev_bf16(normal(np.random.default_rng(2), 3, 2, 64))
+    out, lse = m.outs()
+    m.dev["suffix_len"].zero_()
+    m.plan.step_mx(m.dev["q"], kn, kn, m.tiles, m.dev["suffix_k"], m.dev["suffix_v"], m.dev["suffix_len"], out, lse)
+    assert m.plan.device_error() == fa.ERR_APPEND_NO_ROOM
+    assert torch.equal(before.view(torch.int16), m.dev["suffix_k"].view(torch.int16))
+
+
 def test_mx_bad_tile_ids_count_as_zeros(fa):
     m = Mx(fa, 35, 8, 2, 128, [3], [500], [9, 0, 40], table=True)
     m.table[0, 1], m.table[0, 3] = -1, 2 ** 31 - 1
