@@ -439,6 +439,7 @@ typedef struct {
  *   suffix_k           bf16 [N][Hkv][suffix_cap][d], rows [suffix_len[b], suffix_len[b] + n) written (suffix_v likewise)
  *   suffix_len         int32 [N] (device), or NULL: rows from 0
  *   err                int32 (device) or NULL
+ * What is written, the cache and (but for q itself) q_out, may not overlap what is read.
  * A sequence without room (suffix_len[b] negative, or past max_len with the new tokens) keeps its cache and length
  * and bit 2 is or-ed into *err; its q_out is written.  Errors: FKA_ERR_INVALID_ARG, FKA_ERR_UNSUPPORTED (head_dim,
  * rotary_dim not a multiple of 16, too many tokens).
@@ -475,7 +476,8 @@ size_t fka_mx_tile_bytes(int32_t n_kv_heads, int32_t head_dim);
 /* Pack positions [from, len) of a prefix, from a multiple of 128 (the last tile of a prefix that grows is packed again).
  *   k_src, v_src  bf16 [Hkv][src_cap][d], position p in row p - from
  *   tiles         pool of n_pool_tiles tiles, 16-byte aligned
- *   tile_row      int32 [ceil(len / 128)] (device), the id of the tile of positions 128 i ..; NULL: id i
+ *   tile_row      int32 [ceil(len / 128)] (device), the id of the tile of positions 128 i .. (a different one for each that is
+ *                 written: two with one id would be mixed); NULL: id i
  *   err           int32 (device) or NULL: bit 4 for an id outside [0, n_pool_tiles), whose tile is not written */
 fka_status fka_mx_pack(int32_t n_kv_heads, int32_t head_dim, int32_t from, int32_t len, const void *k_src, const void *v_src,
                        int32_t src_cap, void *tiles, const int32_t *tile_row, int32_t n_pool_tiles, int32_t *err, void *stream);
@@ -548,7 +550,8 @@ size_t fka_evict_bytes(int32_t n_kv_heads, int32_t len);
  * positions are copied in order; the next plan's prefix_len is keep (keys carry their rotation, so their positions stay theirs).
  *   k, v         bf16 [Hkv][kv_cap][d];  weights fp32 [Hkv][weights_cap]
  *   index        int32 [Hkv][keep]: the kept positions, ascending
- *   k_out, v_out bf16 [Hkv][keep][d];  weights_out fp32 [Hkv][keep] or NULL; none may overlap an input
+ *   k_out, v_out bf16 [Hkv][keep][d];  weights_out fp32 [Hkv][keep] or NULL; none may overlap an input or another
+ *                (FKA_ERR_INVALID_ARG)
  *   workspace    fka_evict_bytes(Hkv, len) device bytes (16-byte aligned), used by one call at a time; its contents before and after do not matter
  */
 fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t keep, int32_t n_first, int32_t n_last,

@@ -2139,6 +2139,27 @@ fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t 
     REQUIRE_PTR16(workspace);
     const size_t need = fka_evict_bytes(n_kv_heads, len);
     REQUIRE(workspace_bytes >= need, "workspace of %zu bytes, %zu are needed", workspace_bytes, need);
+    // what the kernels write must not be what others of their blocks still read
+    const struct {
+        const void *at;
+        size_t bytes;
+        const char *name;
+    } all[] = {
+        {k, (((size_t)n_kv_heads - 1) * kv_cap + len) * head_dim * 2, "k"},
+        {v, (((size_t)n_kv_heads - 1) * kv_cap + len) * head_dim * 2, "v"},
+        {weights, (((size_t)n_kv_heads - 1) * weights_cap + len) * 4, "weights"},
+        {index, (size_t)n_kv_heads * keep * 4, "index"},
+        {k_out, (size_t)n_kv_heads * keep * head_dim * 2, "k_out"},
+        {v_out, (size_t)n_kv_heads * keep * head_dim * 2, "v_out"},
+        {weights_out, weights_out ? (size_t)n_kv_heads * keep * 4 : 0, "weights_out"},
+        {workspace, need, "workspace"},
+    };
+    for (int i = 3; i < 8; ++i)
+        for (int j = 0; j < i; ++j) {
+            const uintptr_t x = reinterpret_cast<uintptr_t>(all[i].at), y = reinterpret_cast<uintptr_t>(all[j].at);
+            REQUIRE(all[i].bytes == 0 || all[j].bytes == 0 || x >= y + all[j].bytes || y >= x + all[i].bytes, "%s overlaps %s",
+                    all[i].name, all[j].name);
+        }
     fka::EvictArgs a{};
     a.k = static_cast<const uint16_t *>(k);
     a.v = static_cast<const uint16_t *>(v);

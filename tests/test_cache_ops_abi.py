@@ -131,6 +131,24 @@ def test_evict_rejects(fa, over, status, needle):
     assert st == status and needle in fa.last_error()
 
 
+@pytest.mark.parametrize("name", ["index", "k_out", "v_out", "weights_out", "work"])
+def test_evict_rejects_overlaps(fa, name):
+    """Each of what it writes against each other range, overlapping by a few bytes at either end; ranges that only touch would pass."""
+    hkv, d, n, cap, keep = 2, 64, 100, 128, 50
+    size = dict(k=(cap + n) * d * 2, v=(cap + n) * d * 2, weights=(cap + n) * 4, index=hkv * keep * 4, k_out=hkv * keep * d * 2,
+                v_out=hkv * keep * d * 2, weights_out=hkv * keep * 4, work=fa.raw_call("fka_evict_bytes", hkv, n))
+    for other in size:
+        if other == name:
+            continue
+        for shift in (16 - size[name] + size[name] % 16, (size[other] - 16) // 16 * 16, 0):
+            at = {x: (1 << 30) + (i << 24) for i, x in enumerate(size)}
+            at[name] = at[other] + shift
+            p = {x: C.c_void_p(y) for x, y in at.items()}
+            st = fa.raw_call("fka_evict", hkv, d, n, keep, 4, 10, p["k"], p["v"], cap, p["weights"], cap, p["index"], p["k_out"],
+                             p["v_out"], p["weights_out"], p["work"], size["work"], None)
+            assert st == -1 and "overlaps" in fa.last_error() and name.replace("work", "workspace") in fa.last_error(), (other, shift)
+
+
 def test_evict_sizes(fa):
     lib = fa._lib
     assert lib.fka_evict_bytes(0, 5) == 0 and lib.fka_evict_bytes(2, -1) == 0
