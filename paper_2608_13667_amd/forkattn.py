@@ -211,6 +211,7 @@ class Plan:
         self.paged = paged
         self.heads = heads
         self.n_seqs = n_seqs
+        self._mx = None  # of a plan over 4-bit tiles: tiles of the pool, a tile's shape, entries of the tile table
 
     @classmethod
     def contig(cls, n_q_heads, n_kv_heads, head_dim, n_branches, prefix_len, suffix_cap, max_suffix_len,
@@ -285,10 +286,22 @@ class Plan:
         d = MxDesc(int(gs[-1]), len(gl), max_tiles, n_pool_tiles, suffix_cap, max_suffix_len, blocks)
         out = _vp()
         _check(_lib.fka_plan_create_mx(C.byref(h), C.byref(d), gs.ctypes.data_as(_vp), gl.ctypes.data_as(_vp), C.byref(out)))
-        return cls(out.value, False, h, int(gs[-1]))
+        plan = cls(out.value, False, h, int(gs[-1]))
+        plan._mx = n_pool_tiles, (n_kv_heads, 136 * head_dim), len(gl) * max_tiles
+        return plan
+
+    def _mx_tiles(self, tiles, tile_table):
+        if self._mx is None:
+            return  # refused by the call
+        n, of, entries = self._mx
+        if n and (tiles is None or tiles.dim() != 3 or tiles.shape[0] < n or tiles.shape[1:] != of):
+            raise ValueError(f"tiles must be uint8 [{n}][{of[0]}][{of[1]}], the pool that the plan was made for")
+        if tile_table is not None and tile_table.numel() < entries:
+            raise ValueError(f"tile_table must have {entries} entries, the plan's groups x max_tiles")
 
     def decode_mx(self, q, tiles, suffix_k, suffix_v, suffix_len, out, out_lse=None, tile_table=None, stream=None):
         """fka_fork_decode_mx: tiles uint8 [pool][Hkv][136 d], tile_table int32 [groups][max_tiles] or None."""
+        self._mx_tiles(tiles, tile_table)
         d = self.device
         _check(_lib.fka_fork_decode_mx(self._h, _p(q, "bf16", d), _p(tiles, "u8", d), _p(tile_table, "i32", d),
                                        _p(suffix_k, "bf16", d), _p(suffix_v, "bf16", d), _p(suffix_len, "i32", d),
@@ -296,6 +309,7 @@ class Plan:
 
     def step_mx(self, q, k_new, v_new, tiles, suffix_k, suffix_v, suffix_len, out, out_lse=None, tile_table=None, stream=None):
         """fka_fork_step_mx: append and decode."""
+        self._mx_tiles(tiles, tile_table)
         d = self.device
         _check(_lib.fka_fork_step_mx(self._h, _p(q, "bf16", d), _p(k_new, "bf16", d), _p(v_new, "bf16", d), _p(tiles, "u8", d),
                                      _p(tile_table, "i32", d), _p(suffix_k, "bf16", d), _p(suffix_v, "bf16", d),

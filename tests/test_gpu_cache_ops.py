@@ -511,6 +511,15 @@ def test_mx_plan_without_any_keys(fa):
     assert torch.equal(before.view(torch.int16), m.dev["suffix_k"].view(torch.int16))
 
 
+def test_mx_pool_of_another_size_is_refused(fa):
+    m = Mx(fa, 42, 8, 2, 64, [2, 1], [300, 100], [3, 4, 5], table=True)
+    for tiles, table in ((m.tiles[:-1], m.dev_table), (m.tiles[:, :1].contiguous(), m.dev_table), (m.tiles, m.dev_table[:1])):
+        with pytest.raises(ValueError, match="tile"):
+            out, lse = m.outs()
+            m.plan.decode_mx(m.dev["q"], tiles, m.dev["suffix_k"], m.dev["suffix_v"], m.dev["suffix_len"], out, lse, table)
+    m.check(*m.decode(), "its own pool")
+
+
 def test_mx_bad_tile_ids_count_as_zeros(fa):
     m = Mx(fa, 35, 8, 2, 128, [3], [500], [9, 0, 40], table=True)
     m.table[0, 1], m.table[0, 3] = -1, 2 ** 31 - 1
