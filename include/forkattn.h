@@ -466,8 +466,8 @@ fka_status fka_rotate_append_paged(const fka_rotate_desc *desc, const void *q, c
  * at most 6 2^E.  A block that holds an infinity or a NaN becomes all NaN.  Values on normal data come back with 19 dB
  * signal to noise.
  * The prefix is cut into tiles of 128 tokens (all KV heads; fka_mx_tile_bytes bytes, 136 d per KV head, in an order of the
- * library's own), which live in a pool indexed by tile id.  A tile's unused tokens are written as zeros.  fka_pool_*
- * can count the tiles' references as it does the pages'.
+ * library's own), which live in a pool indexed by tile id.  A tile's unused tokens are written as zeros.  A pool of
+ * fka_pool_create's ids can stand for tiles as well as for pages (fka_pool_alloc, fka_pool_retain, fka_pool_release).
  */
 
 /* Bytes of one tile of all KV heads; 0 for a head_dim other than 64 and 128. */
