@@ -211,7 +211,7 @@ class Plan:
         self.paged = paged
         self.heads = heads
         self.n_seqs = n_seqs
-        self._mx = None  # of a plan over 4-bit tiles: tiles of the pool, a tile's shape, entries of the tile table
+        self._mx = None  # of a plan over 4-bit tiles: the pool's shape, entries of the tile table
 
     @classmethod
     def contig(cls, n_q_heads, n_kv_heads, head_dim, n_branches, prefix_len, suffix_cap, max_suffix_len,
@@ -287,15 +287,16 @@ class Plan:
         out = _vp()
         _check(_lib.fka_plan_create_mx(C.byref(h), C.byref(d), gs.ctypes.data_as(_vp), gl.ctypes.data_as(_vp), C.byref(out)))
         plan = cls(out.value, False, h, int(gs[-1]))
-        plan._mx = n_pool_tiles, (n_kv_heads, 136 * head_dim), len(gl) * max_tiles
+        plan._mx = (n_pool_tiles, n_kv_heads, 136 * head_dim), len(gl) * max_tiles
         return plan
 
     def _mx_tiles(self, tiles, tile_table):
         if self._mx is None:
             return  # refused by the call
-        n, of, entries = self._mx
-        if n and (tiles is None or tiles.dim() != 3 or tiles.shape[0] < n or tiles.shape[1:] != of):
-            raise ValueError(f"tiles must be uint8 [{n}][{of[0]}][{of[1]}], the pool that the plan was made for")
+        want, entries = self._mx
+        got = () if tiles is None else tiles.shape
+        if want != got and want[0] and (len(got) != 3 or got[0] < want[0] or got[1:] != want[1:]):
+            raise ValueError(f"tiles must be uint8 {list(want)}, the pool that the plan was made for")
         if tile_table is not None and tile_table.numel() < entries:
             raise ValueError(f"tile_table must have {entries} entries, the plan's groups x max_tiles")
 
