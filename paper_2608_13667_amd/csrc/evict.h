@@ -263,7 +263,7 @@ struct EvictLds {
     int32_t wave[kEvictThreads / 64];
     int32_t bin, want;
     int32_t sums[3];
-    uint32_t ranks[8 * kEvictThreads / 64];  // per (load, wave): keys above the threshold << 16, keys at it
+    uint32_t ranks[16 * kEvictThreads / 64];  // per (load, wave): keys above the threshold << 16, keys at it
 };
 
 // The bin that holds the want-th largest key: thread t has the counts of bins 2047 - 2 t and 2046 - 2 t.
@@ -562,10 +562,12 @@ inline hipError_t launch_evict_kernels(const EvictArgs &a, hipStream_t s)
 {
     if (a.keep <= 0) return hipSuccess;
     const dim3 block(kEvictThreads), chunks(a.chunks, a.n_kv_heads), heads(a.n_kv_heads);
-    // 8 heads, with 256 rows' copies: 8192 positions in one block's registers 12.8 us, a kernel per digit 22.1; past them, 32 to a
-    // thread, 16384 24.8 and 23.6, 32768 31.3 and 25.7
+    // one block's registers (1024 threads) or a kernel per digit, 8 heads, with 256 rows' copies: 8192 positions 12.8 and 22.1 us,
+    // 16384 at 16 a thread 18.8 and 23.6, 32768 at 32 a thread 31.3 and 25.7
     if (a.len <= 8 * kEvictThreads) {
         evict_one_kernel<8><<<heads, block, 0, s>>>(a);
+    } else if (a.len <= 16 * kEvictThreads) {
+        evict_one_kernel<16><<<heads, block, 0, s>>>(a);
     } else {
         if (a.keep > a.n_first + a.n_last) {
             evict_hist_kernel<8, 0><<<chunks, block, 0, s>>>(a);

@@ -793,7 +793,7 @@ def test_evict_long(fa):
     run_evict(fa, np.exp(1.5 * rng.standard_normal((2, 131072))).astype(np.float32), 32768, 4, 512)
 
 
-@pytest.mark.parametrize("L", [8191, 8192, 8193, 32767, 32768, 32769, 40000, 73729, 600001])
+@pytest.mark.parametrize("L", [8191, 8192, 8193, 12289, 16383, 16384, 16385, 32767, 32768, 32769, 40000, 73729, 600001])
 def test_evict_at_the_kernels_sizes(fa, L):
     """Around the lengths where a block, several blocks, and several groups of positions per block take a head; values that differ
     in each of the three digits, many equal ones, and the choice's border at every place."""
