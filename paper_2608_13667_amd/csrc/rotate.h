@@ -11,6 +11,9 @@
 // A head is held by d / 16 lanes, 16 channels each: the two 8-channel chunks whose pairs it rotates, so
 // that the pairs stay within a lane and the norm's sum is two or three steps across lanes.  A wave takes
 // 1024 / d heads at a time (a unit).
+//
+// Bound by the bytes for many tokens: 32768 of 40 + 8 + 8 heads of 128 (0.94 GB read and written) 186 us, 5.0 TB/s, the
+// rate of a large copy; by latency for few, five tokens 4.3 us.
 #pragma once
 
 #include "internal.h"
