@@ -299,9 +299,15 @@ __device__ inline void evict_hist(EvictLds &l, const uint32_t (&k)[E], uint32_t 
     __syncthreads();
     const int above = digit == 0 ? 31 : evict_shift(digit - 1);  // the digits before it start here
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-        if ((in >> i & 1) && (digit == 0 || (k[i] >> above) == (key >> above)))
-            atomicAdd(&l.bins[(k[i] >> evict_shift(digit)) & evict_mask(digit)], 1u);
+    for (int i = 0; i < E; ++i) {
+        if (!(in >> i & 1) || (digit != 0 && (k[i] >> above) != (key >> above))) continue;
+        const uint32_t bin = (k[i] >> evict_shift(digit)) & evict_mask(digit);
+        // one bin's lanes together: many equal keys (a fresh cache's zeros) would follow one another on its address
+        // (8192 equal ones 31 us, 13 so)
+        const bool first = bin == (uint32_t)__builtin_amdgcn_readfirstlane((int)bin);
+        const uint64_t same = __builtin_amdgcn_ballot_w64(first);
+        if (!first || (tid & 63) == __builtin_ctzll(same)) atomicAdd(&l.bins[bin], first ? (uint32_t)__builtin_popcountll(same) : 1u);
+    }
     __syncthreads();
 }
 
@@ -563,8 +569,8 @@ inline hipError_t launch_evict_kernels(const EvictArgs &a, hipStream_t s)
 {
     if (a.keep <= 0) return hipSuccess;
     const dim3 block(kEvictThreads), chunks(a.chunks, a.n_kv_heads), heads(a.n_kv_heads);
-    // one block's registers (1024 threads) or a kernel per digit, 8 heads, with 256 rows' copies: 8192 positions 12.8 and 22.1 us,
-    // 16384 at 16 a thread 18.8 and 23.6, 32768 at 32 a thread 31.3 and 25.7
+    // one block's registers (1024 threads) or a kernel per digit, 8 heads, with 256 rows' copies: 8192 positions 13.3 and 22.1 us,
+    // 16384 at 16 a thread 19.5 and 23.6, 32768 at 32 a thread 31.3 and 25.7
     if (a.len <= 8 * kEvictThreads) {
         evict_one_kernel<8><<<heads, block, 0, s>>>(a);
     } else if (a.len <= 16 * kEvictThreads) {
