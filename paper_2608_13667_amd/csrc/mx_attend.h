@@ -507,6 +507,37 @@ __global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
                 for (int n = 0; n < 3; ++n) acc[0][e] = mx_mfma(__builtin_bit_cast(mx_bf16x8, v), p3[n], acc[0][e]);
             }
         }
+        // An infinite value has met the three terms of p, of either sign or zero: NaN, where the result is that infinity (of both
+        // signs: NaN).  So where a sum is not finite (products of pairs tell in few steps), the channel's values are looked up.
+        mx_result_wait();
+        float fold = 0.f;
+#pragma unroll
+        for (int e = 0; e < NE; ++e) {
+            mx_result(acc[0][e]);
+            fold = __builtin_fmaf(acc[0][e][0], acc[0][e][1], fold);
+            fold = __builtin_fmaf(acc[0][e][2], acc[0][e][3], fold);
+        }
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(__builtin_fabsf(fold) < INFINITY)) != 0, 0)) {
+            // lane l looks at channels CL l .. of this wave's keys; bits 3 i of `seen`: channel CL l + i has +inf, -inf, a NaN
+            constexpr int CL = HD / 64;
+            const uint16_t *v = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(a.suffix_v) + base);
+            uint32_t seen = 0;
+            for (int sl = begin + wave; sl < end; sl += NW)
+                for (int k = sl * kSlice; k < min(L, (sl + 1) * kSlice); ++k)
+#pragma unroll
+                    for (int i = 0; i < CL; ++i) {
+                        const uint32_t x = v[(size_t)k * HD + CL * lane + i];
+                        seen |= (x == 0x7f80u ? 1u : x == 0xff80u ? 2u : (x & 0x7fffu) > 0x7f80u ? 4u : 0u) << (3 * i);
+                    }
+#pragma unroll
+            for (int e = 0; e < NE; ++e)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = 16 * e + 4 * q4 + j;
+                    const uint32_t f = (uint32_t)__shfl((int)seen, c / CL) >> (3 * (c % CL)) & 7u;
+                    if (f == 1 || f == 2) acc[0][e][j] = f == 1 ? INFINITY : -INFINITY;
+                }
+        }
     }
 
     // ---- the waves' (max, sum, accumulator) into one partial per row
