@@ -13,8 +13,8 @@
 // in its M row, its 16 bytes of V 32 keys of the channel in its M row, and the keys of S^T that a lane gets in two
 // products (x = 0, 1) are the eight that it has to supply as P in the one with its V bytes: nothing crosses lanes
 // and no tile passes through LDS.  Codes become bf16 (K) and fp16 (V) by v_cvt_scalef32_pk_*_fp4, exactly.  p enters
-// the second product as two fp16 terms (2^-21 of p; two bf16 terms left 2e-6 in the output, one 1e-3), times
-// 2^7 so that the second term of a small p is no subnormal.  A tile with a V scale outside fp16's exact
+// the second product as two fp16 terms (mx_split16; two bf16 terms left 2e-6 in the output, one 1e-3), times
+// 2^7 so that the second term is a normal number down to p = 2^-9 of the reference.  A tile with a V scale outside fp16's exact
 // range, [2^-23, 2^8], takes bf16 and three terms instead, as do the suffixes, whose values are bf16.  The
 // running maximum is a reference only: it moves when a score passes it by 2^8.
 //
@@ -135,7 +135,7 @@ __device__ __attribute__((always_inline)) inline float mx_max(const float (&x)[N
 }
 
 // x becomes p = 2^(scaled x - reference + kMxShift), summed into l_run.  The shift keeps the second fp16
-// term of small p from the subnormals; with the gap of 2^8 a p is at most 2^15.
+// term of p from the subnormals down to 2^-9 of the reference; with the gap of 2^8 a p is at most 2^15.
 constexpr float kMxShift = 7.f;
 template <int N>
 __device__ __attribute__((always_inline)) inline void mx_exp(float (&x)[N], float scale_log2, float m_ref, float &l_run)
@@ -162,14 +162,20 @@ __device__ __attribute__((always_inline)) inline float mx_rest(uint32_t h, float
     return r;
 }
 
-// Eight p as two fp16 terms, each cut (not rounded: one instruction for two values), 2^-21 of p together.
+// Eight p as two fp16 terms, both to nearest (v_cvt_pk_f16_f32 takes two values, as the instruction that cuts does): within 2^-23 of p
+// down to 2^-9 of the reference, below it, where the second term is a subnormal, within 2^-32 of the reference.  To nearest, since a second
+// term that is never negative is lost one way: added to a sum 2^24 times as large it rounds to nothing, and 2^19 keys of value 1
+// with some 2^-16 of the largest weight each came out 2.4e-4 short, 1e-7 this way (the mean of 128 rows).
 __device__ __attribute__((always_inline)) inline void mx_split16(const float *p, mx_f16x8 &hi, mx_f16x8 &lo)
 {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    auto pair = [](float x, float y) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, f16x2)); };
     uint32_t h[4], l[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        h[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(p[2 * i], p[2 * i + 1]));
-        l[i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(mx_rest<0>(h[i], p[2 * i]), mx_rest<1>(h[i], p[2 * i + 1])));
+        h[i] = pair(p[2 * i], p[2 * i + 1]);
+        l[i] = pair(mx_rest<0>(h[i], p[2 * i]), mx_rest<1>(h[i], p[2 * i + 1]));
     }
     hi = __builtin_bit_cast(mx_f16x8, h);
     lo = __builtin_bit_cast(mx_f16x8, l);

@@ -47,3 +47,31 @@ def test_mx_infinite_suffix_values(fa, step, d, hkv, G, N):  # noqa: F811
     out, lse = run()
     assert np.array_equal(out, want, equal_nan=True), np.argwhere((out != want) & ~(np.isnan(out) & np.isnan(want)))[:8]
     assert np.array_equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_mx_small_weights_add_up(fa, d):  # noqa: F811
+    """One key that gets most of the weight and half a million small ones beside it, all values 1: the output is 1.  A wave sums half of them
+    in n / 64 steps of products, and a lane n / 64 numbers: roundings of either sign, each at most half a step of the sum (2^-24, a standard
+    deviation of 2^-23 / sqrt(12)), in all sqrt(n / 32) of that in a row; what loses a part of each small weight shows in the mean
+    over the rows, which is held to six deviations of its own."""
+    n, hkv, G, N = 1 << 19, 2, 16, 4
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(90 + d)
+    k = torch.zeros(hkv, n, d, dtype=torch.bfloat16, device="cuda")
+    k[..., 32:64].normal_(generator=gen)
+    k[:, 0, 32:64], k[:, 0, 0] = 0, 6
+    q = torch.zeros(N, hkv * G, d, dtype=torch.bfloat16, device="cuda")
+    q[..., 32:64].normal_(std=0.1, generator=gen)
+    q[..., 0] = 11 / 6  # the others have some 2^-16 of that key's weight each, 10 times as much together
+    tiles = torch.empty(n // 128, hkv, 136 * d, dtype=torch.uint8, device="cuda")
+    fa.mx_pack(k, torch.ones_like(k), tiles)
+    plan = fa.Plan.mx_plan(hkv * G, hkv, d, [0, N], [n], 1, 0, n_pool_tiles=n // 128, softmax_scale=1.0, blocks=1)
+    suffix = torch.zeros(N, hkv, 1, d, dtype=torch.bfloat16, device="cuda")
+    out, lse = torch.empty(N, hkv * G, d, device="cuda"), torch.empty(N, hkv * G, device="cuda")
+    plan.decode_mx(q, tiles, suffix, suffix, dev_i32([0] * N), out, lse)
+    err = out.cpu().numpy().astype(np.float64)[..., 0] - 1
+    dev = np.sqrt(n / 32) * 2.0 ** -23 / np.sqrt(12)
+    print(f"[small weights] mean {err.mean():.2e} of {6 * dev / np.sqrt(err.size):.2e}, worst {np.abs(err).max():.2e} of {6 * dev:.2e}", flush=True)
+    assert abs(err.mean()) <= 6 * dev / np.sqrt(err.size) and np.abs(err).max() <= 6 * dev
+    assert (out == out[..., :1]).all()
