@@ -75,3 +75,41 @@ def test_mx_small_weights_add_up(fa, d):  # noqa: F811
     print(f"[small weights] mean {err.mean():.2e} of {6 * dev / np.sqrt(err.size):.2e}, worst {np.abs(err).max():.2e} of {6 * dev:.2e}", flush=True)
     assert abs(err.mean()) <= 6 * dev / np.sqrt(err.size) and np.abs(err).max() <= 6 * dev
     assert (out == out[..., :1]).all()
+
+
+@pytest.mark.parametrize("where", ["prefix", "suffix", "wide prefix"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_mx_products_keep_all_of_p(fa, d, where):  # noqa: F811
+    """Three keys whose scores are exact in fp32 and close to each other, values 1 and -1: what is left is the error of p and of its terms.
+    A weight: its exponent, below 8, is off by 2^-22 (half a step) and by 2^-24 of at most 1 (the scale), times ln 2, the exponential by
+    2^-23; its terms by 2^-23 at most; then 16 fp32 steps of sums, reciprocals and joins.  A term of p less is off by 2^-18 of p
+    (suffixes, values outside fp16's range: three bf16 terms) or by 2^-12 (two fp16 terms), and fails."""
+    rng = np.random.default_rng(95)
+    hkv, G, N, n, scale = 8, 8, 8, 3, 2.0 ** -6
+    grid = lambda step, top, *s: np.clip(np.round(rng.standard_normal(s) / step) * step, -top, top)  # noqa: E731
+    # the values of a block come back as they are: 0, 0.5, .. 6 under one scale
+    size = 2.0 ** 40 if where == "wide prefix" else 1.0
+    v = np.where(rng.random((hkv, n, d)) < 0.5, -size, size)
+    q, k = grid(0.25, 2, N, hkv * G, d), grid(0.5, 2, hkv, n, d)
+    to_bits = lambda x: torch.from_numpy(np.asarray(x, np.float32)).bfloat16().cuda()  # noqa: E731
+    prefix = 0 if where == "suffix" else n
+    plan = fa.Plan.mx_plan(hkv * G, hkv, d, [0, N], [prefix], n, n, n_pool_tiles=1, softmax_scale=scale)
+    tiles = torch.zeros(1, hkv, 136 * d, dtype=torch.uint8, device="cuda")
+    sk, sv = torch.zeros(N, hkv, n, d, dtype=torch.bfloat16, device="cuda"), torch.zeros(N, hkv, n, d, dtype=torch.bfloat16, device="cuda")
+    if prefix:
+        fa.mx_pack(to_bits(k), to_bits(v), tiles)
+        back = [torch.empty(hkv, n, d, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+        fa.mx_unpack(tiles, *back)
+        assert torch.equal(back[0], to_bits(k)) and torch.equal(back[1], to_bits(v))
+    else:
+        sk[:], sv[:] = to_bits(k), to_bits(v)
+    out, lse = torch.empty(N, hkv * G, d, device="cuda"), torch.empty(N, hkv * G, device="cuda")
+    plan.decode_mx(to_bits(q), tiles, sk, sv, dev_i32([0 if prefix else n] * N), out, lse)
+    w = np.exp(scale * np.matmul(q.reshape(N, hkv, G, d), k.transpose(0, 2, 1)[None]))
+    total = w.sum(-1, keepdims=True)
+    ref = np.matmul(w / total, v[None]).reshape(N, hkv * G, d)
+    tol = ((2.0 ** -22 + 2.0 ** -24) * np.log(2) + 2.0 ** -23 + 2.0 ** -23 + 16 * 2.0 ** -24) * size
+    err = np.abs(out.cpu().numpy() - ref).max()
+    print(f"[terms of p] d {d} {where}: {err / size:.2e} of {tol / size:.2e}", flush=True)
+    assert err <= tol
+    assert np.abs(lse.cpu().numpy().reshape(N, hkv, G) - np.log(total)[..., 0]).max() <= 2.0 ** -19
