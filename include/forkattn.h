@@ -510,7 +510,8 @@ fka_status fka_plan_create_mx(const fka_heads *heads, const fka_mx_desc *desc, c
  * One decode step, as fka_fork_decode, over the values that the tiles stand for.
  *   tiles        the pool
  *   tile_table   int32 [n_groups][max_tiles_per_group] (device): the tile ids of each group's prefix; NULL: the groups'
- *                tiles lie one after the other in the pool, those of group 0 from id 0
+ *                tiles lie one after the other in the pool, those of group 0 from id 0 (FKA_ERR_INVALID_ARG if the pool has
+ *                fewer than that)
  *   others       as in fka_fork_decode, with the sequences of all groups
  * A tile id outside [0, n_pool_tiles) is not read: its keys count as zeros and flag 4 is raised.  A NaN block of V makes its
  * channel NaN in every row of the group, one of K the rows themselves.  An infinite value in a sequence's suffix makes its channel that

@@ -51,7 +51,7 @@ struct fka_plan {
     size_t workspace_bytes = 0;
     // decode over 4-bit tiles: the blocks' jobs and each output row's merge record, fixed by the plan
     bool mx = false;
-    int32_t max_tiles = 0, n_pool_tiles = 0;
+    int32_t max_tiles = 0, n_pool_tiles = 0, all_tiles = 0;  // (all_tiles: of all prefixes)
     std::vector<fka::MxJob> jobs;
     std::vector<int32_t> rowrec;
     int device = 0;
@@ -812,6 +812,7 @@ fka_status build_mx_jobs(fka_plan *p, int32_t blocks)
         }
         tile0 += tiles;
     }
+    p->all_tiles = tile0;
     // the longest first, so that short ones fill the end
     std::stable_sort(p->jobs.begin(), p->jobs.end(), [](const fka::MxJob &x, const fka::MxJob &y) { return x.end - x.begin > y.end - y.begin; });
     p->jobs.insert(p->jobs.end(), tail.begin(), tail.end());
@@ -829,6 +830,8 @@ fka_status check_mx_call(const fka_plan *p, const void *q, const void *tiles, co
     REQUIRE_PTR16(q);
     if (p->n_pool_tiles > 0) REQUIRE_PTR16(tiles);
     REQUIRE_OPT4(tile_table);
+    REQUIRE(tile_table != nullptr || p->all_tiles <= p->n_pool_tiles, "without a tile_table the prefixes need %d tiles, the plan's n_pool_tiles is %d",
+            p->all_tiles, p->n_pool_tiles);
     REQUIRE_PTR16(suffix_k);
     REQUIRE_PTR16(suffix_v);
     REQUIRE_PTR4(suffix_len);

@@ -51,7 +51,7 @@ def test_mx_infinite_suffix_values(fa, step, d, hkv, G, N):  # noqa: F811
 
 @pytest.mark.parametrize("d", [64, 128])
 def test_mx_small_weights_add_up(fa, d):  # noqa: F811
-    """One key that gets most of the weight and half a million small ones beside it, all values 1: the output is 1.  A wave sums half of them
+    """One key with 2^16 times the weight of any other and half a million of those beside it, all values 1: the output is 1.  A wave sums half of them
     in n / 64 steps of products, and a lane n / 64 numbers: roundings of either sign, each at most half a step of the sum (2^-24, a standard
     deviation of 2^-23 / sqrt(12)), in all sqrt(n / 32) of that in a row; what loses a part of each small weight shows in the mean
     over the rows, which is held to six deviations of its own."""
@@ -113,3 +113,25 @@ def test_mx_products_keep_all_of_p(fa, d, where):  # noqa: F811
     print(f"[terms of p] d {d} {where}: {err / size:.2e} of {tol / size:.2e}", flush=True)
     assert err <= tol
     assert np.abs(lse.cpu().numpy().reshape(N, hkv, G) - np.log(total)[..., 0]).max() <= 2.0 ** -19
+
+
+def test_mx_pool_without_room_for_the_prefixes(fa):  # noqa: F811
+    """Without a tile table the ids are known: a pool with fewer tiles is refused, by the decode and the step, and nothing runs; with a
+    table the same plan works."""
+    m = Mx(fa, 97, 8, 2, 64, [2, 1], [300, 129], [3, 4, 5])  # 3 + 2 tiles
+    kn = dev_bf16(normal(np.random.default_rng(98), 3, 2, 64))
+    for pool in (4, 0):
+        plan = fa.Plan.mx_plan(8, 2, 64, [0, 2, 3], [300, 129], m.cap, m.cap, n_pool_tiles=pool)
+        out, lse = m.outs()
+        with pytest.raises(fa.FkaError, match="need 5 tiles, the plan's n_pool_tiles is"):
+            plan.decode_mx(out=out, out_lse=lse, **m.dev)
+        with pytest.raises(fa.FkaError, match="need 5 tiles"):
+            plan.step_mx(m.dev["q"], kn, kn, m.tiles, m.dev["suffix_k"], m.dev["suffix_v"], m.dev["suffix_len"], out, lse)
+        torch.cuda.synchronize()
+        assert torch.isnan(out).all() and np.array_equal(m.dev["suffix_len"].cpu().numpy(), m.lens) and plan.device_error() == 0
+    plan = fa.Plan.mx_plan(8, 2, 64, [0, 2, 3], [300, 300], m.cap, m.cap, n_pool_tiles=5)  # two forks of one prefix
+    m.prefixes, m.pk[1], m.pv[1] = [300, 300], m.pk[0], m.pv[0]
+    out, lse = m.outs()
+    plan.decode_mx(out=out, out_lse=lse, tile_table=dev_i32([[0, 1, 2], [0, 1, 2]]), **m.dev)
+    m.check(out.cpu().numpy(), lse.cpu().numpy(), "a shared prefix")
+    assert plan.device_error() == 0
