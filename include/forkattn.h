@@ -439,7 +439,8 @@ typedef struct {
  *   suffix_k           bf16 [N][Hkv][suffix_cap][d], rows [suffix_len[b], suffix_len[b] + n) written (suffix_v likewise)
  *   suffix_len         int32 [N] (device), or NULL: rows from 0
  *   err                int32 (device) or NULL
- * What is written, the cache and (but for q itself) q_out, may not overlap what is read.
+ * What is written, q_out and the cache, may overlap neither each other nor what is read (FKA_ERR_INVALID_ARG), but that q_out may be q
+ * itself where q is dense.
  * A sequence without room (suffix_len[b] negative, or past max_len with the new tokens) keeps its cache and length
  * and bit 2 is or-ed into *err; its q_out is written.  Errors: FKA_ERR_INVALID_ARG, FKA_ERR_UNSUPPORTED (head_dim,
  * rotary_dim not a multiple of 16, too many tokens).

@@ -128,6 +128,36 @@ bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
         if ((p) && !aligned4(p)) return fail(FKA_ERR_INVALID_ARG, "%s is not 4-byte aligned", #p); \
     } while (0)
 
+// A caller's memory: `rows` rows of `bytes` bytes, `step` bytes apart (one row: a dense range).  Nothing where `at` is null.
+struct Span {
+    const void *at;
+    size_t bytes;
+    const char *name;
+    size_t rows = 1, step = 0;
+};
+
+// Whether the dense range w has a byte in common with a row of r.
+bool overlap(const Span &w, const Span &r)
+{
+    if (!w.at || !r.at || w.bytes == 0 || r.bytes == 0) return false;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(w.at), z = a + w.bytes, r0 = reinterpret_cast<uintptr_t>(r.at);
+    // the first row that ends behind a
+    const size_t i = a < r0 + r.bytes ? 0 : r.step == 0 ? r.rows : (a - r0 - r.bytes) / r.step + 1;
+    return i < r.rows && r0 + i * r.step < z;
+}
+
+// What a call's kernels write must not be what others of their blocks still read or write: each of `written` against those behind it and
+// against all of `read`.
+template <size_t W, size_t R>
+fka_status check_apart(const Span (&written)[W], const Span (&read)[R])
+{
+    for (size_t i = 0; i < W; ++i) {
+        for (size_t j = i + 1; j < W; ++j) REQUIRE(!overlap(written[i], written[j]), "%s overlaps %s", written[i].name, written[j].name);
+        for (size_t j = 0; j < R; ++j) REQUIRE(!overlap(written[i], read[j]), "%s overlaps %s", written[i].name, read[j].name);
+    }
+    return FKA_OK;
+}
+
 fka_status check_heads(const fka_heads *h)
 {
     REQUIRE(h != nullptr, "heads is null");
@@ -912,6 +942,29 @@ fka_status run_mx_copy(bool pack, int32_t n_kv_heads, int32_t head_dim, int32_t 
     hipError_t e = pack ? fka::launch_mx_pack(a, head_dim, s) : fka::launch_mx_unpack(a, head_dim, s);
     if (e != hipSuccess) return hip_fail(e, pack ? "pack kernel launch" : "unpack kernel launch");
     return ok();
+}
+
+// q_out and the cache (dst_rows rows per buffer) may overlap neither each other nor what is read, but that q_out may be q itself where q is dense.
+fka_status check_rotate_apart(const fka_rotate_desc *desc, const fka::RotateArgs &a, size_t dst_rows, const Span &table)
+{
+    const size_t tokens = (size_t)desc->n_seqs * desc->n_tokens, head = (size_t)desc->head_dim * 2;
+    const size_t qb = desc->n_q_heads * head, kb = desc->n_kv_heads * head;
+    const bool in_place = a.q_out == a.q && (desc->q_stride * 2 == (int64_t)qb || tokens == 1);
+    const Span written[] = {{a.q_out, tokens * qb, "q_out"}, {a.k_dst, dst_rows * head, "the K cache"}, {a.v_dst, dst_rows * head, "the V cache"}};
+    const Span read[] = {
+        {in_place ? nullptr : a.q, qb, "q", tokens, (size_t)desc->q_stride * 2},
+        {a.k, kb, "k", tokens, (size_t)desc->k_stride * 2},
+        {a.v, kb, "v", tokens, (size_t)desc->v_stride * 2},
+        {a.q_weight, head, "q_weight"},
+        {a.k_weight, head, "k_weight"},
+        {a.freq, (size_t)desc->rotary_dim / 2 * sizeof(double), "freq"},
+        {a.positions, desc->rotary_dim ? tokens * 4 : 0, "positions"},
+        {a.suffix_len, (size_t)desc->n_seqs * 4, "suffix_len"},
+        {a.seq_prefix_len, (size_t)desc->n_seqs * 4, "prefix_len"},
+        {a.err, 4, "err"},
+        table,
+    };
+    return check_apart(written, read);
 }
 
 // The checks and arguments that the contiguous and the paged store share.
@@ -1929,6 +1982,7 @@ fka_status fka_rotate_append(const fka_rotate_desc *desc, const void *q, const v
     if (st != FKA_OK) return st;
     REQUIRE(desc->max_len <= suffix_cap, "max_len (%d) must be at most suffix_cap (%d)", desc->max_len, suffix_cap);
     a.suffix_cap = suffix_cap;
+    if ((st = check_rotate_apart(desc, a, (size_t)desc->n_seqs * desc->n_kv_heads * suffix_cap, {nullptr, 0, ""})) != FKA_OK) return st;
     hipError_t e = fka::launch_rotate(a, desc->head_dim, desc->interleaved != 0, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "rotate kernel launch");
     return ok();
@@ -1950,6 +2004,9 @@ fka_status fka_rotate_append_paged(const fka_rotate_desc *desc, const void *q, c
     a.seq_prefix_len = prefix_len;
     a.max_pages = max_pages_per_seq;
     a.n_pool_pages = n_pool_pages;
+    if ((st = check_rotate_apart(desc, a, (size_t)n_pool_pages * desc->n_kv_heads * fka::kPageSize,
+                                 {page_table, (size_t)desc->n_seqs * max_pages_per_seq * 4, "page_table"})) != FKA_OK)
+        return st;
     hipError_t e = fka::launch_rotate(a, desc->head_dim, desc->interleaved != 0, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "rotate kernel launch");
     return ok();
@@ -2142,27 +2199,12 @@ fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t 
     REQUIRE_PTR16(workspace);
     const size_t need = fka_evict_bytes(n_kv_heads, len);
     REQUIRE(workspace_bytes >= need, "workspace of %zu bytes, %zu are needed", workspace_bytes, need);
-    // what the kernels write must not be what others of their blocks still read
-    const struct {
-        const void *at;
-        size_t bytes;
-        const char *name;
-    } all[] = {
-        {k, (((size_t)n_kv_heads - 1) * kv_cap + len) * head_dim * 2, "k"},
-        {v, (((size_t)n_kv_heads - 1) * kv_cap + len) * head_dim * 2, "v"},
-        {weights, (((size_t)n_kv_heads - 1) * weights_cap + len) * 4, "weights"},
-        {index, (size_t)n_kv_heads * keep * 4, "index"},
-        {k_out, (size_t)n_kv_heads * keep * head_dim * 2, "k_out"},
-        {v_out, (size_t)n_kv_heads * keep * head_dim * 2, "v_out"},
-        {weights_out, weights_out ? (size_t)n_kv_heads * keep * 4 : 0, "weights_out"},
-        {workspace, need, "workspace"},
-    };
-    for (int i = 3; i < 8; ++i)
-        for (int j = 0; j < i; ++j) {
-            const uintptr_t x = reinterpret_cast<uintptr_t>(all[i].at), y = reinterpret_cast<uintptr_t>(all[j].at);
-            REQUIRE(all[i].bytes == 0 || all[j].bytes == 0 || x >= y + all[j].bytes || y >= x + all[i].bytes, "%s overlaps %s",
-                    all[i].name, all[j].name);
-        }
+    const size_t in = ((size_t)n_kv_heads - 1) * kv_cap + len, kept = (size_t)n_kv_heads * keep;
+    const Span written[] = {{workspace, need, "workspace"}, {weights_out, kept * 4, "weights_out"}, {v_out, kept * head_dim * 2, "v_out"},
+                            {k_out, kept * head_dim * 2, "k_out"}, {index, kept * 4, "index"}};
+    const Span read[] = {{k, in * head_dim * 2, "k"}, {v, in * head_dim * 2, "v"}, {weights, (((size_t)n_kv_heads - 1) * weights_cap + len) * 4, "weights"}};
+    const fka_status st = check_apart(written, read);
+    if (st != FKA_OK) return st;
     fka::EvictArgs a{};
     a.k = static_cast<const uint16_t *>(k);
     a.v = static_cast<const uint16_t *>(v);

@@ -189,3 +189,46 @@ def test_binding_checks_tensors(fa):
                  workspace=None)
     with pytest.raises(ValueError, match="group_prefix_len"):
         fa.Plan.mx_plan(8, 2, 64, [0, 5], [1, 2], 64, 64, n_pool_tiles=1)
+
+
+def _rotate_at(fa, paged, at, sizes):
+    """A rotate call with every buffer at an address of its own; nothing is launched where it is refused."""
+    n, cap, pages = sizes
+    desc = fa.RotateDesc(3, n, 4, 2, 64, 64, 0, cap, 0, 1e-6, 768, 768, 768)
+    p = {x: C.c_void_p(y) for x, y in at.items()}
+    head = [C.byref(desc), p["q"], p["k"], p["v"], p["q_weight"], p["k_weight"], p["freq"], p["positions"], p["q_out"], p["the K cache"],
+            p["the V cache"]]
+    if paged:
+        return fa.raw_call("fka_rotate_append_paged", *head, p["page_table"], p["prefix_len"], 4, pages, p["suffix_len"], p["err"], None)
+    return fa.raw_call("fka_rotate_append", *head, cap, p["suffix_len"], p["err"], None)
+
+
+@pytest.mark.parametrize("name", ["q_out", "the K cache", "the V cache"])
+@pytest.mark.parametrize("paged", [False, True])
+def test_rotate_rejects_overlaps(fa, paged, name):
+    """Each of what it writes against each other buffer, by a few bytes at either end; q, k and v by their rows, the last one too."""
+    n, cap, pages = 5, 16, 7
+    tokens, row = 3 * n, 768 * 2
+    cache = (pages * 16 if paged else 3 * cap) * 2 * 64 * 2
+    size = {"q": 4 * 128, "k": 2 * 128, "v": 2 * 128, "q_weight": 128, "k_weight": 128, "freq": 256, "positions": tokens * 4,
+            "suffix_len": 12, "err": 4, "q_out": tokens * 4 * 128, "the K cache": cache, "the V cache": cache}
+    if paged:
+        size.update(page_table=3 * 4 * 4, prefix_len=12)
+    for other in size:
+        if other == name:
+            continue
+        for r in (0, 1, tokens - 1) if other in "qkv" else (0,):
+            for shift in (16 - size[name], (size[other] - 1) // 16 * 16, 0):
+                at = {x: (1 << 30) + (i << 24) for i, x in enumerate(size)}
+                at[name] = at[other] + r * row + shift
+                assert _rotate_at(fa, paged, at, (n, cap, pages)) == -1, (other, r, shift)
+                # (a row's neighbours may be met first)
+                assert f"{name} overlaps {other}" in fa.last_error() or f"{other} overlaps {name}" in fa.last_error(), fa.last_error()
+
+
+def test_rotate_q_out_is_q_or_apart(fa):
+    """q_out at q's own address is refused where q's rows have gaps, in which q_out's rows would lie."""
+    size = ["q", "k", "v", "q_weight", "k_weight", "freq", "positions", "suffix_len", "err", "q_out", "the K cache", "the V cache"]
+    at = {x: (1 << 30) + (i << 24) for i, x in enumerate(size)}
+    at["q_out"] = at["q"]
+    assert _rotate_at(fa, False, at, (1, 16, 0)) == -1 and "q_out overlaps q" in fa.last_error()

@@ -135,3 +135,35 @@ def test_mx_pool_without_room_for_the_prefixes(fa):  # noqa: F811
     plan.decode_mx(out=out, out_lse=lse, tile_table=dev_i32([[0, 1, 2], [0, 1, 2]]), **m.dev)
     m.check(out.cpu().numpy(), lse.cpu().numpy(), "a shared prefix")
     assert plan.device_error() == 0
+
+
+def test_rotate_buffers_side_by_side(fa):  # noqa: F811
+    """Buffers that touch, q_out in a gap between two tokens' rows, and q_out at a dense q are not overlaps: the results are those of
+    buffers apart."""
+    rng = np.random.default_rng(99)
+    n, hq, hkv, d = 2, 4, 2, 64
+    width, qn, kn = (hq + 2 * hkv) * d, n * hq * d, hkv * n * d
+    step = width + qn + 2 * kn
+    rows = normal(rng, n, width)
+    arena = torch.zeros(2 * step, dtype=torch.bfloat16, device="cuda")
+    tok = arena[: n * step].view(1, n, step)
+    tok[..., :width] = dev_bf16(rows)
+    part = lambda t, a, b: t[..., a * d: b * d].unflatten(-1, (-1, d))  # noqa: E731
+    pos, freq = dev_i32([[5, 6]]), torch.full((32,), 0.7, dtype=torch.float64, device="cuda")
+
+    def run(t, q_out, kc, vc):
+        fa.rotate_append(part(t, 0, hq), part(t, hq, hq + hkv), part(t, hq + hkv, hq + 2 * hkv), pos, freq, q_out, kc, vc)
+        return [host(x) for x in (q_out, kc, vc)]
+
+    apart = [torch.empty(1, n, hq, d, dtype=torch.bfloat16, device="cuda")] + [
+        torch.empty(1, hkv, n, d, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    want = run(dev_bf16(rows).view(1, n, width), *apart)
+    gap = arena[width: step]  # between the first token's row and the second's
+    got = run(tok, gap[:qn].view(1, n, hq, d), gap[qn: qn + kn].view(1, hkv, n, d), gap[qn + kn:].view(1, hkv, n, d))
+    for a, b in zip(got, want):
+        assert np.array_equal(a, b)
+    assert np.array_equal(host(tok[0, :, :width]), rows), "what was read is as it was"
+    q = dev_bf16(rows)[None, :, : hq * d].contiguous().view(1, n, hq, d)
+    t = dev_bf16(rows).view(1, n, width)
+    fa.rotate_append(q, part(t, hq, hq + hkv), part(t, hq + hkv, hq + 2 * hkv), pos, freq, q, *apart[1:])
+    assert np.array_equal(host(q), want[0])
