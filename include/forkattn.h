@@ -483,7 +483,8 @@ size_t fka_mx_tile_bytes(int32_t n_kv_heads, int32_t head_dim);
 fka_status fka_mx_pack(int32_t n_kv_heads, int32_t head_dim, int32_t from, int32_t len, const void *k_src, const void *v_src,
                        int32_t src_cap, void *tiles, const int32_t *tile_row, int32_t n_pool_tiles, int32_t *err, void *stream);
 
-/* The values of positions [from, len) (any from) back as bf16, exactly; an id outside the pool gives zeros and bit 4. */
+/* The values of positions [from, len) (any from) back as bf16, exactly; an id outside the pool gives zeros and bit 4.  Here and in the
+ * pack, what is written may not overlap what is read, nor k_dst v_dst (FKA_ERR_INVALID_ARG). */
 fka_status fka_mx_unpack(int32_t n_kv_heads, int32_t head_dim, int32_t from, int32_t len, const void *tiles,
                          const int32_t *tile_row, int32_t n_pool_tiles, void *k_dst, void *v_dst, int32_t dst_cap, int32_t *err,
                          void *stream);
@@ -539,7 +540,7 @@ fka_status fka_fork_step_mx(const fka_plan *plan, const void *q, const void *k_n
  *   q        bf16 [n_rows][Hq][d];  lse fp32 [n_rows][Hq]
  *   k        bf16 [Hkv][k_cap][d], the first len rows read
  *   weights  fp32 [Hkv][weights_cap], the first len entries updated
- * The sums' order is fixed: the same call gives the same bits.
+ * weights may not overlap what is read (FKA_ERR_INVALID_ARG).  The sums' order is fixed: the same call gives the same bits.
  */
 fka_status fka_key_weights(const fka_heads *heads, int32_t n_rows, int32_t len, const void *q, const float *lse, const void *k,
                            int32_t k_cap, float *weights, int32_t weights_cap, float decay, void *stream);

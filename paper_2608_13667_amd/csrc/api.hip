@@ -922,6 +922,11 @@ fka_status run_mx_copy(bool pack, int32_t n_kv_heads, int32_t head_dim, int32_t 
     REQUIRE_PTR16(tiles);
     REQUIRE_OPT4(tile_row);
     REQUIRE_OPT4(err);
+    const size_t side = (((size_t)n_kv_heads - 1) * cap + (len - from)) * head_dim * 2;
+    const Span ks{k, side, "k"}, vs{v, side, "v"}, pool{tiles, (size_t)n_pool_tiles * fka_mx_tile_bytes(n_kv_heads, head_dim), "tiles"},
+        ids{tile_row, (size_t)ceil_div(len, fka::kMxTile) * 4, "tile_row"}, flag{err, 4, "err"};
+    const fka_status st = pack ? check_apart({pool}, {ks, vs, ids, flag}) : check_apart({ks, vs}, {pool, ids, flag});
+    if (st != FKA_OK) return st;
     fka::MxCopyArgs a{};
     if (pack) {
         a.k_src = static_cast<const uint16_t *>(k);
@@ -2149,6 +2154,10 @@ fka_status fka_key_weights(const fka_heads *heads, int32_t n_rows, int32_t len, 
     }
     REQUIRE_PTR16(k);
     REQUIRE_PTR4(weights);
+    const size_t d = heads->head_dim, rows = (size_t)n_rows * heads->n_q_heads, sides = (size_t)heads->n_kv_heads - 1;
+    st = check_apart({{weights, (sides * weights_cap + len) * 4, "weights"}},
+                     {{q, rows * d * 2, "q"}, {lse, rows * 4, "lse"}, {k, (sides * k_cap + len) * d * 2, "k"}});
+    if (st != FKA_OK) return st;
     fka::WeightsArgs a{};
     a.q = static_cast<const uint16_t *>(q);
     a.lse = lse;

@@ -232,3 +232,38 @@ def test_rotate_q_out_is_q_or_apart(fa):
     at = {x: (1 << 30) + (i << 24) for i, x in enumerate(size)}
     at["q_out"] = at["q"]
     assert _rotate_at(fa, False, at, (1, 16, 0)) == -1 and "q_out overlaps q" in fa.last_error()
+
+
+def _places(size):
+    return {x: (1 << 30) + (i << 24) for i, x in enumerate(size)}
+
+
+def _each_overlap(size, names):
+    """Addresses with one of `names` upon another buffer, by a few bytes at either end."""
+    for name in names:
+        for other in size:
+            for shift in (16 - (size[name] + 15) // 16 * 16, (size[other] - 1) // 16 * 16, 0):
+                if other != name:
+                    at = _places(size)
+                    at[name] = at[other] + shift
+                    yield name, other, {x: C.c_void_p(y) for x, y in at.items()}
+
+
+def test_mx_copies_reject_overlaps(fa):
+    hkv, d, n, cap, pool = 2, 64, 200, 230, 3
+    side = (cap + n) * d * 2
+    size = dict(k=side, v=side, tiles=pool * hkv * 136 * d, tile_row=8, err=4)
+    for name, other, p in _each_overlap(size, ["tiles"]):
+        st = fa.raw_call("fka_mx_pack", hkv, d, 0, n, p["k"], p["v"], cap, p["tiles"], p["tile_row"], pool, p["err"], None)
+        assert st == -1 and f"{name} overlaps {other}" in fa.last_error(), (name, other)
+    for name, other, p in _each_overlap(size, ["k", "v"]):
+        st = fa.raw_call("fka_mx_unpack", hkv, d, 0, n, p["tiles"], p["tile_row"], pool, p["k"], p["v"], cap, p["err"], None)
+        assert st == -1 and "overlaps" in fa.last_error() and {name, other} == set(fa.last_error().split(" overlaps ")), (name, other)
+
+
+def test_key_weights_reject_overlaps(fa):
+    h, rows, n, kcap, wcap = fa.Heads(8, 2, 64, 0.0), 5, 100, 130, 120
+    size = dict(weights=(wcap + n) * 4, q=rows * 8 * 64 * 2, lse=rows * 8 * 4, k=(kcap + n) * 64 * 2)
+    for name, other, p in _each_overlap(size, ["weights"]):
+        st = fa.raw_call("fka_key_weights", C.byref(h), rows, n, p["q"], p["lse"], p["k"], kcap, p["weights"], wcap, 0.5, None)
+        assert st == -1 and f"weights overlaps {other}" in fa.last_error(), (other, fa.last_error())
