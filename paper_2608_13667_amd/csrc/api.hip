@@ -2180,7 +2180,7 @@ fka_status fka_key_weights(const fka_heads *heads, int32_t n_rows, int32_t len, 
 
 size_t fka_evict_bytes(int32_t n_kv_heads, int32_t len)
 {
-    if (n_kv_heads < 1 || len < 0) return 0;
+    if (n_kv_heads < 1 || n_kv_heads > 65535 || len < 0 || len > kMaxTokens) return 0;  // as fka_evict
     const size_t chunks = std::min(ceil_div(len, fka::kEvictGroup), fka::kEvictChunks);
     return (size_t)n_kv_heads * (chunks * (3 * fka::kEvictBins * sizeof(uint32_t) + 2 * sizeof(int32_t)) + 4 * sizeof(int32_t));
 }

@@ -267,3 +267,9 @@ def test_key_weights_reject_overlaps(fa):
     for name, other, p in _each_overlap(size, ["weights"]):
         st = fa.raw_call("fka_key_weights", C.byref(h), rows, n, p["q"], p["lse"], p["k"], kcap, p["weights"], wcap, 0.5, None)
         assert st == -1 and f"weights overlaps {other}" in fa.last_error(), (other, fa.last_error())
+
+
+@pytest.mark.parametrize("hkv,length", [(65535, 100), (2, 2**30), (65536, 100), (2**31 - 1, 100), (2, 2**30 + 1), (2, 2**31 - 1), (0, 9), (2, -1)])
+def test_evict_bytes_are_zero_where_evict_refuses(fa, hkv, length):
+    st = fa.raw_call("fka_evict", hkv, 64, length, 0, 0, 0, None, None, length, None, length, None, None, None, None, None, 0, None)
+    assert (st == 0) == (fa._lib.fka_evict_bytes(hkv, length) > 0), (st, fa.last_error())
