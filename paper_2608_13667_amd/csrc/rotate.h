@@ -123,10 +123,23 @@ __global__ void rotate_kernel(RotateArgs a)
             rot_f32x8 y1 = rot_widen(x1), y2 = rot_widen(x2);
             const uint16_t *w = is_q ? a.q_weight : a.k_weight;
             if (w) {
-                float ss = 0.f;
+                auto mean = [&](float eps) {
+                    float ss = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(y1[i], y1[i], __builtin_fmaf(y2[i], y2[i], ss));
-                const float inv = 1.f / sqrtf(rot_sum<LPH>(ss) * (1.f / HD) + a.eps);
+                    for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(y1[i], y1[i], __builtin_fmaf(y2[i], y2[i], ss));
+                    return rot_sum<LPH>(ss) * (1.f / HD) + eps;
+                };
+                float ms = mean(a.eps);
+                // a head whose squares leave fp32's range (values past 2^50, or eps next to nothing and values below 2^-50) is
+                // normed times 2^-100 or 2^100: exact, and gone again in the quotient
+                const bool far = !(ms > 0x1p-100f && ms < 0x1p100f);
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
+                    const float s = !far ? 1.f : ms <= 0x1p-100f ? 0x1p100f : 0x1p-100f;
+                    y1 *= s;
+                    y2 *= s;
+                    ms = mean(a.eps * s * s);
+                }
+                const float inv = 1.f / sqrtf(ms);
                 y1 *= rot_widen(*reinterpret_cast<const uint4 *>(w + c1)) * inv;
                 y2 *= rot_widen(*reinterpret_cast<const uint4 *>(w + c2)) * inv;
             }

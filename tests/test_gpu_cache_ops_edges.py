@@ -5,7 +5,8 @@ import pytest
 import torch
 
 from tests.gpu_util import dev_bf16, dev_i32
-from tests.test_gpu_cache_ops import Mx, fa, host, normal, value  # noqa: F401  (fa is the fixture)
+from tests.test_gpu_cache_ops import (Mx, bits_of, close_rotated, fa, host, normal, ref_rotate,  # noqa: F401  (fa is the fixture)
+                                      value)
 
 pytestmark = pytest.mark.gpu
 
@@ -167,3 +168,27 @@ def test_rotate_buffers_side_by_side(fa):  # noqa: F811
     t = dev_bf16(rows).view(1, n, width)
     fa.rotate_append(q, part(t, hq, hq + hkv), part(t, hq + hkv, hq + 2 * hkv), pos, freq, q, *apart[1:])
     assert np.array_equal(host(q), want[0])
+
+
+@pytest.mark.parametrize("d,inter,tokens", [(64, False, 12), (128, True, 12), (128, False, 2052)])
+@pytest.mark.parametrize("eps", [0.0, 1e-6, 1e-35])
+def test_rotate_norms_heads_of_every_magnitude(fa, eps, d, inter, tokens):  # noqa: F811
+    """Heads from bf16's smallest numbers to its largest, beside ordinary ones in the same wave, are normed as the formula says, though
+    their squares leave fp32's range."""
+    rng = np.random.default_rng(101)
+    hq, hkv = 11, 3
+    exps = np.array([0, 127, 64, -64, -133, 100, -40, 0, -120, 63, -70])
+    x = rng.uniform(0.5, 1, (1, tokens, hq, d)) * rng.choice([-1, 1], (1, tokens, hq, d)) * 2.0 ** exps[None, None, :, None]
+    rows = bits_of(np.concatenate([x, x[:, :, 1:4], x[:, :, 4:7]], 2))
+    rows[0, 0, 0, 1:] = 0  # one channel only
+    w = bits_of(1 + 0.3 * rng.standard_normal(d))
+    freq, pos = 1e4 ** (-np.arange(0, d, 2) / d), np.arange(tokens)[None]
+    t = dev_bf16(rows)
+    q_out = torch.empty(1, tokens, hq, d, dtype=torch.bfloat16, device="cuda")
+    kc, vc = (torch.empty(1, hkv, tokens, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    fa.rotate_append(t[:, :, :hq], t[:, :, hq: hq + hkv], t[:, :, hq + hkv:], dev_i32(pos), torch.from_numpy(freq).cuda(), q_out, kc, vc,
+                     q_weight=dev_bf16(w), k_weight=dev_bf16(w), eps=eps, interleaved=inter)
+    e32 = float(np.float32(eps))
+    for got, a, b in ((host(q_out), 0, hq), (host(kc).transpose(0, 2, 1, 3), hq, hq + hkv)):
+        close_rotated(got, ref_rotate(value(rows[:, :, a:b]), value(w), pos.astype(float), freq, d, inter, e32), (eps, a))
+    assert np.array_equal(host(vc).transpose(0, 2, 1, 3), rows[:, :, hq + hkv:])
