@@ -5,8 +5,8 @@ import pytest
 import torch
 
 from tests.gpu_util import dev_bf16, dev_i32
-from tests.test_gpu_cache_ops import (Mx, bits_of, close_rotated, fa, host, normal, ref_rotate,  # noqa: F401  (fa is the fixture)
-                                      value)
+from tests.test_gpu_cache_ops import (Mx, bits_of, close_rotated, fa, host, normal, ref_evict,  # noqa: F401  (fa is the fixture)
+                                      ref_rotate, value)
 
 pytestmark = pytest.mark.gpu
 
@@ -192,3 +192,42 @@ def test_rotate_norms_heads_of_every_magnitude(fa, eps, d, inter, tokens):  # no
     for got, a, b in ((host(q_out), 0, hq), (host(kc).transpose(0, 2, 1, 3), hq, hq + hkv)):
         close_rotated(got, ref_rotate(value(rows[:, :, a:b]), value(w), pos.astype(float), freq, d, inter, e32), (eps, a))
     assert np.array_equal(host(vc).transpose(0, 2, 1, 3), rows[:, :, hq + hkv:])
+
+
+def test_copies_past_4_gib(fa):  # noqa: F811
+    """Pack, unpack and evict where the last head's rows, and a tile's id, lie past 32 bits of bytes: as from small buffers."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GiB")
+    rng = np.random.default_rng(110)
+    hkv, d, n, cap, pool = 8, 128, 20000, 2_400_000, 32000
+    assert (hkv - 1) * cap * d * 2 > 1 << 32 and (pool - 1) * hkv * 136 * d > 1 << 32
+    small = [dev_bf16(normal(rng, hkv, n, d)) for _ in "kv"]
+    big = [torch.empty(hkv, cap, d, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    for b, s in zip(big, small):
+        b[:, :n] = s
+    # evict
+    w = rng.random((hkv, n)).astype(np.float32)
+    keep, weights = 700, torch.from_numpy(w).cuda()
+    index = torch.empty(hkv, keep, dtype=torch.int32, device="cuda")
+    ko, vo = (torch.empty(hkv, keep, d, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    fa.evict(*big, weights, index, ko, vo, n_first=3, n_last=5, length=n, workspace=fa.evict_workspace(hkv, n))
+    want = ref_evict(w, keep, 3, 5)
+    assert np.array_equal(index.cpu().numpy(), want)
+    for got, s in zip((ko, vo), small):
+        assert np.array_equal(host(got), host(s)[np.arange(hkv)[:, None], want])
+    # pack and unpack
+    m = 300
+    row = [pool - 1, 7, pool - 2]
+    tiles = torch.empty(pool, hkv, 136 * d, dtype=torch.uint8, device="cuda")
+    fa.mx_pack(*big, tiles, tile_row=dev_i32(row), length=m)
+    near = torch.empty(3, hkv, 136 * d, dtype=torch.uint8, device="cuda")
+    fa.mx_pack(*[s[:, :m].contiguous() for s in small], near)
+    for i, r in enumerate(row):
+        assert torch.equal(tiles[r], near[i])
+    back = [torch.empty(hkv, m, d, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    fa.mx_unpack(near, *back)
+    for b in big:
+        b[:, : m + 1] = 7.0
+    fa.mx_unpack(tiles, *big, tile_row=dev_i32(row), length=m)
+    for b, s in zip(big, back):
+        assert torch.equal(b[:, :m], s) and (b[:, m] == 7.0).all()
