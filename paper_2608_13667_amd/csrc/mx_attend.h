@@ -523,7 +523,8 @@ __global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
             fold = __builtin_fmaf(acc[0][e][0], acc[0][e][1], fold);
             fold = __builtin_fmaf(acc[0][e][2], acc[0][e][3], fold);
         }
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(__builtin_fabsf(fold) < INFINITY)) != 0, 0)) {
+        // (a row with a NaN sum is NaN whatever its values are)
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(l_run[0] < INFINITY && !(__builtin_fabsf(fold) < INFINITY)) != 0, 0)) {
             // lane l looks at channels CL l .. of this wave's keys; bits 3 i of `seen`: channel CL l + i has +inf, -inf, a NaN
             constexpr int CL = HD / 64;
             const uint16_t *v = reinterpret_cast<const uint16_t *>(reinterpret_cast<const char *>(a.suffix_v) + base);
