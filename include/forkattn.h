@@ -517,7 +517,8 @@ fka_status fka_plan_create_mx(const fka_heads *heads, const fka_mx_desc *desc, c
  *   others       as in fka_fork_decode, with the sequences of all groups
  * A tile id outside [0, n_pool_tiles) is not read: its keys count as zeros and flag 4 is raised.  A NaN block of V makes its
  * channel NaN in every row of the group, one of K the rows themselves.  An infinite value in a sequence's suffix makes its channel that
- * infinity in the sequence's rows (of both signs, or beside a NaN: NaN).  A group's prefix_len is that of its pack (a tile's unused
+ * infinity in the sequence's rows (of both signs, or beside a NaN: NaN).  The sums are kept in fp32 under weights of up to 2^15, so finite
+ * values past 2^80 may come out infinite.  A group's prefix_len is that of its pack (a tile's unused
  * tokens have to be the zeros that the pack wrote).
  */
 fka_status fka_fork_decode_mx(const fka_plan *plan, const void *q, const void *tiles, const int32_t *tile_table,

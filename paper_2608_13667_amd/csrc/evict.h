@@ -20,7 +20,10 @@ namespace fka {
 // Both kernels hold 64 keys per wave as the products' A operands (keys on M), so a lane sums its rows' weights of 16 keys over all
 // row tiles, and the 16 lanes of a key are summed once at the end; query rows (N) are read from LDS, for all waves of a block.
 constexpr int kWeightsKeys = 64;   // keys of a wave
-constexpr int kWeightsFew = 32;    // query rows of a KV head that the few-rows kernel holds in LDS
+// Query rows of a KV head that the few-rows kernel holds in LDS.  8 heads of 128, 128k keys: 32 rows 44.0 us and 50.7 by the kernel for many,
+// 32k keys 14.4 and 15.8; 8192 keys of 2 heads 5.7 and 5.7.  With room for 48 rows (another block's LDS still fits), 40 rows over 128k
+// keys 45.2 us and 50.6, 32k 15.5 and 15.7, 8192 of 2 heads 6.5 and 5.6: not taken so far.
+constexpr int kWeightsFew = 32;
 
 // 1 / log of the exponentials' base in the rows' -lse; -inf: a row past the end or without keys, weight 0.
 __device__ inline float weights_offset(float lse) { return lse != -INFINITY ? -lse * 1.44269504088896341f : -INFINITY; }

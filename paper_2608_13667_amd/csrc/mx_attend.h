@@ -18,8 +18,8 @@
 // range, [2^-23, 2^8], takes bf16 and three terms instead, as do the suffixes, whose values are bf16.  The
 // running maximum is a reference only: it moves when a score passes it by 2^8.
 //
-// Up to 16 rows bound by the tiles' bytes (128k keys of 8 heads of 128, 143 MB, with the merge 31 us), past them by the vector
-// instructions and the products: 20 rows 39 us, 40 rows 58.  In a 32k step of 25 rows 18.3 us, the bf16 kernel 29.
+// Up to 16 rows bound by the tiles' bytes (128k keys of 8 heads of 128, 143 MB: 5 rows 26.1 us and 4.5 of the merge), past them by the
+// vector instructions and the products: 20 rows 31.6 us, 40 rows 49.1.  In a 32k step of 25 rows 18.3 us, the bf16 kernel 29.
 #pragma once
 
 #include <type_traits>
@@ -294,7 +294,8 @@ __global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
         for (; tile < job.end; tile += NG) {
             const int valid = job.prefix_len - tile * kMxTile;
             const __amdgpu_buffer_rsrc_t next = tile_rsrc(tile + NG);
-            // V scales 2^-23 .. 2^8, as bytes 104 .. 135: exact in fp16 (a byte below 104 borrows, and shows so itself)
+            // V scales 2^-23 .. 2^8, as bytes 104 .. 135: exact in fp16 (a byte below 104 borrows, and shows so itself).  A block of
+            // zeros has byte 2 and counts as outside, though its scale does not matter: see the loop behind
             uint32_t odd = (vs[0] - 0x68686868u) & 0xe0e0e0e0u;
             if constexpr (HD == 128) odd |= (vs[1] - 0x68686868u) & 0xe0e0e0e0u;
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0) != 0, 0)) break;  // the loop behind takes the rest
@@ -391,8 +392,10 @@ __global__ __launch_bounds__(256, 2) void mx_partials_kernel(MxArgs a)
             }
             load_v(next);  // its time: the next tile's scores and first softmax
         }
-        // the same with V in bf16 and three terms of p, from the first tile with another scale on: 32 keys at
-        // a time straight from memory, since such values are not what a cache is made of
+        // the same with V in bf16 and three terms of p, from the first tile with another scale on: 32 keys at a time straight from
+        // memory.  What comes here, with the rest of its wave's tiles: a block whose largest value is past 7 2^8 or at most 7 2^-24;
+        // a prefix's last tile of at most 96 tokens (25 rows over 32668 keys 19.6 us, 32767 or 32768 17.9); and a V channel of
+        // zeros (25 rows over 32k keys 27.0 us, 40 rows over 128k 148 against 69)
         for (; tile < job.end; tile += NG) {
             const int valid = job.prefix_len - tile * kMxTile;
             const __amdgpu_buffer_rsrc_t rt = tile_rsrc(tile);

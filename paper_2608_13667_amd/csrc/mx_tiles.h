@@ -7,8 +7,8 @@
 //   2^E = the power of two at or below amax, over 4; twice that where amax > 7 2^E (6 2^E would cut it by more
 //   than an eighth; measured on normal values 19.0 dB signal to noise, 18.8 without),  -125 <= E <= 125,
 // and each value is x / 2^E rounded to the nearest code, ties to the even one, at most 6.  The limits of E keep
-// every value an ordinary bf16 number (0.5 2^-125 is the smallest normal one), so a tile unpacks exactly.  A
-// block with an infinity or a NaN becomes all NaN (scale byte 255).
+// every value an ordinary bf16 number (0.5 2^-125 is the smallest normal one), so a tile unpacks exactly; a block of
+// zeros has the lowest one.  A block with an infinity or a NaN becomes all NaN (scale byte 255).
 //
 // A tile holds 128 tokens of one KV head, 136 d bytes: K codes, V codes (64 d each), K scales, V scales
 // (4 d each), in the order in which the attention kernel's lanes read them (mx_attend.h).  With token
