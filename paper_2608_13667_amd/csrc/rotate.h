@@ -13,7 +13,7 @@
 // 1024 / d heads at a time (a unit).
 //
 // Bound by the bytes for many tokens: 32768 of 40 + 8 + 8 heads of 128 (0.94 GB read and written) 187 us, 5.0 TB/s, the
-// rate of a large copy; by latency for few, five tokens 4.3 us.
+// rate of a large copy; by latency for few, five tokens 4.5 us.
 #pragma once
 
 #include "internal.h"
