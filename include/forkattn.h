@@ -403,6 +403,87 @@ fka_status fka_prefill_paged(const fka_plan *plan, const void *q, const void *k_
                              const int32_t *page_table, const int32_t *suffix_len, float *out, float *out_lse,
                              void *stream);
 
+/* ---------------------------------------------------------------------- drafted trees */
+
+/*
+ * A decode step that checks n drafted tokens of every branch reads the shared prefix once for all of them instead of n times.  Each
+ * branch has a tree of n nodes: node 0, the root, is the token that was chosen last and is not in the cache yet, the others are
+ * drafted continuations, each with a parent before it.  A step is
+ *   fka_tree_layout    which nodes each node reads, and their positions
+ *   fka_rotate_append  (for each layer) the nodes' K and V at suffix positions [suffix_len[b], suffix_len[b] + n), advance = 0
+ *   fka_tree_attend    (for each layer) every node over the prefix, its branch's suffix and the nodes that it reads
+ *   fka_sample         the token that the model chooses behind each node
+ *   fka_tree_accept    (for each layer) the nodes that these tokens confirm stay in the cache
+ */
+
+/*
+ * parents int32 [N][n] (device): parents[b][0] is -1; node i > 0 has its parent in [0, i), or -1 where it is not used (a tree with
+ * fewer than n nodes).  Any other value counts as -1 and bit 16 is or-ed into *err (device int32, nullable).
+ *   masks      uint64 [N][n]: bit j of masks[b][i] is set where node i reads node j: itself and what is above it
+ *   base       int32 [N]: the root's position
+ *   positions  int32 [N][n]: base[b] + the nodes above node i
+ * masks and positions may overlap neither each other nor what is read (FKA_ERR_INVALID_ARG).  FKA_ERR_UNSUPPORTED for more than 64 nodes
+ * or 2^20 trees.
+ */
+fka_status fka_tree_layout(int32_t n_branches, int32_t n_nodes, const int32_t *parents, const int32_t *base, uint64_t *masks,
+                           int32_t *positions, int32_t *err, void *stream);
+
+/* Build a plan for the attention of trees of desc->n_tokens <= 64 nodes, with sizes, limits and errors as in
+ * fka_plan_create_prefill[_paged] (N x n at most 512; more than 64 nodes: FKA_ERR_UNSUPPORTED).  Only fka_tree_attend[_paged],
+ * fka_plan_get_info, fka_plan_device_error and fka_plan_destroy take it. */
+fka_status fka_plan_create_tree(const fka_heads *heads, const fka_prefill_desc *desc, fka_plan **out);
+fka_status fka_plan_create_tree_paged(const fka_heads *heads, const fka_prefill_paged_desc *desc, fka_plan **out);
+
+/*
+ * Arguments as in fka_prefill and fka_prefill_paged, token t being node t, and
+ *   masks  uint64 [N][n] (device, 8-byte aligned): node i of branch b reads the whole prefix, b's suffix positions
+ *          [0, suffix_len[b]) and position suffix_len[b] + j for every bit j < n of masks[b][i].  Any set of bits will do, its own bit and later nodes'
+ *          included or not (bits from n on are ignored); a row without any key gets out = 0 and out_lse = -inf.
+ * A key that no bit shows has no influence on a row, whatever it holds.  A non-finite value of a suffix or node's V makes the rows that
+ * read its key NaN.
+ */
+fka_status fka_tree_attend(const fka_plan *plan, const void *q, const void *prefix_k, const void *prefix_v, const void *suffix_k,
+                           const void *suffix_v, const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse,
+                           void *stream);
+fka_status fka_tree_attend_paged(const fka_plan *plan, const void *q, const void *k_pool, const void *v_pool, const int32_t *page_table,
+                                 const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse, void *stream);
+
+typedef struct {
+    int32_t n_branches; /* N >= 1, at most 2^20 */
+    int32_t n_nodes;    /* n in [1, 64] */
+    int32_t n_kv_heads;
+    int32_t head_dim;   /* 64 or 128 */
+    int32_t max_len;    /* bound on suffix_len[b] + n (contiguous: at most suffix_cap) */
+    int32_t advance;    /* 1: suffix_len[b] += count[b] (0: the caller advances it: one layer of several) */
+} fka_accept_desc;
+
+/*
+ * The root is accepted.  Another node is right where its parent is in [0, i), its token is the one chosen behind its parent
+ * (tokens[b][i] == targets[b][parent]) and no node before it has this parent and token; it is accepted where all the nodes that it reads
+ * (masks[b][i], and itself) are right, the root counting as right.  With the masks of fka_tree_layout the accepted nodes i_0 = 0 < i_1 < .. are a path.  K and V row
+ * suffix_len[b] + i_j of every KV head is moved to row suffix_len[b] + j; rows behind the last accepted node's keep what they hold, and
+ * are no part of the context.
+ *   parents, tokens, targets int32 [N][n]; masks uint64 [N][n] (device)
+ *   suffix_k    bf16 [N][Hkv][suffix_cap][d] (suffix_v likewise)
+ *   suffix_len  int32 [N], the suffixes before the nodes
+ *   path        int32 [N][n]: the accepted nodes, then -1
+ *   count       int32 [N]: how many
+ *   next        int32 [N]: targets of the last accepted node, the root's token of the next step
+ *   err         int32 (device) or NULL
+ * A branch without room (suffix_len[b] negative, or past max_len with n more) keeps its cache and length; its path is -1, its count 0,
+ * its next -1, and bit 2 is or-ed into *err.  What is written may overlap neither itself nor what is read (FKA_ERR_INVALID_ARG).
+ */
+fka_status fka_tree_accept(const fka_accept_desc *desc, const int32_t *parents, const uint64_t *masks, const int32_t *tokens,
+                           const int32_t *targets, void *suffix_k, void *suffix_v, int32_t suffix_cap, int32_t *suffix_len,
+                           int32_t *path, int32_t *count, int32_t *next, int32_t *err, void *stream);
+
+/* The same in the page pool (suffix position u as in fka_rotate_append_paged; the sequences' suffix pages are their own).  A branch whose
+ * accepted rows need a page that is not in [0, n_pool_pages) counts as one without room. */
+fka_status fka_tree_accept_paged(const fka_accept_desc *desc, const int32_t *parents, const uint64_t *masks, const int32_t *tokens,
+                                 const int32_t *targets, void *k_pool, void *v_pool, const int32_t *page_table,
+                                 const int32_t *prefix_len, int32_t max_pages_per_seq, int32_t n_pool_pages, int32_t *suffix_len,
+                                 int32_t *path, int32_t *count, int32_t *next, int32_t *err, void *stream);
+
 /* -------------------------------------------------- new tokens: norm, rotation, store */
 
 /*

@@ -28,6 +28,7 @@ struct fka_plan {
     // instruction prefill on the tiled kernel: blocks of up to eight 32-row units, key ranges (all,
     // those with prefix tiles), whole prefix tiles of 64 keys
     bool prefill_tiles = false;
+    bool tree = false;          // attention of drafted trees (tokens are nodes), on the tiled kernel
     int32_t tile_unit_groups = 0, tile_ranges = 0, tile_prefix_ranges = 0, tile_prefix = 0;
     fka::TileSplit tile_split{};
     int32_t max_suffix_len = 0;
@@ -126,6 +127,12 @@ bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0
 #define REQUIRE_OPT4(p)                                                           \
     do {                                                                          \
         if ((p) && !aligned4(p)) return fail(FKA_ERR_INVALID_ARG, "%s is not 4-byte aligned", #p); \
+    } while (0)
+
+#define REQUIRE_PTR8(p)                                                           \
+    do {                                                                          \
+        if (!(p)) return fail(FKA_ERR_INVALID_ARG, "%s is null", #p);             \
+        if (reinterpret_cast<uintptr_t>(p) & 7u) return fail(FKA_ERR_INVALID_ARG, "%s is not 8-byte aligned", #p); \
     } while (0)
 
 // A caller's memory: `rows` rows of `bytes` bytes, `step` bytes apart (one row: a dense range).  Nothing where `at` is null.
@@ -452,11 +459,13 @@ fka_status run_decode(const fka_plan *p, const fka::AttnArgs &a, const int32_t *
 // The instruction prefill's two launches: the tiled kernel with the merge in its
 // explicit mode (every row merges its ranges' partials), or the partial kernel's prefill
 // instantiation with the plan-mode merge.
-fka_status run_prefill(const fka_plan *p, const fka::AttnArgs &a, float *out, float *out_lse, hipStream_t s)
+fka_status run_prefill(const fka_plan *p, const fka::AttnArgs &a, float *out, float *out_lse, hipStream_t s,
+                       const uint64_t *masks = nullptr)
 {
     hipError_t e;
     if (p->prefill_tiles) {
-        fka::PrefillArgs t{};
+        fka::TreeArgs t{};
+        t.masks = masks;  // a tree plan's only
         t.q = a.q;
         t.prefix_k = a.prefix_k;
         t.prefix_v = a.prefix_v;
@@ -486,7 +495,7 @@ fka_status run_prefill(const fka_plan *p, const fka::AttnArgs &a, float *out, fl
         t.prefix_tiles = p->tile_prefix;
         t.split = p->tile_split;
         t.scale_log2 = p->scale * 1.4426950408889634f;
-        e = fka::launch_prefill_tiles(t, p->n_blocks, p->d, s);
+        e = p->tree ? fka::launch_tree_tiles(t, p->n_blocks, p->d, s) : fka::launch_prefill_tiles(t, p->n_blocks, p->d, s);
         if (e != hipSuccess) return hip_fail(e, "prefill kernel launch");
         fka::MergeArgs m{};
         m.part_o = p->part_o;
@@ -590,7 +599,7 @@ bool use_prefill_tiles(const fka_plan *p)
 }
 
 fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t Lp, int32_t max_suffix_len,
-                          int32_t blocks, const PrefillLayout &lay, fka_plan **out)
+                          int32_t blocks, const PrefillLayout &lay, fka_plan **out, bool tree = false)
 {
     const int64_t S = (int64_t)N * n;  // virtual sequences
     if (S > fka::kMaxSeqs)
@@ -610,6 +619,7 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
     };
     init_heads(p, heads);
     p->prefill_n = n;
+    p->tree = tree;
     p->n_branches = N;
     p->n_seqs = (int32_t)S;
     p->share_prefix = 1;
@@ -630,10 +640,10 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
     if ((e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, p->device)) != hipSuccess)
         return bail(hip_fail(e, "hipDeviceGetAttribute"));
     const int tile_rows = fka::prefill_tiles_unit_rows(), tile_waves = fka::prefill_tiles_waves();
-    if (use_prefill_tiles(p)) {
+    if (tree || use_prefill_tiles(p)) {
         // The tiled kernel: units of 32 consecutive rows of a KV head, eight per block (one per
         // wave) over one of R ranges of the keys, R such that the blocks fill the device.
-        const int per_cu = fka::prefill_tiles_blocks_per_cu(p->d, lay.paged);
+        const int per_cu = fka::prefill_tiles_blocks_per_cu(p->d, lay.paged, tree);
         if (per_cu <= 0) return bail(fail(FKA_ERR_HIP, "occupancy query of the prefill kernel failed"));
         const int64_t rows_head = S * G;
         const int32_t U = (int32_t)ceil_div(rows_head, tile_rows);
@@ -757,6 +767,8 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
 
 // Largest device id range of the copies below: a launch's threads stay below 2^32.
 constexpr int32_t kMaxRotateTokens = 1 << 25;
+// Most drafted trees of a call.
+constexpr int32_t kMaxTrees = 1 << 20;
 
 // The jobs of a decode over 4-bit tiles: ranges of prefix tiles and shares of the suffixes.  Two blocks are resident on a
 // compute unit, and each unit is to have one of either kind: a prefix job is bound by the vector units, a suffix job by its
@@ -1076,7 +1088,7 @@ fka_status fka_plan_create_contig(const fka_heads *heads, const fka_contig_desc 
     return ok();
 }
 
-fka_status fka_plan_create_prefill(const fka_heads *heads, const fka_prefill_desc *desc, fka_plan **out)
+static fka_status create_prefill_contig(const fka_heads *heads, const fka_prefill_desc *desc, fka_plan **out, bool tree)
 {
     REQUIRE(out != nullptr, "out is null");
     *out = nullptr;
@@ -1091,11 +1103,23 @@ fka_status fka_plan_create_prefill(const fka_heads *heads, const fka_prefill_des
             "max_suffix_len (%d) must be in [n_tokens=%d, suffix_cap=%d]", desc->max_suffix_len, desc->n_tokens,
             desc->suffix_cap);
     REQUIRE(desc->blocks >= 0, "blocks (%d) must be >= 0", desc->blocks);
+    if (tree && desc->n_tokens > fka::kMaxNodes)
+        return fail(FKA_ERR_UNSUPPORTED, "%d nodes to a tree exceed the limit of %d", desc->n_tokens, fka::kMaxNodes);
     return create_prefill(heads, desc->n_branches, desc->n_tokens, desc->prefix_len, desc->max_suffix_len,
-                          desc->blocks, PrefillLayout{false, desc->suffix_cap, 0, 0}, out);
+                          desc->blocks, PrefillLayout{false, desc->suffix_cap, 0, 0}, out, tree);
 }
 
-fka_status fka_plan_create_prefill_paged(const fka_heads *heads, const fka_prefill_paged_desc *desc, fka_plan **out)
+fka_status fka_plan_create_prefill(const fka_heads *heads, const fka_prefill_desc *desc, fka_plan **out)
+{
+    return create_prefill_contig(heads, desc, out, false);
+}
+
+fka_status fka_plan_create_tree(const fka_heads *heads, const fka_prefill_desc *desc, fka_plan **out)
+{
+    return create_prefill_contig(heads, desc, out, true);
+}
+
+static fka_status create_prefill_pool(const fka_heads *heads, const fka_prefill_paged_desc *desc, fka_plan **out, bool tree)
 {
     REQUIRE(out != nullptr, "out is null");
     *out = nullptr;
@@ -1113,8 +1137,20 @@ fka_status fka_plan_create_prefill_paged(const fka_heads *heads, const fka_prefi
     const int64_t pages = ceil_div(desc->prefix_len, fka::kPageSize) + ceil_div(desc->max_suffix_len, fka::kPageSize);
     REQUIRE(pages <= desc->max_pages_per_seq, "the prefix and max_suffix_len need %lld pages, max_pages_per_seq is %d",
             (long long)pages, desc->max_pages_per_seq);
+    if (tree && desc->n_tokens > fka::kMaxNodes)
+        return fail(FKA_ERR_UNSUPPORTED, "%d nodes to a tree exceed the limit of %d", desc->n_tokens, fka::kMaxNodes);
     return create_prefill(heads, desc->n_branches, desc->n_tokens, desc->prefix_len, desc->max_suffix_len,
-                          desc->blocks, PrefillLayout{true, 0, desc->max_pages_per_seq, desc->n_pool_pages}, out);
+                          desc->blocks, PrefillLayout{true, 0, desc->max_pages_per_seq, desc->n_pool_pages}, out, tree);
+}
+
+fka_status fka_plan_create_prefill_paged(const fka_heads *heads, const fka_prefill_paged_desc *desc, fka_plan **out)
+{
+    return create_prefill_pool(heads, desc, out, false);
+}
+
+fka_status fka_plan_create_tree_paged(const fka_heads *heads, const fka_prefill_paged_desc *desc, fka_plan **out)
+{
+    return create_prefill_pool(heads, desc, out, true);
 }
 
 fka_status fka_plan_create_paged(const fka_heads *heads, const fka_paged_desc *desc, const int32_t *host_group_start,
@@ -1350,13 +1386,11 @@ fka_status fka_fork_decode_noalloc(const fka_heads *heads, const fka_contig_desc
     return run_decode(&p, a, suffix_len, out, out_lse, static_cast<hipStream_t>(stream));
 }
 
-fka_status fka_prefill(const fka_plan *p, const void *q, const void *prefix_k, const void *prefix_v,
-                       const void *suffix_k, const void *suffix_v, const int32_t *suffix_len, float *out,
-                       float *out_lse, void *stream)
+// masks: a tree plan's
+static fka_status prefill_contig(const fka_plan *p, const void *q, const void *prefix_k, const void *prefix_v, const void *suffix_k,
+                                 const void *suffix_v, const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse,
+                                 void *stream)
 {
-    REQUIRE(p != nullptr, "plan is null");
-    REQUIRE(p->prefill_n > 0, "plan is not an instruction-prefill plan (fka_plan_create_prefill)");
-    REQUIRE(!p->paged, "plan is a paged prefill plan: use fka_prefill_paged");
     REQUIRE_PTR16(q);
     if (p->prefix_len > 0) {
         REQUIRE_PTR16(prefix_k);
@@ -1375,15 +1409,12 @@ fka_status fka_prefill(const fka_plan *p, const void *q, const void *prefix_k, c
     a.suffix_v = static_cast<const uint16_t *>(suffix_v);
     a.suffix_len = suffix_len;
     a.prefill_n = p->prefill_n;
-    return run_prefill(p, a, out, out_lse, static_cast<hipStream_t>(stream));
+    return run_prefill(p, a, out, out_lse, static_cast<hipStream_t>(stream), masks);
 }
 
-fka_status fka_prefill_paged(const fka_plan *p, const void *q, const void *k_pool, const void *v_pool,
-                             const int32_t *page_table, const int32_t *suffix_len, float *out, float *out_lse,
-                             void *stream)
+static fka_status prefill_pool(const fka_plan *p, const void *q, const void *k_pool, const void *v_pool, const int32_t *page_table,
+                               const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse, void *stream)
 {
-    REQUIRE(p != nullptr, "plan is null");
-    REQUIRE(p->prefill_n > 0 && p->paged, "plan is not a paged instruction-prefill plan (fka_plan_create_prefill_paged)");
     REQUIRE_PTR16(q);
     REQUIRE_PTR16(k_pool);
     REQUIRE_PTR16(v_pool);
@@ -1398,7 +1429,47 @@ fka_status fka_prefill_paged(const fka_plan *p, const void *q, const void *k_poo
     a.page_table = page_table;
     a.suffix_len = suffix_len;
     a.prefill_n = p->prefill_n;
-    return run_prefill(p, a, out, out_lse, static_cast<hipStream_t>(stream));
+    return run_prefill(p, a, out, out_lse, static_cast<hipStream_t>(stream), masks);
+}
+
+fka_status fka_prefill(const fka_plan *p, const void *q, const void *prefix_k, const void *prefix_v,
+                       const void *suffix_k, const void *suffix_v, const int32_t *suffix_len, float *out,
+                       float *out_lse, void *stream)
+{
+    REQUIRE(p != nullptr, "plan is null");
+    REQUIRE(p->prefill_n > 0, "plan is not an instruction-prefill plan (fka_plan_create_prefill)");
+    REQUIRE(!p->tree, "plan is a tree plan: use fka_tree_attend");
+    REQUIRE(!p->paged, "plan is a paged prefill plan: use fka_prefill_paged");
+    return prefill_contig(p, q, prefix_k, prefix_v, suffix_k, suffix_v, suffix_len, nullptr, out, out_lse, stream);
+}
+
+fka_status fka_prefill_paged(const fka_plan *p, const void *q, const void *k_pool, const void *v_pool,
+                             const int32_t *page_table, const int32_t *suffix_len, float *out, float *out_lse,
+                             void *stream)
+{
+    REQUIRE(p != nullptr, "plan is null");
+    REQUIRE(p->prefill_n > 0 && p->paged, "plan is not a paged instruction-prefill plan (fka_plan_create_prefill_paged)");
+    REQUIRE(!p->tree, "plan is a tree plan: use fka_tree_attend_paged");
+    return prefill_pool(p, q, k_pool, v_pool, page_table, suffix_len, nullptr, out, out_lse, stream);
+}
+
+fka_status fka_tree_attend(const fka_plan *p, const void *q, const void *prefix_k, const void *prefix_v, const void *suffix_k,
+                           const void *suffix_v, const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse,
+                           void *stream)
+{
+    REQUIRE(p != nullptr, "plan is null");
+    REQUIRE(p->tree && !p->paged, "plan is not a tree plan over contiguous buffers (fka_plan_create_tree)");
+    REQUIRE_PTR8(masks);
+    return prefill_contig(p, q, prefix_k, prefix_v, suffix_k, suffix_v, suffix_len, masks, out, out_lse, stream);
+}
+
+fka_status fka_tree_attend_paged(const fka_plan *p, const void *q, const void *k_pool, const void *v_pool, const int32_t *page_table,
+                                 const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse, void *stream)
+{
+    REQUIRE(p != nullptr, "plan is null");
+    REQUIRE(p->tree && p->paged, "plan is not a paged tree plan (fka_plan_create_tree_paged)");
+    REQUIRE_PTR8(masks);
+    return prefill_pool(p, q, k_pool, v_pool, page_table, suffix_len, masks, out, out_lse, stream);
 }
 
 fka_status fka_partials(const fka_plan *p, const void *q, const void *prefix_k, const void *prefix_v,
@@ -2239,6 +2310,137 @@ fka_status fka_evict(int32_t n_kv_heads, int32_t head_dim, int32_t len, int32_t 
     hipError_t e = fka::launch_evict(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "evict kernel launch");
     return ok();
+}
+
+/* ------------------------------------------------------------------ drafted trees */
+
+fka_status fka_tree_layout(int32_t n_branches, int32_t n_nodes, const int32_t *parents, const int32_t *base, uint64_t *masks,
+                           int32_t *positions, int32_t *err, void *stream)
+{
+    REQUIRE(n_branches >= 1 && n_nodes >= 1, "n_branches (%d) and n_nodes (%d) must be >= 1", n_branches, n_nodes);
+    if (n_nodes > fka::kMaxNodes) return fail(FKA_ERR_UNSUPPORTED, "%d nodes to a tree exceed the limit of %d", n_nodes, fka::kMaxNodes);
+    if (n_branches > kMaxTrees) return fail(FKA_ERR_UNSUPPORTED, "%d trees exceed the limit of %d", n_branches, kMaxTrees);
+    REQUIRE_PTR4(parents);
+    REQUIRE_PTR4(base);
+    REQUIRE_PTR8(masks);
+    REQUIRE_PTR4(positions);
+    REQUIRE_OPT4(err);
+    const size_t N = n_branches, nodes = N * n_nodes;
+    const fka_status st = check_apart({{masks, nodes * 8, "masks"}, {positions, nodes * 4, "positions"}},
+                                      {{parents, nodes * 4, "parents"}, {base, N * 4, "base"}, {err, 4, "err"}});
+    if (st != FKA_OK) return st;
+    fka::LayoutArgs a{parents, base, masks, positions, n_branches, n_nodes, err};
+    const hipError_t e = fka::launch_tree_layout(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "tree layout kernel launch");
+    return ok();
+}
+
+// The checks and arguments that the contiguous and the paged acceptance share; dst_rows rows a cache.
+static fka_status run_accept(const fka_accept_desc *desc, fka::AcceptArgs &a, size_t dst_rows, size_t table_entries, void *stream)
+{
+    REQUIRE_PTR4(a.parents);
+    REQUIRE(a.masks != nullptr && (reinterpret_cast<uintptr_t>(a.masks) & 7u) == 0, "masks is null or not 8-byte aligned");
+    REQUIRE(a.tokens != nullptr && aligned4(a.tokens), "tokens is null or not 4-byte aligned");
+    REQUIRE(a.targets != nullptr && aligned4(a.targets), "targets is null or not 4-byte aligned");
+    REQUIRE(a.k != nullptr && a.v != nullptr && aligned16(a.k) && aligned16(a.v), "the K or V cache is null or not 16-byte aligned");
+    REQUIRE(a.suffix_len != nullptr && aligned4(a.suffix_len), "suffix_len is null or not 4-byte aligned");
+    REQUIRE(a.path != nullptr && aligned4(a.path), "path is null or not 4-byte aligned");
+    REQUIRE(a.count != nullptr && aligned4(a.count), "count is null or not 4-byte aligned");
+    REQUIRE(a.next != nullptr && aligned4(a.next), "next is null or not 4-byte aligned");
+    REQUIRE(aligned4(a.err), "err is not 4-byte aligned");
+    a.n_branches = desc->n_branches;
+    a.n_nodes = desc->n_nodes;
+    a.n_kv_heads = desc->n_kv_heads;
+    a.max_len = desc->max_len;
+    a.advance = desc->advance;
+    const size_t N = desc->n_branches, nodes = N * desc->n_nodes, cache = dst_rows * desc->head_dim * 2;
+    const fka_status st = check_apart({{a.k, cache, "the K cache"},
+                                       {a.v, cache, "the V cache"},
+                                       {a.path, nodes * 4, "path"},
+                                       {a.count, N * 4, "count"},
+                                       {a.next, N * 4, "next"},
+                                       {a.suffix_len, N * 4, "suffix_len"}},
+                                      {{a.parents, nodes * 4, "parents"},
+                                       {a.masks, nodes * 8, "masks"},
+                                       {a.tokens, nodes * 4, "tokens"},
+                                       {a.targets, nodes * 4, "targets"},
+                                       {a.page_table, table_entries * 4, "page_table"},
+                                       {a.seq_prefix_len, N * 4, "prefix_len"},
+                                       {a.err, 4, "err"}});
+    if (st != FKA_OK) return st;
+    const hipError_t e = fka::launch_tree_accept(a, desc->head_dim, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "tree accept kernel launch");
+    return ok();
+}
+
+static fka_status check_accept(const fka_accept_desc *desc)
+{
+    REQUIRE(desc != nullptr, "desc is null");
+    REQUIRE(desc->n_branches >= 1 && desc->n_nodes >= 1, "n_branches (%d) and n_nodes (%d) must be >= 1", desc->n_branches, desc->n_nodes);
+    REQUIRE(desc->n_kv_heads >= 1 && desc->n_kv_heads <= 65535, "n_kv_heads %d outside [1, 65535]", desc->n_kv_heads);
+    if (desc->head_dim != 64 && desc->head_dim != 128)
+        return fail(FKA_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", desc->head_dim);
+    if (desc->n_nodes > fka::kMaxNodes)
+        return fail(FKA_ERR_UNSUPPORTED, "%d nodes to a tree exceed the limit of %d", desc->n_nodes, fka::kMaxNodes);
+    if (desc->n_branches > kMaxTrees) return fail(FKA_ERR_UNSUPPORTED, "%d trees exceed the limit of %d", desc->n_branches, kMaxTrees);
+    REQUIRE(desc->max_len >= 0, "max_len (%d) must be >= 0", desc->max_len);
+    if (desc->max_len > kMaxTokens) return fail(FKA_ERR_UNSUPPORTED, "max_len %d is too long (limit %d)", desc->max_len, kMaxTokens);
+    REQUIRE(desc->advance == 0 || desc->advance == 1, "advance must be 0 or 1");
+    return FKA_OK;
+}
+
+fka_status fka_tree_accept(const fka_accept_desc *desc, const int32_t *parents, const uint64_t *masks, const int32_t *tokens,
+                           const int32_t *targets, void *suffix_k, void *suffix_v, int32_t suffix_cap, int32_t *suffix_len,
+                           int32_t *path, int32_t *count, int32_t *next, int32_t *err, void *stream)
+{
+    const fka_status st = check_accept(desc);
+    if (st != FKA_OK) return st;
+    REQUIRE(desc->max_len <= suffix_cap, "max_len (%d) must be at most suffix_cap (%d)", desc->max_len, suffix_cap);
+    fka::AcceptArgs a{};
+    a.parents = parents;
+    a.masks = masks;
+    a.tokens = tokens;
+    a.targets = targets;
+    a.k = static_cast<uint16_t *>(suffix_k);
+    a.v = static_cast<uint16_t *>(suffix_v);
+    a.suffix_cap = suffix_cap;
+    a.suffix_len = suffix_len;
+    a.path = path;
+    a.count = count;
+    a.next = next;
+    a.err = err;
+    return run_accept(desc, a, (size_t)desc->n_branches * desc->n_kv_heads * suffix_cap, 0, stream);
+}
+
+fka_status fka_tree_accept_paged(const fka_accept_desc *desc, const int32_t *parents, const uint64_t *masks, const int32_t *tokens,
+                                 const int32_t *targets, void *k_pool, void *v_pool, const int32_t *page_table,
+                                 const int32_t *prefix_len, int32_t max_pages_per_seq, int32_t n_pool_pages, int32_t *suffix_len,
+                                 int32_t *path, int32_t *count, int32_t *next, int32_t *err, void *stream)
+{
+    const fka_status st = check_accept(desc);
+    if (st != FKA_OK) return st;
+    REQUIRE(max_pages_per_seq >= 1, "max_pages_per_seq must be >= 1");
+    REQUIRE(n_pool_pages >= 0, "n_pool_pages must be >= 0");
+    REQUIRE_PTR4(page_table);
+    REQUIRE_PTR4(prefix_len);
+    fka::AcceptArgs a{};
+    a.parents = parents;
+    a.masks = masks;
+    a.tokens = tokens;
+    a.targets = targets;
+    a.k = static_cast<uint16_t *>(k_pool);
+    a.v = static_cast<uint16_t *>(v_pool);
+    a.page_table = page_table;
+    a.seq_prefix_len = prefix_len;
+    a.max_pages = max_pages_per_seq;
+    a.n_pool_pages = n_pool_pages;
+    a.suffix_len = suffix_len;
+    a.path = path;
+    a.count = count;
+    a.next = next;
+    a.err = err;
+    return run_accept(desc, a, (size_t)n_pool_pages * desc->n_kv_heads * fka::kPageSize, (size_t)desc->n_branches * max_pages_per_seq,
+                      stream);
 }
 
 }  // extern "C"

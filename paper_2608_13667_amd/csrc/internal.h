@@ -361,6 +361,13 @@ struct PrefillArgs {
     TileSplit split;
 };
 
+// Attention of drafted trees (prefill.hip): token t of a branch is node t of its tree, whose key is at suffix position L_b + t.  A node
+// reads the prefix, its branch's suffix and node j's key where its mask has bit j.
+struct TreeArgs : PrefillArgs {
+    const uint64_t *masks;  // [N][n], n <= 64
+};
+constexpr int kMaxNodes = 64;
+
 // New tokens' norm, rotation and store (rotate.h).
 struct RotateArgs {
     const uint16_t *q, *k, *v;       // [tokens] rows of heads x d, q_stride / k_stride / v_stride elements apart
@@ -463,11 +470,37 @@ struct EvictArgs {
     int32_t n_kv_heads, head_dim, chunks, chunk_blocks;
 };
 
+// Drafted trees (tree.h): what each node reads; the accepted nodes and their cache rows.
+struct LayoutArgs {
+    const int32_t *parents;  // [N][n]
+    const int32_t *base;     // [N]
+    uint64_t *masks;         // [N][n]
+    int32_t *positions;      // [N][n]
+    int32_t n_branches, n_nodes;
+    int32_t *err;            // nullable
+};
+
+struct AcceptArgs {
+    const int32_t *parents, *tokens, *targets;  // [N][n]
+    const uint64_t *masks;                      // [N][n]
+    uint16_t *k, *v;                 // contiguous [N][Hkv][cap][d] or pools [pages][Hkv][16][d]
+    int32_t *suffix_len;             // [N]
+    const int32_t *page_table;       // paged: [N][max_pages]; else null
+    const int32_t *seq_prefix_len;   // paged: [N]
+    int32_t *path;                   // [N][n]
+    int32_t *count, *next;           // [N]
+    int32_t n_branches, n_nodes, n_kv_heads;
+    int32_t max_len, suffix_cap, max_pages, n_pool_pages;
+    int32_t advance;
+    int32_t *err;                    // nullable
+};
+
 // error-flag bits (device)
 constexpr int32_t kErrSuffixClamped = 1;
 constexpr int32_t kErrAppendNoRoom = 2;
 constexpr int32_t kErrBadPage = 4;
 constexpr int32_t kErrBadSchedule = 8;
+constexpr int32_t kErrBadTree = 16;
 
 hipError_t launch_partials(const AttnArgs &a, int n_blocks, int head_dim, int row_tiles, hipStream_t s);
 // Resident blocks per compute unit of the partial kernel for this shape (0 on error).
@@ -488,8 +521,9 @@ hipError_t launch_merge(const MergeArgs &a, int head_dim, hipStream_t s);
 // so units) per block, resident blocks per compute unit, and the launch.
 int prefill_tiles_unit_rows();
 int prefill_tiles_waves();
-int prefill_tiles_blocks_per_cu(int head_dim, bool paged);
+int prefill_tiles_blocks_per_cu(int head_dim, bool paged, bool tree = false);
 hipError_t launch_prefill_tiles(const PrefillArgs &a, int n_blocks, int head_dim, hipStream_t s);
+hipError_t launch_tree_tiles(const TreeArgs &a, int n_blocks, int head_dim, hipStream_t s);
 hipError_t launch_append(const AppendArgs &a, int n_seqs, hipStream_t s);
 hipError_t launch_gather(const GatherArgs &a, hipStream_t s);
 hipError_t launch_scatter(const ScatterArgs &a, hipStream_t s);
@@ -501,6 +535,8 @@ int mx_blocks_per_cu(int head_dim, int row_tiles);
 hipError_t launch_mx_partials(const MxArgs &a, int n_jobs, int head_dim, int row_tiles, hipStream_t s);
 hipError_t launch_key_weights(const WeightsArgs &a, int head_dim, hipStream_t s);
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
+hipError_t launch_tree_layout(const LayoutArgs &a, hipStream_t s);
+hipError_t launch_tree_accept(const AcceptArgs &a, int head_dim, hipStream_t s);
 hipError_t launch_read_probe(const void *buf, size_t bytes, int blocks, int threads, int unroll, uint32_t *sink,
                              hipStream_t s);
 

@@ -4,13 +4,15 @@
 // merge_kernel: log-sum-exp combination of the partials of each (sequence, head).
 // append_kernel / gather_kernel: suffix append and paged gather (data movement).
 // The operators around a snapshot's cache are in headers of their own: rotate.h (norm, rotation and store of new
-// tokens), mx_tiles.h (4-bit tiles), mx_attend.h (decode over them), evict.h (key weights, shortening).
+// tokens), mx_tiles.h (4-bit tiles), mx_attend.h (decode over them), evict.h (key weights, shortening); tree.h has the layout and the
+// acceptance of drafted trees (their attention is in prefill.hip, sampling in sample.hip).
 #include "evict.h"
 #include "internal.h"
 #include "merge_row.h"
 #include "mx_attend.h"
 #include "mx_tiles.h"
 #include "rotate.h"
+#include "tree.h"
 
 namespace fka {
 namespace {
@@ -418,5 +420,9 @@ hipError_t launch_mx_partials(const MxArgs &a, int n_jobs, int head_dim, int row
 hipError_t launch_key_weights(const WeightsArgs &a, int head_dim, hipStream_t s) { return launch_key_weights_kernel(a, head_dim, s); }
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s) { return launch_evict_kernels(a, s); }
+
+hipError_t launch_tree_layout(const LayoutArgs &a, hipStream_t s) { return launch_tree_layout_kernel(a, s); }
+
+hipError_t launch_tree_accept(const AcceptArgs &a, int head_dim, hipStream_t s) { return launch_tree_accept_kernel(a, head_dim, s); }
 
 }  // namespace fka

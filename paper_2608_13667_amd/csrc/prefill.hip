@@ -313,9 +313,13 @@ struct MatrixPlan {
 // needs fewer cross-lane steps, but the same products take half as much energy again there: at the
 // power limit, registers only, 1370 TFLOP/s against 2000; here the clock fell from 2.4 to 2.0 GHz
 // and the call took as long.)
-template <int HD, bool PAGED>
-__device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
+//
+// With TreeArgs the tokens of a branch are the nodes of a tree: a row reads its branch's whole suffix and, of the nodes' keys
+// behind it, those of its mask's bits.  A row's keys of a tail tile are then bits too, eight to each of the lane's groups.
+template <int HD, bool PAGED, class Args>
+__device__ INLINE inline void prefill_tiles(const Args &a)
 {
+    constexpr bool TREE = std::is_same<Args, TreeArgs>::value;
     constexpr int ROWB = HD * 2;            // bytes per key row
     constexpr int CPR = HD / 8;             // 16-byte chunks per key row
     constexpr int NC = HD / 32;             // k-steps of the q.k product
@@ -339,6 +343,8 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
     __shared__ __attribute__((aligned(1024))) char lds[LDS_BYTES];
     // per tile buffer, the groups of a tail tile: branch and last key (see issue_tail)
     __shared__ __attribute__((aligned(16))) int2 s_grp[STAGES][NW];
+    // the nodes that each row of each unit reads (in registers they are four of the ten that do not fit)
+    __shared__ __attribute__((aligned(16))) uint64_t s_mask[TREE ? NW * 32 : 1];
 
     const int tid = threadIdx.x;
     const int lane = tid & 63, l16 = lane & 15, q4 = lane >> 4;
@@ -377,12 +383,14 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
     // Lane i of a chunk of 64 branches: branch br_first + i's length before the instruction, and the
     // inclusive scan of the branches' groups (br_base groups precede the chunk)
     int br_len = 0, br_scan = 0, br_first = br_a, br_base = pre_groups, n_groups = 0;
+    // the last token of branch b whose key a row of the block reads (a node may read any node of its branch)
+    auto last_token = [&](int b) INLINE { return TREE ? n - 1 : min(n - 1, seq_z - b * n); };
     auto request_branches = [&](int first) INLINE { return first + lane <= br_z ? a.suffix_len[first + lane] : 0; };
     auto take_branches = [&](int first, int raw) INLINE {
         const int b = first + lane;
         br_len = min(max(raw, 0), a.max_suffix_len - n);
         if (b <= br_z && br_len != raw) atomicOr(a.err, kErrSuffixClamped);
-        br_scan = scan64(b <= br_z ? (br_len + min(n - 1, seq_z - b * n) + GRP) / GRP : 0);  // (keys + 7) / 8, keys = len + t + 1
+        br_scan = scan64(b <= br_z ? (br_len + last_token(b) + GRP) / GRP : 0);  // (keys + 7) / 8, keys = len + t + 1
         br_first = first;
     };
     // (requested in front of the first tile: loads return in order)
@@ -482,7 +490,8 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
 
     // Tail tile j: this wave loads group 8 j + wave of the tail and leaves the group's branch (-1: the
     // prefix, -2: no group) and limit in s_grp: a row of the branch with token t reads the group's
-    // keys k <= limit + t, every row those of the prefix with k <= limit.
+    // keys k <= limit + t, every row those of the prefix with k <= limit.  (A node reads k < limit, and key limit + j where
+    // its mask has bit j.)
     auto issue_tail = [&](int j, int st) INLINE {
         const int idx = j * NW + wave;
         int b = -2, limit = -1, rows_ok = 0, pos = 0;
@@ -498,7 +507,7 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
             const int i = uni(__builtin_ctzll(__builtin_amdgcn_ballot_w64(br_scan > k)));
             b = br_first + i;
             const int L = __builtin_amdgcn_readlane(br_len, i);
-            const int keys = L + min(n - 1, seq_z - b * n) + 1;
+            const int keys = L + last_token(b) + 1;
             pos = GRP * (k - (__builtin_amdgcn_readlane(br_scan, i) - (keys + GRP - 1) / GRP));
             limit = L - pos;
             rows_ok = min(GRP, keys - pos);
@@ -766,16 +775,24 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
     // each row's limit.  What follows describes the tile whose q.k was last taken.
     // A lane's four keys of score tile i are keys 4 (q4 mod 2) + j of group 2 i + q4 / 2.
     bool use = true, tail = false;
-    int lim[2][MT];  // row t reads the keys k <= lim[t][i] of group 2 i + q4 / 2
+    [[maybe_unused]] int lim[2][MT];  // row t reads the keys k <= lim[t][i] of group 2 i + q4 / 2
+    static_assert(!TREE || MT * GRP == 32, "a row's keys of the lane's groups are the bits of a word");
+    [[maybe_unused]] uint32_t vis[2] = {~0u, ~0u};  // a tree's row t reads key k of group 2 i + q4 / 2 where bit 8 i + k is set
     uint32_t suffix_groups = 0;  // bit i: that group holds suffix keys (not the prefix's, which every row reads)
 #pragma unroll
     for (int i = 0; i < MT; ++i) lim[0][i] = lim[1][i] = KT;
     int row_bt[2];  // the rows' branch (past every branch beyond the head's rows) << 16 | token
+    // where this lane's rows' masks are in LDS
+    auto mask_at = [&]() INLINE {
+        return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&s_mask[wave * 32] + 8 * (opaque_lane_id() & 15);
+    };
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const int lr = u * 32 + 16 * t + l16;
         const int br = lr / a.split.branch_rows;
         row_bt[t] = lr < rows_head ? br << 16 | (lr / a.split.group - br * n) : 0x7fff0000;
+        if constexpr (TREE)  // (only this wave reads them, behind these writes; the four lanes of a row write the same)
+            ds_write_b64(mask_at() + 128 * t, lr < rows_head ? a.masks[lr / a.split.group] & ~0ull >> (64 - n) : 0);
     }
     const uint32_t grp0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&s_grp[0][0] + 8 * (q4 >> 1);
     auto any_qk = [&](int i) INLINE {
@@ -784,13 +801,22 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
         if (!tail) {
 #pragma unroll
             for (int q = 0; q < MT; ++q) lim[0][q] = lim[1][q] = KT;
+            vis[0] = vis[1] = ~0u;
         } else {
             uint64_t d[MT];
             static_for<MT>([&](auto Qc) INLINE {
                 constexpr int q = decltype(Qc)::value;
                 d[q] = ds_read_b64_at<16 * q>(grp0 + (i % STAGES) * (uint32_t)sizeof(s_grp[0]));
             });
+            [[maybe_unused]] uint64_t row_mask[2];
+            if constexpr (TREE) {
+                const uint32_t at = mask_at();
+                row_mask[0] = ds_read_b64_at<0>(at);
+                row_mask[1] = ds_read_b64_at<128>(at);
+                vis[0] = vis[1] = 0;
+            }
             lds_wait();
+            if constexpr (TREE) asm volatile("" : "+v"(row_mask[0]), "+v"(row_mask[1]));
 #pragma unroll
             for (int q = 0; q < MT; ++q) asm volatile("" : "+v"(d[q]));
             int most = -1;
@@ -801,11 +827,21 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
                 suffix_groups |= b >= 0 ? 1u << q : 0;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    lim[t][q] = b == -1 ? base : b == row_bt[t] >> 16 ? base + (row_bt[t] & 0xffff) : -1;
-                    most = max(most, lim[t][q]);
+                    if constexpr (TREE) {
+                        // the keys in front of the nodes' (`base` of them or all eight), then the mask's bits
+                        const int full = b == -1 ? base + 1 : base;
+                        const uint64_t nodes = b == -1 ? 0 : row_mask[t];
+                        const uint32_t bits = full >= GRP ? 0xffu
+                                              : full >= 0 ? (uint32_t)(nodes << full) | ((1u << full) - 1)
+                                                          : (uint32_t)(nodes >> min(-full, 63));
+                        vis[t] |= b == -1 || b == row_bt[t] >> 16 ? (bits & 0xffu) << (GRP * q) : 0;
+                    } else {
+                        lim[t][q] = b == -1 ? base : b == row_bt[t] >> 16 ? base + (row_bt[t] & 0xffff) : -1;
+                        most = max(most, lim[t][q]);
+                    }
                 }
             }
-            use = __builtin_amdgcn_ballot_w64(most >= 0) != 0;
+            use = __builtin_amdgcn_ballot_w64(TREE ? (vis[0] | vis[1]) != 0 : most >= 0) != 0;
         }
         if (use) matrix(std::false_type{}, zero{}, zero{}, (uint32_t)(i % STAGES) * KBYTES, 0u, sc, ph, pl);
     };
@@ -818,7 +854,8 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 4 * MT; ++i)
-                x[t][i] = (k0 + (i & 3) <= lim[t][i >> 2]) ? sc[t][i >> 2][i & 3] : -INFINITY;
+                x[t][i] = (TREE ? (vis[t] >> k0 & 1u << (GRP * (i >> 2) + (i & 3))) != 0 : k0 + (i & 3) <= lim[t][i >> 2]) ? sc[t][i >> 2][i & 3]
+                                                                                                                  : -INFINITY;
         softmax(x, ph, pl, i == 0);
     };
     auto any_pv = [&](int i) INLINE {
@@ -854,23 +891,27 @@ __device__ INLINE inline void prefill_tiles(const PrefillArgs &a)
                     for (int y = 0; y < 2; ++y) {
                         // the exponent bits that count as non-finite (none for the prefix's keys)
                         const uint32_t bad = (suffix_groups >> (2 * kk + y) & 1) ? 0x7f80u : ~0u;
-                        int first = 0x7fffffff;
+                        int first = TREE ? 0 : 0x7fffffff;  // (a tree: the bits of all such keys)
 #pragma unroll
                         for (int e = 0; e < PG; ++e) {
                             uint64_t w = (uint64_t)v[e / EG][e % EG][y];
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 if (((uint32_t)(w >> (16 * k)) & 0x7f80u) == bad) {
-                                    first = min(first, k0 + k);
+                                    first = TREE ? first | 1 << (k0 + k) : min(first, k0 + k);
                                     w &= ~((uint64_t)0xffffu << (16 * k));
                                 }
                             v[e / EG][e % EG][y] = (vtr_t)w;
                         }
 #pragma unroll
-                        for (int off = 1; off < 32; off <<= 1) first = min(first, __shfl_xor(first, off));
+                        for (int off = 1; off < 32; off <<= 1) {
+                            const int other = __shfl_xor(first, off);
+                            first = TREE ? first | other : min(first, other);
+                        }
 #pragma unroll
                         for (int t = 0; t < 2; ++t)
-                            l_run[t] = lim[t][2 * kk + y] >= first ? __builtin_nanf("") : l_run[t];
+                            l_run[t] = (TREE ? (vis[t] >> (GRP * (2 * kk + y)) & first) != 0 : lim[t][2 * kk + y] >= first) ? __builtin_nanf("")
+                                                                                                                      : l_run[t];
                     }
                 }
             }
@@ -1043,6 +1084,18 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     prefill_tiles<128, PAGED>(a);
 }
 
+template <bool PAGED>  // head_dim 128
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void tree_tiles_kernel(TreeArgs a)
+{
+    prefill_tiles<128, PAGED>(a);
+}
+
+template <bool PAGED>  // head_dim 64
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void tree_tiles_d64_kernel(TreeArgs a)
+{
+    prefill_tiles<64, PAGED>(a);
+}
+
 template <bool PAGED>  // head_dim 64
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void prefill_tiles_d64_kernel(PrefillArgs a)
 {
@@ -1054,10 +1107,15 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
 int prefill_tiles_unit_rows() { return 32; }
 int prefill_tiles_waves() { return NW; }
 
-int prefill_tiles_blocks_per_cu(int head_dim, bool paged)
+int prefill_tiles_blocks_per_cu(int head_dim, bool paged, bool tree)
 {
     const void *f = nullptr;
-    if (head_dim == 128)
+    if (tree && head_dim == 128)
+        f = paged ? reinterpret_cast<const void *>(&tree_tiles_kernel<true>) : reinterpret_cast<const void *>(&tree_tiles_kernel<false>);
+    else if (tree && head_dim == 64)
+        f = paged ? reinterpret_cast<const void *>(&tree_tiles_d64_kernel<true>)
+                  : reinterpret_cast<const void *>(&tree_tiles_d64_kernel<false>);
+    else if (head_dim == 128)
         f = paged ? reinterpret_cast<const void *>(&prefill_tiles_kernel<true>)
                   : reinterpret_cast<const void *>(&prefill_tiles_kernel<false>);
     else if (head_dim == 64)
@@ -1081,6 +1139,25 @@ hipError_t launch_prefill_tiles(const PrefillArgs &a, int n_blocks, int head_dim
             prefill_tiles_d64_kernel<true><<<n_blocks, 64 * NW, 0, s>>>(a);
         else
             prefill_tiles_d64_kernel<false><<<n_blocks, 64 * NW, 0, s>>>(a);
+    } else {
+        return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_tree_tiles(const TreeArgs &a, int n_blocks, int head_dim, hipStream_t s)
+{
+    if (n_blocks <= 0) return hipSuccess;
+    if (head_dim == 128) {
+        if (a.paged)
+            tree_tiles_kernel<true><<<n_blocks, 64 * NW, 0, s>>>(a);
+        else
+            tree_tiles_kernel<false><<<n_blocks, 64 * NW, 0, s>>>(a);
+    } else if (head_dim == 64) {
+        if (a.paged)
+            tree_tiles_d64_kernel<true><<<n_blocks, 64 * NW, 0, s>>>(a);
+        else
+            tree_tiles_d64_kernel<false><<<n_blocks, 64 * NW, 0, s>>>(a);
     } else {
         return hipErrorInvalidValue;
     }

@@ -22,7 +22,7 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 FKA_OK, FKA_ERR_INVALID_ARG, FKA_ERR_UNSUPPORTED, FKA_ERR_HIP, FKA_ERR_NOMEM = 0, -1, -2, -3, -4
-ERR_SUFFIX_CLAMPED, ERR_APPEND_NO_ROOM, ERR_BAD_PAGE, ERR_BAD_SCHEDULE = 1, 2, 4, 8
+ERR_SUFFIX_CLAMPED, ERR_APPEND_NO_ROOM, ERR_BAD_PAGE, ERR_BAD_SCHEDULE, ERR_BAD_TREE = 1, 2, 4, 8, 16
 
 
 class Heads(C.Structure):
@@ -78,6 +78,11 @@ class MxDesc(C.Structure):
                 ("n_pool_tiles", C.c_int32), ("suffix_cap", C.c_int32), ("max_suffix_len", C.c_int32), ("blocks", C.c_int32)]
 
 
+class AcceptDesc(C.Structure):
+    _fields_ = [("n_branches", C.c_int32), ("n_nodes", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("max_len", C.c_int32), ("advance", C.c_int32)]
+
+
 MX_TILE = 128  # tokens of a 4-bit tile
 
 _vp = C.c_void_p
@@ -131,6 +136,13 @@ _sig = {
     "fka_fork_step_mx": ([_vp] * 12, C.c_int),
     "fka_key_weights": ([C.POINTER(Heads), C.c_int32, C.c_int32, _vp, _vp, _vp, C.c_int32, _vp, C.c_int32, C.c_float, _vp],
                         C.c_int),
+    "fka_tree_layout": ([C.c_int32, C.c_int32] + [_vp] * 6, C.c_int),
+    "fka_plan_create_tree": ([C.POINTER(Heads), C.POINTER(PrefillDesc), C.POINTER(_vp)], C.c_int),
+    "fka_plan_create_tree_paged": ([C.POINTER(Heads), C.POINTER(PrefillPagedDesc), C.POINTER(_vp)], C.c_int),
+    "fka_tree_attend": ([_vp] * 11, C.c_int),
+    "fka_tree_attend_paged": ([_vp] * 10, C.c_int),
+    "fka_tree_accept": ([C.POINTER(AcceptDesc)] + [_vp] * 6 + [C.c_int32] + [_vp] * 6, C.c_int),
+    "fka_tree_accept_paged": ([C.POINTER(AcceptDesc)] + [_vp] * 8 + [C.c_int32, C.c_int32] + [_vp] * 6, C.c_int),
     "fka_evict_bytes": ([C.c_int32, C.c_int32], C.c_size_t),
     "fka_evict": ([C.c_int32] * 6 + [_vp, _vp, C.c_int32, _vp, C.c_int32] + [_vp] * 5 + [C.c_size_t, _vp], C.c_int),
 }
@@ -161,7 +173,8 @@ def version() -> int:
     return _lib.fka_version()
 
 
-_KIND_DTYPES = {"bf16": torch.bfloat16, "i32": torch.int32, "f32": torch.float32, "f64": torch.float64, "u8": torch.uint8}
+_KIND_DTYPES = {"bf16": torch.bfloat16, "i32": torch.int32, "f32": torch.float32, "f64": torch.float64, "u8": torch.uint8,
+                "i64": torch.int64}
 
 
 def _p(t: Optional[torch.Tensor], kind: Optional[str] = None, device: Optional[int] = None):
@@ -211,6 +224,7 @@ class Plan:
         self.paged = paged
         self.heads = heads
         self.n_seqs = n_seqs
+        self._tree = None  # of a tree plan: the shapes of q and of the masks
         self._mx = None  # of a plan over 4-bit tiles: the pool's shape, entries of the tile table
 
     @classmethod
@@ -270,6 +284,52 @@ class Plan:
         _check(_lib.fka_prefill(self._h, _p(q, "bf16", d), _p(prefix_k, "bf16", d), _p(prefix_v, "bf16", d),
                                 _p(suffix_k, "bf16", d), _p(suffix_v, "bf16", d), _p(suffix_len, "i32", d),
                                 _p(out, "f32", d), _p(out_lse, "f32", d), _stream(stream)))
+
+    @classmethod
+    def tree_plan(cls, n_q_heads, n_kv_heads, head_dim, n_branches, n_nodes, prefix_len, suffix_cap, max_suffix_len,
+                  softmax_scale=0.0, blocks=0) -> "Plan":
+        """A plan for the attention of drafted trees (fka_plan_create_tree); max_suffix_len counts the nodes."""
+        h = Heads(n_q_heads, n_kv_heads, head_dim, softmax_scale)
+        d = PrefillDesc(n_branches, n_nodes, prefix_len, suffix_cap, max_suffix_len, blocks)
+        out = _vp()
+        _check(_lib.fka_plan_create_tree(C.byref(h), C.byref(d), C.byref(out)))
+        plan = cls(out.value, False, h, n_branches * n_nodes)
+        plan._tree = (n_branches, n_nodes, n_q_heads, head_dim)
+        return plan
+
+    @classmethod
+    def tree_paged_plan(cls, n_q_heads, n_kv_heads, head_dim, n_branches, n_nodes, prefix_len, max_pages_per_seq, n_pool_pages,
+                        max_suffix_len, softmax_scale=0.0, blocks=0, page_size=16) -> "Plan":
+        """The same over the page pool (fka_plan_create_tree_paged)."""
+        h = Heads(n_q_heads, n_kv_heads, head_dim, softmax_scale)
+        d = PrefillPagedDesc(n_branches, n_nodes, prefix_len, page_size, max_pages_per_seq, n_pool_pages, max_suffix_len, blocks)
+        out = _vp()
+        _check(_lib.fka_plan_create_tree_paged(C.byref(h), C.byref(d), C.byref(out)))
+        plan = cls(out.value, True, h, n_branches * n_nodes)
+        plan._tree = (n_branches, n_nodes, n_q_heads, head_dim)
+        return plan
+
+    def _tree_shapes(self, q, masks):
+        if self._tree is None:
+            return  # refused by the call
+        if q.shape != self._tree or masks.shape != self._tree[:2]:
+            raise ValueError(f"q must be {list(self._tree)}, masks int64 {list(self._tree[:2])}, as the plan was made")
+
+    def tree_attend(self, q, prefix_k, prefix_v, suffix_k, suffix_v, suffix_len, masks, out, out_lse=None, stream=None):
+        """fka_tree_attend: q bf16 [N][n][Hq][d], masks int64 [N][n] (the bits of tree_layout) -> out fp32 [N][n][Hq][d]."""
+        self._tree_shapes(q, masks)
+        d = self.device
+        _check(_lib.fka_tree_attend(self._h, _p(q, "bf16", d), _p(prefix_k, "bf16", d), _p(prefix_v, "bf16", d),
+                                    _p(suffix_k, "bf16", d), _p(suffix_v, "bf16", d), _p(suffix_len, "i32", d), _p(masks, "i64", d),
+                                    _p(out, "f32", d), _p(out_lse, "f32", d), _stream(stream)))
+
+    def tree_attend_paged(self, q, k_pool, v_pool, page_table, suffix_len, masks, out, out_lse=None, stream=None):
+        """fka_tree_attend_paged: the same over the page pool."""
+        self._tree_shapes(q, masks)
+        d = self.device
+        _check(_lib.fka_tree_attend_paged(self._h, _p(q, "bf16", d), _p(k_pool, "bf16", d), _p(v_pool, "bf16", d),
+                                          _p(page_table, "i32", d), _p(suffix_len, "i32", d), _p(masks, "i64", d), _p(out, "f32", d),
+                                          _p(out_lse, "f32", d), _stream(stream)))
 
     @classmethod
     def mx_plan(cls, n_q_heads, n_kv_heads, head_dim, group_start, group_prefix_len, suffix_cap, max_suffix_len, *, n_pool_tiles,
@@ -682,6 +742,57 @@ def evict(k, v, weights, index, k_out, v_out, weights_out=None, *, n_first=0, n_
                           _p(k, "bf16", dev), _p(v, "bf16", dev), cap, _p(weights, "f32", dev), weights.shape[1],
                           _p(index, "i32", dev), _p(k_out, "bf16", dev), _p(v_out, "bf16", dev), _p(weights_out, "f32", dev),
                           _p(workspace, "u8", dev), workspace.numel(), _stream(stream)))
+
+
+def tree_layout(parents, base, masks, positions, *, err=None, stream=None):
+    """fka_tree_layout: parents int32 [N][n], base int32 [N] -> masks int64 [N][n] (bit j: the node reads node j), positions int32 [N][n]."""
+    if parents.dim() != 2 or masks.shape != parents.shape or positions.shape != parents.shape or base.shape != parents.shape[:1]:
+        raise ValueError("parents, masks and positions must be [N][n], base [N]")
+    dev = _on_current(parents)
+    N, n = parents.shape
+    _check(_lib.fka_tree_layout(N, n, _p(parents, "i32", dev), _p(base, "i32", dev), _p(masks, "i64", dev), _p(positions, "i32", dev),
+                                _p(err, "i32", dev), _stream(stream)))
+
+
+def _accept_tree(parents, masks, tokens, targets, path, count, next_token, suffix_len):
+    shape = parents.shape
+    if len(shape) != 2 or any(t.shape != shape for t in (masks, tokens, targets, path)):
+        raise ValueError("parents, masks, tokens, targets and path must be [N][n]")
+    if count.shape != shape[:1] or next_token.shape != shape[:1] or suffix_len.shape != shape[:1]:
+        raise ValueError("count, next_token and suffix_len must be [N]")
+    dev = _on_current(parents)
+    return (dev, (_p(parents, "i32", dev), _p(masks, "i64", dev), _p(tokens, "i32", dev), _p(targets, "i32", dev)),
+            (_p(path, "i32", dev), _p(count, "i32", dev), _p(next_token, "i32", dev)))
+
+
+def tree_accept(parents, masks, tokens, targets, suffix_k, suffix_v, suffix_len, path, count, next_token, *, max_len=None,
+                advance=True, err=None, stream=None):
+    """fka_tree_accept: the nodes that targets int32 [N][n] (chosen behind each node) confirm -> path int32 [N][n], count and
+    next_token int32 [N]; their rows of suffix_k / suffix_v bf16 [N][Hkv][cap][d] move behind suffix_len int32 [N]."""
+    dev, tree, result = _accept_tree(parents, masks, tokens, targets, path, count, next_token, suffix_len)
+    N, n = parents.shape
+    if suffix_k.dim() != 4 or suffix_k.shape[0] != N or suffix_v.shape != suffix_k.shape:
+        raise ValueError("suffix_k and suffix_v must be [N][Hkv][cap][d]")
+    _, Hkv, cap, d = suffix_k.shape
+    desc = AcceptDesc(N, n, Hkv, d, cap if max_len is None else max_len, 1 if advance else 0)
+    _check(_lib.fka_tree_accept(C.byref(desc), *tree, _p(suffix_k, "bf16", dev), _p(suffix_v, "bf16", dev), cap,
+                                _p(suffix_len, "i32", dev), *result, _p(err, "i32", dev), _stream(stream)))
+
+
+def tree_accept_paged(parents, masks, tokens, targets, k_pool, v_pool, page_table, prefix_len, suffix_len, path, count, next_token, *,
+                      max_len=None, advance=True, err=None, stream=None):
+    """fka_tree_accept_paged: as tree_accept, in the pages of page_table int32 [N][max_pages] behind prefix_len int32 [N]."""
+    dev, tree, result = _accept_tree(parents, masks, tokens, targets, path, count, next_token, suffix_len)
+    N, n = parents.shape
+    if k_pool.dim() != 4 or k_pool.shape[2] != 16 or v_pool.shape != k_pool.shape:
+        raise ValueError("k_pool and v_pool must be [pages][Hkv][16][d]")
+    if page_table.dim() != 2 or page_table.shape[0] != N or prefix_len.shape != (N,):
+        raise ValueError("page_table must have a row, prefix_len an entry per branch")
+    pages, Hkv, _, d = k_pool.shape
+    desc = AcceptDesc(N, n, Hkv, d, 16 * page_table.shape[1] if max_len is None else max_len, 1 if advance else 0)
+    _check(_lib.fka_tree_accept_paged(C.byref(desc), *tree, _p(k_pool, "bf16", dev), _p(v_pool, "bf16", dev), _p(page_table, "i32", dev),
+                                      _p(prefix_len, "i32", dev), page_table.shape[1], pages, _p(suffix_len, "i32", dev), *result,
+                                      _p(err, "i32", dev), _stream(stream)))
 
 
 def raw_call(name: str, *args) -> int:

@@ -1,0 +1,456 @@
+"""Drafted trees on the GPU: layout, attention and acceptance against plain implementations (attention in 64 bits)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def fa():
+    from paper_2608_13667_amd import forkattn
+    return forkattn
+
+
+def _i32(x):
+    return torch.tensor(np.asarray(x, np.int32), device="cuda")
+
+
+def _i64(masks):
+    return torch.from_numpy(np.asarray(masks, np.uint64).view(np.int64).copy()).cuda()
+
+
+def _parents(rng, n, unused=0.1, back=6):
+    used, out = [0], [-1]
+    for i in range(1, n):
+        if rng.random() < unused:
+            out.append(-1)
+        else:
+            out.append(int(rng.choice(used[-back:])))
+            used.append(i)
+    return out
+
+
+def _masks(parents):
+    m = []
+    for i, a in enumerate(parents):
+        m.append(1 << i | (m[a] if 0 <= a < i else 0))
+    return m
+
+
+# ------------------------------------------------------------------------------------------------- layout
+
+@pytest.mark.parametrize("N,n", [(1, 1), (1, 64), (5, 16), (7, 63), (513, 33)])
+def test_layout(fa, N, n):
+    rng = np.random.default_rng(N * 100 + n)
+    trees = [_parents(rng, n) for _ in range(N - 1)] + [[-1] + list(range(n - 1))]  # the last one a chain
+    base = rng.integers(0, 1 << 30, N)
+    masks = torch.full((N, n), -7, dtype=torch.int64, device="cuda")
+    pos = torch.full((N, n), -7, dtype=torch.int32, device="cuda")
+    err = _i32([0])
+    fa.tree_layout(_i32(trees), _i32(base), masks, pos, err=err)
+    want = np.array([_masks(t) for t in trees], np.uint64)
+    assert np.array_equal(masks.cpu().numpy().view(np.uint64), want)
+    depth = np.array([[bin(int(x)).count("1") - 1 for x in row] for row in want])
+    assert np.array_equal(pos.cpu().numpy(), base[:, None] + depth)
+    assert int(err) == 0
+
+
+def test_layout_flags_parents_that_are_not_before_their_node(fa):
+    for bad, n in (([-1, 0, 2, 1], 4), ([-1, 0, 3, 1], 4), ([0, 0], 2), ([-2], 1), ([-1, 2**31 - 1, -2**31], 3)):
+        masks, pos = torch.empty(2, n, dtype=torch.int64, device="cuda"), torch.empty(2, n, dtype=torch.int32, device="cuda")
+        err = _i32([0])
+        fa.tree_layout(_i32([[-1] * n, bad]), _i32([10, 20]), masks, pos, err=err)
+        assert int(err) == fa.ERR_BAD_TREE
+        good = [a if 0 <= a < i else -1 for i, a in enumerate(bad)]
+        assert masks[1].tolist() == _masks(good) and masks[0].tolist() == [1 << i for i in range(n)]
+        fa.tree_layout(_i32([[-1] * n, bad]), _i32([10, 20]), masks, pos)  # without a place for the flag
+
+
+# ---------------------------------------------------------------------------------------------- attention
+
+def _bf16(rng, *shape):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).bfloat16()
+
+
+class Tree:
+    """Inputs of one call on the CPU, the 64-bit result, and the call."""
+
+    def __init__(self, hq, hkv, d, n, prefix, suffix, masks, paged=False, seed=0, spare=3, scale=0.0, junk=float("nan")):
+        rng = np.random.default_rng(seed)
+        N = len(suffix)
+        self.hq, self.hkv, self.d, self.N, self.n, self.prefix, self.suffix, self.paged = hq, hkv, d, N, n, prefix, suffix, paged
+        self.scale, self.masks, self.cap = scale, masks, max(suffix) + n + spare
+        self.q = _bf16(rng, N, n, hq, d)
+        self.pk, self.pv = _bf16(rng, hkv, prefix, d), _bf16(rng, hkv, prefix, d)
+        self.sk, self.sv = _bf16(rng, N, hkv, self.cap, d), _bf16(rng, N, hkv, self.cap, d)
+        for b, length in enumerate(suffix):  # what is behind the nodes must not count
+            self.sk[b, :, length + n:] = junk
+            self.sv[b, :, length + n:] = junk
+        self.rng = rng
+
+    def want(self):
+        """out, lse, and what a result may be off by: tolerances of each from the sums' sizes."""
+        G, scale = self.hq // self.hkv, self.scale or 1 / math.sqrt(self.d)
+        out = np.zeros((self.N, self.n, self.hq, self.d))
+        lse = np.full((self.N, self.n, self.hq), -np.inf)
+        tol, tol_lse = np.zeros_like(out), np.zeros_like(lse)
+        to64 = lambda t: t.double().numpy()  # noqa: E731
+        q, pk, pv, sk, sv = (to64(t) for t in (self.q, self.pk, self.pv, self.sk, self.sv))
+        for b, length in enumerate(self.suffix):
+            for i in range(self.n):
+                see = list(range(length)) + [length + j for j in range(self.n) if int(self.masks[b][i]) >> j & 1]
+                for h in range(self.hq):
+                    g = h // G
+                    k, v = np.concatenate([pk[g], sk[b, g, see]]), np.concatenate([pv[g], sv[b, g, see]])
+                    if not len(k):
+                        continue
+                    with np.errstate(invalid="ignore"):
+                        s = k @ q[b, i, h] * scale
+                        m = s.max()
+                        p = np.exp(s - m)
+                        out[b, i, h] = p @ v / p.sum()
+                        lse[b, i, h] = m + np.log(p.sum())
+                        # a score: d exact products in steps of 32 and at most 32 roundings in each, relative to the sum of magnitudes,
+                        # and the argument of the exponential; then the exponential.  p is rounded in two bf16 terms (2^-8 squared),
+                        # the sums over keys take two steps for each 32 keys and a few in the merge.
+                        size = (np.abs(k) @ np.abs(q[b, i, h])).max() * scale
+                        rel = 2.0 ** -24 * (2 * ((32 + self.d / 32 + 8) * size + 4) + 2 * (len(k) / 16 + 64))
+                        tol[b, i, h] = (p @ np.abs(v) / p.sum()) * (2.0 ** -16 + rel)
+                        tol_lse[b, i, h] = rel + 2.0 ** -22 * abs(lse[b, i, h])
+        return out, lse, tol, tol_lse
+
+    def place(self):
+        """The call's tensors on the GPU."""
+        c = lambda t: t.cuda()  # noqa: E731
+        self.lens, self.dmasks, self.dq = _i32(self.suffix), _i64(self.masks), c(self.q)
+        self.out = torch.full((self.N, self.n, self.hq, self.d), float("nan"), device="cuda")
+        self.lse = torch.full((self.N, self.n, self.hq), float("nan"), device="cuda")
+        if not self.paged:
+            self.cache = [c(t) for t in (self.pk, self.pv, self.sk, self.sv)]
+            return
+        shared, each = -(-self.prefix // 16), -(-self.cap // 16)
+        pages = shared + self.N * each + 2
+        ids = self.rng.permutation(pages)
+        pools = []
+        for pre, suf in ((self.pk, self.sk), (self.pv, self.sv)):
+            pool = torch.full((pages, self.hkv, 16, self.d), float("nan"), dtype=torch.bfloat16)
+            for i in range(self.prefix):
+                pool[ids[i // 16], :, i % 16] = pre[:, i]
+            for b in range(self.N):
+                for u in range(self.cap):
+                    pool[ids[shared + b * each + u // 16], :, u % 16] = suf[b, :, u]
+            pools.append(c(pool))
+        table = np.array([np.concatenate([ids[:shared], ids[shared + b * each: shared + (b + 1) * each]]) for b in range(self.N)])
+        self.cache = pools + [_i32(table)]
+
+    def plan(self, fa, max_len=None, blocks=0):
+        top = self.cap if max_len is None else max_len
+        if self.paged:
+            return fa.Plan.tree_paged_plan(self.hq, self.hkv, self.d, self.N, self.n, self.prefix, self.cache[2].shape[1],
+                                           self.cache[0].shape[0], top, softmax_scale=self.scale, blocks=blocks)
+        return fa.Plan.tree_plan(self.hq, self.hkv, self.d, self.N, self.n, self.prefix, self.cap, top, softmax_scale=self.scale,
+                                 blocks=blocks)
+
+    def call(self, plan):
+        attend = plan.tree_attend_paged if self.paged else plan.tree_attend
+        attend(self.dq, *self.cache, self.lens, self.dmasks, self.out, self.lse)
+
+
+def _close(t, want):
+    out, lse, tol, tol_lse = want
+    got, got_lse = t.out.double().cpu().numpy(), t.lse.double().cpu().numpy()
+    empty = np.isneginf(lse)
+    assert np.array_equal(np.isneginf(got_lse), empty)
+    assert (got[empty] == 0).all()
+    assert (np.abs(got - out) <= tol).all(), f"worst {np.max(np.abs(got - out) / np.maximum(tol, 1e-300))} of the tolerance"
+    assert (np.abs(got_lse[~empty] - lse[~empty]) <= tol_lse[~empty]).all()
+
+
+def _trees(seed, N, n):
+    rng = np.random.default_rng(seed)
+    return [_masks(_parents(rng, n)) for _ in range(N)]
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("hq,hkv,d,n,prefix,suffix", [
+    (8, 2, 64, 8, 70, [0, 5, 64, 17, 1]),
+    (10, 2, 128, 16, 129, [0, 40, 7]),
+    (4, 4, 128, 1, 200, [3, 0, 130]),        # nothing drafted, one query head per KV head
+    (5, 1, 128, 64, 33, [9, 70]),            # the largest tree
+    (7, 1, 64, 63, 0, [0, 1, 15, 16, 65]),   # no prefix
+    (64, 1, 128, 3, 65, [31, 2]),            # a wide group
+    (2, 2, 64, 13, 300, [700]),              # a long suffix
+    (3, 3, 128, 1, 0, [0, 1]),               # the root alone
+], ids=str)
+def test_attend(fa, hq, hkv, d, n, prefix, suffix, paged):
+    t = Tree(hq, hkv, d, n, prefix, suffix, _trees(n, len(suffix), n), paged, seed=n + prefix)
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    _close(t, t.want())
+    assert plan.device_error() == 0
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+def test_attend_over_a_long_prefix(fa, paged):
+    """Several ranges of whole tiles; the 64-bit result over one head's rows of a few nodes."""
+    t = Tree(10, 2, 128, 9, 5000 + 13, [100, 0, 33], _trees(3, 3, 9), paged, seed=5)
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    _close(t, t.want())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_any_set_of_nodes(fa, d):
+    """Masks that no tree gives: nothing, later nodes, not the node itself, bits past the nodes."""
+    n = 12
+    rng = np.random.default_rng(d)
+    masks = [[int(rng.integers(0, 1 << 63)) for _ in range(n)] for _ in range(3)]
+    masks[0][:4] = [0, 1 << 11, (1 << 64) - 1, 0xfffffffffffff000]
+    t = Tree(6, 2, d, n, 0, [0, 3, 40], masks, seed=d)
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    want = t.want()
+    assert np.isneginf(want[1][0, 0]).all() and np.isneginf(want[1][0, 3]).all()  # bits past the nodes count as none
+    _close(t, want)
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")], ids=str)
+def test_attend_what_no_bit_shows_has_no_influence(fa, value, paged):
+    n, hidden = 10, 6
+    masks = [[m & ~(1 << hidden) for m in row] for row in _trees(1, 3, n)]
+    t = Tree(8, 2, 128, n, 90, [20, 0, 50], masks, paged, seed=1, junk=value)
+    for b, length in enumerate(t.suffix):
+        t.sk[b, :, length + hidden] = value
+        t.sv[b, :, length + hidden] = value
+    t.place()
+    t.call(t.plan(fa))
+    t.sk.nan_to_num_(0, 0, 0), t.sv.nan_to_num_(0, 0, 0)
+    _close(t, t.want())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_a_nan_value_reaches_the_rows_that_read_it(fa, d):
+    n, bad = 11, 4
+    masks = _trees(2, 3, n)
+    t = Tree(8, 2, d, n, 77, [5, 30, 0], masks, seed=2)
+    t.sv[1, 0, 30 + bad, 3] = float("nan")
+    t.place()
+    t.call(t.plan(fa))
+    got = t.out.cpu()
+    t.sv[1, 0, 30 + bad, 3] = 0
+    out, _, tol, _ = t.want()
+    reads = np.array([[b == 1 and masks[b][i] >> bad & 1 for i in range(n)] for b in range(3)], bool)
+    assert reads.any() and not reads[1].all()
+    hit = torch.isnan(got).all(-1).numpy()
+    assert hit[:, :, :4][reads].all() and not hit[:, :, 4:].any() and not hit[:, :, :4][~reads].any()
+    rest = ~hit
+    assert (np.abs(got.double().numpy() - out)[rest] <= tol[rest]).all()
+
+
+def test_attend_a_chain_is_the_prefill(fa):
+    n = 12
+    t = Tree(10, 2, 128, n, 700, [30, 4, 0, 90], [[(2 << i) - 1 for i in range(n)]] * 4, seed=9)
+    t.place()
+    t.call(t.plan(fa))
+    p = fa.Plan.prefill_plan(t.hq, t.hkv, t.d, t.N, n, t.prefix, t.cap, t.cap)
+    out = torch.empty_like(t.out)
+    p.prefill(t.dq, *t.cache, t.lens, out)
+    want = t.want()
+    _close(t, want)
+    assert (np.abs(out.double().cpu().numpy() - want[0]) <= want[2]).all()
+
+
+def test_attend_repeats_and_graphs(fa):
+    """The same bits every time, also from a captured graph replayed between eager calls on changed lengths and masks."""
+    t = Tree(10, 2, 128, 16, 900, [30, 64, 0], _trees(4, 3, 16), seed=4)
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    first = t.out.clone(), t.lse.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        t.call(plan)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        t.call(plan)
+    other_masks = _i64(_trees(5, 3, 16))
+    keep_masks, keep_lens = t.dmasks.clone(), t.lens.clone()
+    for _ in range(3):
+        t.dmasks.copy_(other_masks)
+        t.lens.copy_(_i32([1, 2, 3]))
+        t.call(plan)
+        second = t.out.clone()
+        t.out.fill_(float("nan"))
+        graph.replay()
+        assert torch.equal(t.out.view(torch.int32), second.view(torch.int32))  # (one branch now reads rows that hold NaN)
+        t.dmasks.copy_(keep_masks)
+        t.lens.copy_(keep_lens)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(t.out, first[0]) and torch.equal(t.lse, first[1])
+        assert not torch.equal(second, first[0])
+
+
+def test_attend_flags_what_the_device_holds(fa):
+    t = Tree(8, 2, 64, 4, 20, [10, 50], _trees(1, 2, 4), seed=3)
+    t.place()
+    plan = t.plan(fa, max_len=30 + 4)  # 50 is clamped to 30
+    t.call(plan)
+    assert plan.device_error() == fa.ERR_SUFFIX_CLAMPED
+    t = Tree(8, 2, 64, 4, 20, [10, 20], _trees(1, 2, 4), paged=True, seed=3)
+    t.place()
+    plan = t.plan(fa)
+    t.cache[2][1, -1] = 10 ** 6  # the last page of the second row: positions past the nodes
+    last = (20 + 4 - 1) // 16
+    t.cache[2][1, 2 + last] = -5
+    t.call(plan)
+    torch.cuda.synchronize()
+    assert plan.device_error() == fa.ERR_BAD_PAGE
+
+
+@pytest.mark.parametrize("blocks", [1, 7, 1000])
+def test_attend_any_grid(fa, blocks):
+    t = Tree(8, 2, 128, 5, 700, [30, 200], _trees(6, 2, 5), seed=6)
+    t.place()
+    t.call(t.plan(fa, blocks=blocks))
+    _close(t, t.want())
+
+
+def test_attend_scale_and_more_than_64_branches(fa):
+    t = Tree(2, 1, 64, 3, 40, [i % 7 for i in range(70)], _trees(8, 70, 3), seed=8, scale=0.3)
+    t.place()
+    t.call(t.plan(fa))
+    _close(t, t.want())
+
+
+# ------------------------------------------------------------------------------------------------- accept
+
+def _accept(parents, masks, tokens, targets):
+    """The accepted nodes of one tree, and the token behind the last."""
+    n = len(parents)
+    right = {0}
+    for i in range(1, n):
+        a = parents[i]
+        if 0 <= a < i and tokens[i] == targets[a] and not any(parents[j] == a and tokens[j] == tokens[i] for j in range(1, i)):
+            right.add(i)
+    path = [i for i in range(n) if i == 0 or all(j in right for j in range(n) if (masks[i] | 1 << i) >> j & 1)]
+    return path, targets[path[-1]]
+
+
+def _accept_case(rng, N, n, likely, words=50):
+    trees = [_parents(rng, n) for _ in range(N)]
+    targets = rng.integers(0, words, (N, n))
+    tokens = rng.integers(0, words, (N, n))
+    for b in range(N):
+        for i in range(1, n):
+            if trees[b][i] >= 0 and rng.random() < likely:
+                tokens[b, i] = targets[b, trees[b][i]]
+    return trees, tokens, targets
+
+
+@pytest.mark.parametrize("advance", [False, True])
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("hkv,d,N,n,likely", [(2, 64, 5, 8, 0.5), (8, 128, 3, 16, 0.8), (1, 128, 4, 1, 0.5), (3, 64, 2, 64, 0.97),
+                                              (20, 128, 2, 64, 1.0), (1, 64, 70, 5, 0.3)], ids=str)
+def test_accept(fa, hkv, d, N, n, likely, paged, advance):
+    rng = np.random.default_rng(n + N)
+    trees, tokens, targets = _accept_case(rng, N, n, likely)
+    masks = [_masks(t) for t in trees]
+    lens = rng.integers(0, 60, N)
+    cap = int(lens.max()) + n + 2
+    prefix = rng.integers(0, 40, N)
+    path, count, nxt = (torch.full(s, -9, dtype=torch.int32, device="cuda") for s in ((N, n), (N,), (N,)))
+    dlens, err = _i32(lens), _i32([0])
+    args = (_i32(trees), _i64(masks), _i32(tokens), _i32(targets))
+    bits = lambda *s: torch.randint(-2**15, 2**15, s, dtype=torch.int16)  # noqa: E731  (NaN patterns among them)
+    if paged:
+        first, each = -(-prefix // 16), -(-cap // 16)
+        width = int(first.max()) + each
+        ids = rng.permutation(N * width + 3)[: N * width].reshape(N, width)
+        k, v = bits(N * width + 3, hkv, 16, d), bits(N * width + 3, hkv, 16, d)
+        row = lambda c, b, u: c[ids[b, first[b] + u // 16], :, u % 16]  # noqa: E731
+    else:
+        k, v = bits(N, hkv, cap, d), bits(N, hkv, cap, d)
+        row = lambda c, b, u: c[b, :, u]  # noqa: E731
+    dk, dv = (x.cuda().view(torch.bfloat16) for x in (k, v))
+    if paged:
+        fa.tree_accept_paged(*args, dk, dv, _i32(ids), _i32(prefix), dlens, path, count, nxt, max_len=cap, advance=advance, err=err)
+    else:
+        fa.tree_accept(*args, dk, dv, dlens, path, count, nxt, advance=advance, err=err)
+    moved = 0
+    for b in range(N):
+        want, behind = _accept(trees[b], masks[b], tokens[b], targets[b])
+        assert path[b].tolist() == want + [-1] * (n - len(want))
+        assert int(count[b]) == len(want) and int(nxt[b]) == behind
+        assert int(dlens[b]) == lens[b] + (len(want) if advance else 0)
+        for j, i in enumerate(want):
+            for c in (k, v):
+                row(c, b, int(lens[b]) + j)[...] = row(c, b, int(lens[b]) + i).clone()
+            moved += i != j
+    assert n == 1 or moved or likely < 0.4
+    assert torch.equal(dk.view(torch.int16).cpu(), k) and torch.equal(dv.view(torch.int16).cpu(), v)
+    assert int(err) == 0
+
+
+def test_accept_takes_the_first_of_two_equal_children_and_no_child_of_an_unused_node(fa):
+    parents = [[-1, 0, 0, 1, 2, -1, 5, 3, 3], [-1, -1, 0, 0, 2, 3, -1, 6, 5]]
+    tokens = [[0, 7, 7, 8, 8, 7, 1, 9, 9], [0, 4, 4, 5, 1, 2, 9, 9, 3]]
+    targets = [[7, 8, 8, 9, 1, 1, 1, 6, 6], [5, 1, 1, 2, 1, 3, 9, 1, 77]]
+    masks = [_masks(p) for p in parents]
+    k = torch.zeros(2, 1, 20, 64, dtype=torch.bfloat16, device="cuda")
+    path, count, nxt, lens = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((2, 9), (2,), (2,), (2,)))
+    fa.tree_accept(_i32(parents), _i64(masks), _i32(tokens), _i32(targets), k, k.clone(), lens, path, count, nxt)
+    assert path.tolist() == [[0, 1, 3, 7] + [-1] * 5, [0, 3, 5, 8] + [-1] * 5]
+    assert nxt.tolist() == [6, 77] and lens.tolist() == [4, 4]
+
+
+def test_accept_without_room_or_pages(fa):
+    n, N = 4, 4
+    trees, tokens, targets = [[-1, 0, 1, 2]] * N, [[5, 6, 7, 8]] * N, [[6, 7, 8, 9]] * N
+    args = (_i32(trees), _i64([_masks(t) for t in trees]), _i32(tokens), _i32(targets))
+    new = lambda: tuple(torch.full(s, -9, dtype=torch.int32, device="cuda") for s in ((N, n), (N,), (N,)))  # noqa: E731
+    k = torch.arange(N * 20 * 64, device="cuda").view(N, 1, 20, 64).bfloat16()
+    v, before = k.clone(), k.clone()
+    path, count, nxt = new()
+    lens, err = _i32([16, 17, -1, 2**31 - 1]), _i32([0])
+    fa.tree_accept(*args, k, v, lens, path, count, nxt, err=err)
+    assert count.tolist() == [4, 0, 0, 0] and nxt.tolist() == [9, -1, -1, -1] and path[1:].eq(-1).all()
+    assert lens.tolist() == [20, 17, -1, 2**31 - 1] and int(err) == fa.ERR_APPEND_NO_ROOM and torch.equal(k, before)
+    # pages: one past the pool, one negative, one past the table
+    pool = torch.zeros(4, 1, 16, 64, dtype=torch.bfloat16, device="cuda")
+    path, count, nxt = new()
+    lens, err = _i32([14, 14, 14, 30]), _i32([0])
+    table = _i32([[0, 1], [0, 4], [-1, 2], [2, 3]])
+    fa.tree_accept_paged(*args, pool, pool.clone(), table, _i32([0] * N), lens, path, count, nxt, max_len=1000, err=err)
+    assert count.tolist() == [4, 0, 0, 0] and lens.tolist() == [18, 14, 14, 30] and int(err) == fa.ERR_APPEND_NO_ROOM
+
+
+def test_accept_from_a_graph(fa):
+    rng = np.random.default_rng(1)
+    trees, tokens, targets = _accept_case(rng, 3, 16, 0.9)
+    args = (_i32(trees), _i64([_masks(t) for t in trees]), _i32(tokens), _i32(targets))
+    k = torch.randn(3, 2, 100, 128, device="cuda").bfloat16()
+    v, lens = k.clone(), _i32([0, 7, 20])
+    path, count, nxt = (torch.zeros(s, dtype=torch.int32, device="cuda") for s in ((3, 16), (3,), (3,)))
+    state = (k, v, lens)
+    start = [x.clone() for x in state]
+    fa.tree_accept(*args, k, v, lens, path, count, nxt)
+    want = [x.clone() for x in state + (path, count, nxt)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fa.tree_accept(*args, k, v, lens, path, count, nxt)
+    for _ in range(3):
+        for x, y in zip(state, start):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(state + (path, count, nxt), want))
