@@ -449,6 +449,41 @@ fka_status fka_tree_attend_paged(const fka_plan *plan, const void *q, const void
                                  const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse, void *stream);
 
 typedef struct {
+    int32_t n_rows;        /* rows of logits, >= 0: the branches of a step, or the nodes of its trees; at most 2^20 */
+    int32_t n_vocab;       /* logits of a row, in [1, 2^18] */
+    int32_t logits_bf16;   /* 1: bf16, 0: fp32 */
+    int64_t logits_stride; /* elements from one row to the next, >= n_vocab (any: rows need not be aligned) */
+} fka_sample_desc;
+
+/* Device bytes of fka_sample's workspace (0 for sizes that it refuses). */
+size_t fka_sample_bytes(int32_t n_rows, int32_t n_vocab);
+
+/*
+ * The token that each row of logits gives for a random number.  With M the row's largest logit and t its temperature, logit l has the weight
+ * w = round(2^44 exp((l - M) / t)).  In the order of falling logits, equal ones by place (-0 equals 0), are kept
+ *   top-k  the first k of them (k <= 0 or k >= n_vocab: all)
+ *   top-p  of those, the ones with less than p of their sum in front of them, the first in any case (p >= 1 or NaN: all)
+ *   min-p  of those, the ones with w >= min_p 2^44 (min_p <= 0 or NaN: all; more than 1 counts as 1)
+ * and the token is the first place, in the order of the vocabulary, up to which the kept weights sum to more than floor(u S), S their
+ * sum.  The products and comparisons of sums with p and u are in fp64.
+ * A temperature of 0 (or less, or NaN) chooses the first of the largest logits.  A NaN logit counts as -inf, which is never chosen; beside a logit of +inf
+ * the others have no weight.  A row without any logit above -inf gets the token -1 and bit 32 in *err.
+ *   logits                     [n_rows] rows of n_vocab
+ *   temperature, top_p, min_p  fp32 [n_rows] (device) or NULL: 1, 1 and 0 for all;  top_k int32 [n_rows] or NULL
+ *   u                          fp32 [n_rows] (device), in [0, 1); a value outside counts as the nearest within, NaN as 0
+ *   tokens                     int32 [n_rows]
+ *   logprob                    fp32 [n_rows] or NULL: ln(w / S) of the token (0 at temperature 0, -inf for the token -1)
+ *   err                        int32 (device) or NULL
+ *   workspace                  fka_sample_bytes(n_rows, n_vocab) device bytes (16-byte aligned), used by one call at a time; its contents before
+ *                              and after do not matter
+ * What is written, the workspace too, may overlap neither itself nor what is read (FKA_ERR_INVALID_ARG).  FKA_ERR_UNSUPPORTED for more than
+ * 2^18 logits or 2^20 rows.  The same call gives the same bits.
+ */
+fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, const float *u, int32_t *tokens, float *logprob, int32_t *err,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+typedef struct {
     int32_t n_branches; /* N >= 1, at most 2^20 */
     int32_t n_nodes;    /* n in [1, 64] */
     int32_t n_kv_heads;

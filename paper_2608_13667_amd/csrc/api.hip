@@ -2443,4 +2443,65 @@ fka_status fka_tree_accept_paged(const fka_accept_desc *desc, const int32_t *par
                       stream);
 }
 
+size_t fka_sample_bytes(int32_t n_rows, int32_t n_vocab)
+{
+    if (n_rows < 0 || n_rows > kMaxTrees || n_vocab < 1 || n_vocab > fka::kMaxVocab) return 0;  // as fka_sample
+    return 16;
+}
+
+fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const float *temperature, const int32_t *top_k,
+                      const float *top_p, const float *min_p, const float *u, int32_t *tokens, float *logprob, int32_t *err,
+                      void *workspace, size_t workspace_bytes, void *stream)
+{
+    REQUIRE(desc != nullptr, "desc is null");
+    REQUIRE(desc->n_rows >= 0 && desc->n_vocab >= 1, "n_rows (%d) must be >= 0, n_vocab (%d) >= 1", desc->n_rows, desc->n_vocab);
+    REQUIRE(desc->logits_bf16 == 0 || desc->logits_bf16 == 1, "logits_bf16 must be 0 or 1");
+    if (desc->n_vocab > fka::kMaxVocab)
+        return fail(FKA_ERR_UNSUPPORTED, "%d logits to a row exceed the limit of %d", desc->n_vocab, fka::kMaxVocab);
+    if (desc->n_rows > kMaxTrees) return fail(FKA_ERR_UNSUPPORTED, "%d rows exceed the limit of %d", desc->n_rows, kMaxTrees);
+    REQUIRE(desc->logits_stride >= desc->n_vocab, "logits_stride (%lld) is less than n_vocab (%d)", (long long)desc->logits_stride,
+            desc->n_vocab);
+    if (desc->n_rows == 0) return ok();
+    REQUIRE(logits != nullptr, "logits is null");
+    const size_t R = desc->n_rows, size = desc->logits_bf16 ? 2 : 4;
+    REQUIRE((reinterpret_cast<uintptr_t>(logits) & (size - 1)) == 0, "logits is not %zu-byte aligned", size);
+    REQUIRE_OPT4(temperature);
+    REQUIRE_OPT4(top_k);
+    REQUIRE_OPT4(top_p);
+    REQUIRE_OPT4(min_p);
+    REQUIRE_PTR4(u);
+    REQUIRE_PTR4(tokens);
+    REQUIRE_OPT4(logprob);
+    REQUIRE_OPT4(err);
+    REQUIRE_PTR16(workspace);
+    const size_t need = fka_sample_bytes(desc->n_rows, desc->n_vocab);
+    REQUIRE(workspace_bytes >= need, "workspace of %zu bytes, %zu are needed", workspace_bytes, need);
+    const fka_status st = check_apart({{workspace, need, "workspace"}, {tokens, R * 4, "tokens"}, {logprob, R * 4, "logprob"}},
+                                      {{logits, desc->n_vocab * size, "logits", R, (size_t)desc->logits_stride * size},
+                                       {temperature, R * 4, "temperature"},
+                                       {top_k, R * 4, "top_k"},
+                                       {top_p, R * 4, "top_p"},
+                                       {min_p, R * 4, "min_p"},
+                                       {u, R * 4, "u"},
+                                       {err, 4, "err"}});
+    if (st != FKA_OK) return st;
+    fka::SampleArgs a{};
+    a.logits = logits;
+    a.stride = desc->logits_stride;
+    a.bf16 = desc->logits_bf16;
+    a.n_rows = desc->n_rows;
+    a.n_vocab = desc->n_vocab;
+    a.temperature = temperature;
+    a.top_k = top_k;
+    a.top_p = top_p;
+    a.min_p = min_p;
+    a.u = u;
+    a.tokens = tokens;
+    a.logprob = logprob;
+    a.err = err;
+    const hipError_t e = fka::launch_sample(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "sample kernel launch");
+    return ok();
+}
+
 }  // extern "C"

@@ -495,12 +495,28 @@ struct AcceptArgs {
     int32_t *err;                    // nullable
 };
 
+// The token that a row of logits gives (sample.h).
+struct SampleArgs {
+    const void *logits;      // [rows] of n_vocab fp32 or bf16, `stride` elements apart
+    int64_t stride;
+    int32_t bf16;
+    int32_t n_rows, n_vocab;
+    const float *temperature, *top_p, *min_p;  // [rows], each nullable
+    const int32_t *top_k;                      // [rows], nullable
+    const float *u;                            // [rows]
+    int32_t *tokens;                           // [rows]
+    float *logprob;                            // [rows], nullable
+    int32_t *err;                              // nullable
+};
+constexpr int kMaxVocab = 1 << 18;
+
 // error-flag bits (device)
 constexpr int32_t kErrSuffixClamped = 1;
 constexpr int32_t kErrAppendNoRoom = 2;
 constexpr int32_t kErrBadPage = 4;
 constexpr int32_t kErrBadSchedule = 8;
 constexpr int32_t kErrBadTree = 16;
+constexpr int32_t kErrNoToken = 32;
 
 hipError_t launch_partials(const AttnArgs &a, int n_blocks, int head_dim, int row_tiles, hipStream_t s);
 // Resident blocks per compute unit of the partial kernel for this shape (0 on error).
@@ -537,6 +553,7 @@ hipError_t launch_key_weights(const WeightsArgs &a, int head_dim, hipStream_t s)
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s);
 hipError_t launch_tree_layout(const LayoutArgs &a, hipStream_t s);
 hipError_t launch_tree_accept(const AcceptArgs &a, int head_dim, hipStream_t s);
+hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
 hipError_t launch_read_probe(const void *buf, size_t bytes, int blocks, int threads, int unroll, uint32_t *sink,
                              hipStream_t s);
 

@@ -5,13 +5,14 @@
 // append_kernel / gather_kernel: suffix append and paged gather (data movement).
 // The operators around a snapshot's cache are in headers of their own: rotate.h (norm, rotation and store of new
 // tokens), mx_tiles.h (4-bit tiles), mx_attend.h (decode over them), evict.h (key weights, shortening); tree.h has the layout and the
-// acceptance of drafted trees (their attention is in prefill.hip, sampling in sample.hip).
+// acceptance of drafted trees (their attention is in prefill.hip), sample.h the choice of tokens.
 #include "evict.h"
 #include "internal.h"
 #include "merge_row.h"
 #include "mx_attend.h"
 #include "mx_tiles.h"
 #include "rotate.h"
+#include "sample.h"
 #include "tree.h"
 
 namespace fka {
@@ -420,6 +421,8 @@ hipError_t launch_mx_partials(const MxArgs &a, int n_jobs, int head_dim, int row
 hipError_t launch_key_weights(const WeightsArgs &a, int head_dim, hipStream_t s) { return launch_key_weights_kernel(a, head_dim, s); }
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s) { return launch_evict_kernels(a, s); }
+
+hipError_t launch_sample(const SampleArgs &a, hipStream_t s) { return launch_sample_kernels(a, s); }
 
 hipError_t launch_tree_layout(const LayoutArgs &a, hipStream_t s) { return launch_tree_layout_kernel(a, s); }
 

@@ -22,7 +22,7 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 FKA_OK, FKA_ERR_INVALID_ARG, FKA_ERR_UNSUPPORTED, FKA_ERR_HIP, FKA_ERR_NOMEM = 0, -1, -2, -3, -4
-ERR_SUFFIX_CLAMPED, ERR_APPEND_NO_ROOM, ERR_BAD_PAGE, ERR_BAD_SCHEDULE, ERR_BAD_TREE = 1, 2, 4, 8, 16
+ERR_SUFFIX_CLAMPED, ERR_APPEND_NO_ROOM, ERR_BAD_PAGE, ERR_BAD_SCHEDULE, ERR_BAD_TREE, ERR_NO_TOKEN = 1, 2, 4, 8, 16, 32
 
 
 class Heads(C.Structure):
@@ -83,6 +83,10 @@ class AcceptDesc(C.Structure):
                 ("max_len", C.c_int32), ("advance", C.c_int32)]
 
 
+class SampleDesc(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("n_vocab", C.c_int32), ("logits_bf16", C.c_int32), ("logits_stride", C.c_int64)]
+
+
 MX_TILE = 128  # tokens of a 4-bit tile
 
 _vp = C.c_void_p
@@ -141,6 +145,8 @@ _sig = {
     "fka_plan_create_tree_paged": ([C.POINTER(Heads), C.POINTER(PrefillPagedDesc), C.POINTER(_vp)], C.c_int),
     "fka_tree_attend": ([_vp] * 11, C.c_int),
     "fka_tree_attend_paged": ([_vp] * 10, C.c_int),
+    "fka_sample_bytes": ([C.c_int32, C.c_int32], C.c_size_t),
+    "fka_sample": ([C.POINTER(SampleDesc)] + [_vp] * 10 + [C.c_size_t, _vp], C.c_int),
     "fka_tree_accept": ([C.POINTER(AcceptDesc)] + [_vp] * 6 + [C.c_int32] + [_vp] * 6, C.c_int),
     "fka_tree_accept_paged": ([C.POINTER(AcceptDesc)] + [_vp] * 8 + [C.c_int32, C.c_int32] + [_vp] * 6, C.c_int),
     "fka_evict_bytes": ([C.c_int32, C.c_int32], C.c_size_t),
@@ -752,6 +758,27 @@ def tree_layout(parents, base, masks, positions, *, err=None, stream=None):
     N, n = parents.shape
     _check(_lib.fka_tree_layout(N, n, _p(parents, "i32", dev), _p(base, "i32", dev), _p(masks, "i64", dev), _p(positions, "i32", dev),
                                 _p(err, "i32", dev), _stream(stream)))
+
+
+def sample_workspace(n_rows, n_vocab, device="cuda"):
+    """A workspace for sample over up to n_rows rows of n_vocab logits."""
+    return torch.empty(_lib.fka_sample_bytes(n_rows, n_vocab), dtype=torch.uint8, device=device)
+
+
+def sample(logits, u, tokens, logprob=None, *, temperature=None, top_k=None, top_p=None, min_p=None, workspace, err=None, stream=None):
+    """fka_sample: logits fp32 or bf16 [R][V] (rows any stride apart), u fp32 [R] -> tokens int32 [R], logprob fp32 [R]."""
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("logits must be fp32 or bf16 [R][V]")
+    R, V = logits.shape
+    if V > 1 and logits.stride(1) != 1:
+        raise ValueError("the logits of a row must be dense")
+    if any(t is not None and t.shape != (R,) for t in (u, tokens, logprob, temperature, top_k, top_p, min_p)):
+        raise ValueError("u, tokens, logprob, temperature, top_k, top_p and min_p must be [R]")
+    dev = _on_current(logits)
+    desc = SampleDesc(R, V, 1 if logits.dtype is torch.bfloat16 else 0, logits.stride(0) if R > 1 else V)
+    _check(_lib.fka_sample(C.byref(desc), logits.data_ptr(), _p(temperature, "f32", dev), _p(top_k, "i32", dev), _p(top_p, "f32", dev),
+                           _p(min_p, "f32", dev), _p(u, "f32", dev), _p(tokens, "i32", dev), _p(logprob, "f32", dev), _p(err, "i32", dev),
+                           _p(workspace, "u8", dev), workspace.numel(), _stream(stream)))
 
 
 def _accept_tree(parents, masks, tokens, targets, path, count, next_token, suffix_len):

@@ -1,0 +1,222 @@
+"""The choice of tokens on the GPU against its definition in whole numbers and fp64 on the CPU.  A weight may differ from the
+definition's by a unit of 2^-44 (the last bit of an exponential), so a token could only differ where u falls within some
+units of a border: the cases' numbers do not.  A logprob is a quotient of whole numbers, its logarithm in fp64, rounded to fp32."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+UNIT = 2.0 ** 44
+
+
+@pytest.fixture(scope="module")
+def fa():
+    from paper_2608_13667_amd import forkattn
+    return forkattn
+
+
+def _definition(x, t, k, p, m, u):
+    """Token and logprob of one row of fp32 values."""
+    x = np.where(np.isnan(x), -np.inf, x.astype(np.float64)) + 0.0
+    n, top = len(x), x.max()
+    if top == -np.inf:
+        return -1, -math.inf
+    if not t > 0:
+        return int(np.argmax(x)), 0.0
+    with np.errstate(invalid="ignore", over="ignore"):
+        w = np.rint(UNIT * np.exp((x - top) / np.float64(t)))
+    w[(x == -np.inf) | (top == np.inf)] = 0
+    w[x == top] = UNIT
+    w = [int(v) for v in w]
+    order = sorted(range(n), key=lambda i: (-x[i], i))
+    if 0 < k < n:
+        order = order[:k]
+    if p < 1:
+        total, front, kept = sum(w[i] for i in order), 0, []
+        for i in order:
+            if kept and not float(front) < float(np.float64(p) * np.float64(total)):
+                break
+            kept.append(i)
+            front += w[i]
+        order = kept
+    least = min(float(m), 1.0) * UNIT if m > 0 else 0.0
+    kept = sorted(i for i in order if float(w[i]) >= least)
+    total = sum(w[i] for i in kept)
+    mark = min(int(math.floor((float(u) if u > 0 else 0.0) * float(total))), total - 1) if not u == math.inf else total - 1
+    front = 0
+    for i in kept:
+        front += w[i]
+        if front > mark:
+            return i, math.log(w[i] / total)
+    raise AssertionError
+
+
+def _check(fa, logits, t, k, p, m, u, flag=0):
+    """logits: fp32 or bf16 [R][V] on the CPU, or any view of them on the GPU; the others arrays [R] or None."""
+    R, V = logits.shape
+    dev = logits.cuda()
+    f32 = lambda a: None if a is None else torch.tensor(np.asarray(a, np.float32), device="cuda")  # noqa: E731
+    i32 = lambda a: None if a is None else torch.tensor(np.asarray(a, np.int32), device="cuda")  # noqa: E731
+    tokens = torch.full((R,), -9, dtype=torch.int32, device="cuda")
+    logprob, err = torch.full((R,), float("nan"), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    work = fa.sample_workspace(R, V)
+    work.fill_(255)
+    fa.sample(dev, f32(u), tokens, logprob, temperature=f32(t), top_k=i32(k), top_p=f32(p), min_p=f32(m), workspace=work, err=err)
+    got, got_lp = tokens.tolist(), logprob.tolist()
+    x = logits.float().cpu().numpy()
+    pick = lambda a, r, d: d if a is None else np.float32(a[r])  # noqa: E731
+    for r in range(R):
+        args = (pick(t, r, 1.0), 0 if k is None else int(k[r]), pick(p, r, 1.0), 0.0 if m is None else np.float32(m[r]), np.float32(u[r]))
+        want, lp = _definition(x[r], *args)
+        assert got[r] == want, (r, args, got[r], want)
+        assert got_lp[r] == lp or abs(got_lp[r] - lp) <= 2.0 ** -24 * abs(lp) + 2.0 ** -40, (r, args, got_lp[r], lp)
+    assert int(err) == flag
+    return dev, tokens, work
+
+
+def _logits(rng, R, V, bf16, spread=2.5):
+    x = rng.standard_normal((R, V)) * spread
+    for r in range(R):
+        at = rng.integers(0, V, 20)
+        x[r, at] += 6 + 3 * rng.standard_normal(20)
+    x = torch.from_numpy(x.astype(np.float32))
+    return x.bfloat16() if bf16 else x
+
+
+GRID = [(t, k, p, m) for t in (0.0, 0.35, 1.0, 3.0) for k in (0, 1, 7, 300, 10**6) for p in (1.0, 0.3, 0.95, 0.0) for m in (0.0, 0.05)]
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 63, 64, 1000, 4097, 8192, 33333])
+def test_every_filter(fa, V, bf16):
+    rng = np.random.default_rng(V)
+    R = len(GRID)
+    t, k, p, m = (np.array(c) for c in zip(*GRID))
+    _check(fa, _logits(rng, R, V, bf16), t, k, p, m, rng.random(R))
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V", [131072, 200003, 262144])
+def test_large_vocabularies(fa, V, bf16):
+    rng = np.random.default_rng(V)
+    picks = [(1.0, 0, 1.0, 0.0), (0.8, 50, 0.9, 0.0), (1.0, 0, 0.9, 0.0), (1.5, 5000, 0.99, 0.01), (0.7, 0, 1.0, 0.02), (1.3, 40000, 1.0, 0.0),
+             (0.0, 3, 0.5, 0.5)]
+    t, k, p, m = (np.array(c) for c in zip(*picks))
+    _check(fa, _logits(rng, len(picks), V, bf16), t, k, p, m, rng.random(len(picks)))
+
+
+def test_nothing_given_and_no_logprob(fa):
+    rng = np.random.default_rng(0)
+    x = _logits(rng, 9, 5000, False)
+    u = rng.random(9)
+    _, tokens, work = _check(fa, x, None, None, None, None, u)
+    again = torch.empty_like(tokens)
+    fa.sample(x.cuda(), torch.tensor(u, dtype=torch.float32, device="cuda"), again, workspace=work)
+    assert torch.equal(tokens, again)
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_equal_logits(fa, bf16):
+    """All equal, a few values only, and the top of the order all ties: the lowest places are kept."""
+    R, V = 60, 9000
+    rng = np.random.default_rng(1)
+    x = np.zeros((R, V), np.float32)
+    x[20:40] = rng.integers(0, 4, (20, V))
+    x[40:] = np.where(rng.random((20, V)) < 0.3, 5.0, -1.0)
+    x[5:10] = -0.0
+    x[5:10, ::3] = 0.0
+    t = rng.choice([0.0, 0.5, 1.0], R)
+    k = rng.choice([0, 1, 100, 4096, 8999], R)
+    p = rng.choice([1.0, 0.5, 0.25, 0.9], R)
+    m = rng.choice([0.0, 1.0], R)
+    x = torch.from_numpy(x)
+    _check(fa, x.bfloat16() if bf16 else x, t, k, p, m, rng.random(R))
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_infinities_and_nan(fa, bf16):
+    V = 3000
+    rng = np.random.default_rng(2)
+    x = rng.standard_normal((8, V)).astype(np.float32)
+    x[0, ::2] = -np.inf
+    x[1, ::2] = np.nan
+    x[2] = -np.inf
+    x[2, 1234] = -50.0
+    x[3, [5, 700, 2999]] = np.inf
+    x[4, [9, 11]] = [np.inf, np.nan]
+    x[5] = -np.inf
+    x[6] = np.nan
+    x[7, :] = [1e38, -1e38] * (V // 2)
+    x = torch.from_numpy(x)
+    x = x.bfloat16() if bf16 else x
+    for t, k, p in ((1.0, 0, 1.0), (0.0, 0, 1.0), (0.5, 10, 0.9), (2.0, 0, 0.5), (np.inf, 0, 0.7), (1e-45, 5, 1.0), (np.nan, 1, 0.0), (-1.0, 0, 1.0)):
+        _check(fa, x, [t] * 8, [k] * 8, [p] * 8, [0.0] * 8, rng.random(8), flag=fa.ERR_NO_TOKEN)
+
+
+def test_odd_parameters(fa):
+    """Values outside their ranges count as the documentation says."""
+    x = _logits(np.random.default_rng(3), 1, 2000, False)
+    nan, inf = float("nan"), float("inf")
+    rows = [(1.0, -5, 1.0, 0.0, 0.5), (1.0, 0, nan, nan, 0.5), (1.0, 0, 2.0, -1.0, 0.5), (1.0, 0, -3.0, 0.0, 0.5), (1.0, 0, 1.0, 7.0, 0.5),
+            (1.0, 0, 1.0, inf, 0.5), (1.0, 3, 1.0, 0.0, 1.0), (1.0, 3, 1.0, 0.0, 7.0), (1.0, 3, 1.0, 0.0, inf), (1.0, 3, 1.0, 0.0, nan),
+            (1.0, 3, 1.0, 0.0, -1.0), (1.0, 0, 1.0, 0.0, 1.0 - 2.0 ** -24), (1.0, 0, 1.0, 0.0, 0.0), (1.0, 2**31 - 1, 1e-30, 1e-30, 0.3),
+            (1.0, -2**31, 1.0 - 2.0 ** -24, 0.0, 0.999), (1e-30, 0, 1.0, 0.0, 0.9), (3e38, 0, 1.0, 0.0, 0.9)]
+    t, k, p, m, u = (np.array(c) for c in zip(*rows))
+    _check(fa, x.expand(len(rows), -1).contiguous(), t, k, p, m, u)
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_rows_anywhere(fa, bf16):
+    """Rows a stride apart that start at any element, what lies between them not read into the result."""
+    rng = np.random.default_rng(4)
+    big = torch.full((6, 5003), 1e30)
+    big = (big.bfloat16() if bf16 else big).cuda()
+    for start, V in ((0, 4999), (1, 4998), (3, 777), (5, 1)):
+        x = _logits(rng, 6, V, bf16)
+        big.fill_(1e30)
+        view = big[:, start: start + V]
+        view.copy_(x)
+        _check(fa, view, [1.0] * 6, [0, 0, 5, 5, 0, 0], [1.0, 0.9, 1.0, 0.9, 1.0, 0.5], [0.0] * 4 + [0.1, 0.0], rng.random(6))
+
+
+def test_every_token_can_come(fa):
+    """u over all of [0, 1): each token as often as its weight says, in the vocabulary's order."""
+    x = torch.tensor([[1.0, -math.inf, 0.0, 2.0, 1.0]]).expand(4096, -1)
+    u = (np.arange(4096) + 0.5) / 4096
+    _, tokens, _ = _check(fa, x.contiguous(), None, None, None, None, u)
+    got = tokens.cpu().numpy()
+    assert (np.diff(got) >= 0).all()
+    w = np.exp([1.0, -np.inf, 0.0, 2.0, 1.0])
+    assert (np.abs(np.bincount(got, minlength=5) - 4096 * w / w.sum()) <= 1).all()
+
+
+def test_graph_replays(fa):
+    rng = np.random.default_rng(5)
+    R, V = 40, 20000
+    x = _logits(rng, R, V, True).cuda()
+    f32 = lambda a: torch.tensor(np.asarray(a, np.float32), device="cuda")  # noqa: E731
+    u, t, p = f32(rng.random(R)), f32(rng.choice([0.0, 0.7, 1.2], R)), f32(rng.choice([1.0, 0.9], R))
+    k = torch.tensor(rng.choice([0, 50], R).astype(np.int32), device="cuda")
+    tokens, logprob, work = torch.zeros(R, dtype=torch.int32, device="cuda"), torch.zeros(R, device="cuda"), fa.sample_workspace(R, V)
+    call = lambda: fa.sample(x, u, tokens, logprob, temperature=t, top_k=k, top_p=p, workspace=work)  # noqa: E731
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for step in range(4):
+        u.copy_(f32(rng.random(R)))
+        x.copy_(_logits(rng, R, V, True))
+        call()
+        want = tokens.clone(), logprob.clone()
+        work.fill_(step)
+        tokens.zero_(), logprob.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tokens, want[0]) and torch.equal(logprob.view(torch.int32), want[1].view(torch.int32))
+
+
+def test_no_rows(fa):
+    empty = torch.empty(0, dtype=torch.int32, device="cuda")
+    fa.sample(torch.empty(0, 10, device="cuda"), torch.empty(0, device="cuda"), empty, workspace=fa.sample_workspace(0, 10))

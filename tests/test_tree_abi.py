@@ -144,3 +144,49 @@ def test_binding_checks_shapes(fa):
         fa.tree_accept(i(2, 4), m(2, 4), i(2, 4), i(2, 4), kv, kv, i(2), i(2, 4), i(1), i(2))
     with pytest.raises(ValueError, match="on the GPU"):
         fa.tree_accept(i(2, 4), m(2, 4), i(2, 4), i(2, 4), kv, kv, i(2), i(2, 4), i(2), i(2))
+
+
+def _sample(fa, R=3, V=100, bf16=0, stride=100, work=1 << 20, **over):
+    a = dict(logits=_ptr(), temperature=_ptr(), top_k=_ptr(), top_p=_ptr(), min_p=_ptr(), u=_ptr(), tokens=_ptr(), logprob=_ptr(), err=None,
+             workspace=_ptr())
+    a.update(over)
+    desc = fa.SampleDesc(R, V, bf16, stride)
+    return fa.raw_call("fka_sample", C.byref(desc), *a.values(), work, None)
+
+
+@pytest.mark.parametrize("over,status,needle", [
+    (dict(R=-1), -1, "n_rows"), (dict(V=0), -1, "n_vocab"), (dict(V=2**18 + 1, stride=2**19), -2, "logits"), (dict(R=2**20 + 1), -2, "rows"),
+    (dict(bf16=2), -1, "bf16"), (dict(stride=99), -1, "logits_stride"), (dict(stride=-1), -1, "logits_stride"),
+    (dict(logits=None), -1, "logits is null"), (dict(logits=ODD), -1, "logits is not 4-byte"), (dict(bf16=1, logits=C.c_void_p(4097)), -1, "2-byte"),
+    (dict(u=None), -1, "u is null"), (dict(tokens=None), -1, "tokens"), (dict(temperature=ODD), -1, "temperature"), (dict(top_k=ODD), -1, "top_k"),
+    (dict(top_p=ODD), -1, "top_p"), (dict(min_p=ODD), -1, "min_p"), (dict(logprob=ODD), -1, "logprob"), (dict(err=ODD), -1, "err"),
+    (dict(workspace=None), -1, "workspace"), (dict(work=0), -1, "workspace of 0"),
+])
+def test_sample_rejects(fa, over, status, needle):
+    assert _sample(fa, **over) == status
+    assert needle in fa.last_error()
+
+
+def test_sample_rejects_overlaps(fa):
+    p = _ptr()
+    q = C.c_void_p(p.value + 8)
+    for over, needle in ((dict(tokens=p, logprob=q), "overlaps logprob"), (dict(u=p, tokens=q), "overlaps u"), (dict(logits=p, tokens=q), "overlaps logits"),
+                         (dict(workspace=p, top_p=p), "overlaps top_p"), (dict(err=p, logprob=p), "overlaps err")):
+        assert _sample(fa, **over) == -1
+        assert needle in fa.last_error()
+    assert fa.raw_call("fka_sample", *[None] * 11, 0, None) == -1 and "desc" in fa.last_error()
+    assert fa.raw_call("fka_sample_bytes", -1, 5) == 0 and fa.raw_call("fka_sample_bytes", 5, 2**18 + 1) == 0
+    assert fa.raw_call("fka_sample_bytes", 5, 2**18) > 0
+
+
+def test_sample_binding_checks_shapes(fa):
+    f = lambda *s: torch.zeros(s)  # noqa: E731
+    i, w = torch.zeros(2, dtype=torch.int32), torch.zeros(1 << 20, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="fp32 or bf16"):
+        fa.sample(f(2, 5).half(), f(2), i, workspace=w)
+    with pytest.raises(ValueError, match="dense"):
+        fa.sample(f(5, 2).t(), f(2), i, workspace=w)
+    with pytest.raises(ValueError, match="must be"):
+        fa.sample(f(2, 5), f(3), i, workspace=w)
+    with pytest.raises(ValueError, match="on the GPU"):
+        fa.sample(f(2, 5), f(2), i, workspace=w)
