@@ -449,7 +449,7 @@ fka_status fka_tree_attend_paged(const fka_plan *plan, const void *q, const void
                                  const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse, void *stream);
 
 typedef struct {
-    int32_t n_rows;        /* rows of logits, >= 0: the branches of a step, or the nodes of its trees; at most 2^20 */
+    int32_t n_rows;        /* rows of logits, >= 0: the branches of a step, or the nodes of its trees; at most 2^17 */
     int32_t n_vocab;       /* logits of a row, in [1, 2^18] */
     int32_t logits_bf16;   /* 1: bf16, 0: fp32 */
     int64_t logits_stride; /* elements from one row to the next, >= n_vocab (any: rows need not be aligned) */
@@ -477,7 +477,7 @@ size_t fka_sample_bytes(int32_t n_rows, int32_t n_vocab);
  *   workspace                  fka_sample_bytes(n_rows, n_vocab) device bytes (16-byte aligned), used by one call at a time; its contents before
  *                              and after do not matter
  * What is written, the workspace too, may overlap neither itself nor what is read (FKA_ERR_INVALID_ARG).  FKA_ERR_UNSUPPORTED for more than
- * 2^18 logits or 2^20 rows.  The same call gives the same bits.
+ * 2^18 logits or 2^17 rows.  The same call gives the same bits.
  */
 fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const float *temperature, const int32_t *top_k,
                       const float *top_p, const float *min_p, const float *u, int32_t *tokens, float *logprob, int32_t *err,

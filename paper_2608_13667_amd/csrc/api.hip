@@ -769,6 +769,8 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
 constexpr int32_t kMaxRotateTokens = 1 << 25;
 // Most drafted trees of a call.
 constexpr int32_t kMaxTrees = 1 << 20;
+// Most rows of logits of a call: with 64 tiles to a row the scan's threads stay below 2^32.
+constexpr int32_t kMaxSampleRows = 1 << 17;
 
 // The jobs of a decode over 4-bit tiles: ranges of prefix tiles and shares of the suffixes.  Two blocks are resident on a
 // compute unit, and each unit is to have one of either kind: a prefix job is bound by the vector units, a suffix job by its
@@ -2445,8 +2447,9 @@ fka_status fka_tree_accept_paged(const fka_accept_desc *desc, const int32_t *par
 
 size_t fka_sample_bytes(int32_t n_rows, int32_t n_vocab)
 {
-    if (n_rows < 0 || n_rows > kMaxTrees || n_vocab < 1 || n_vocab > fka::kMaxVocab) return 0;  // as fka_sample
-    return 16;
+    if (n_rows < 0 || n_rows > kMaxSampleRows || n_vocab < 1 || n_vocab > fka::kMaxVocab) return 0;  // as fka_sample
+    const size_t tiles = ceil_div(n_vocab, fka::kSampleTile), groups = ceil_div(n_vocab, fka::kSampleGroup);
+    return std::max<size_t>(16, n_rows * (tiles * 12 + groups * 4));
 }
 
 fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const float *temperature, const int32_t *top_k,
@@ -2458,7 +2461,7 @@ fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const flo
     REQUIRE(desc->logits_bf16 == 0 || desc->logits_bf16 == 1, "logits_bf16 must be 0 or 1");
     if (desc->n_vocab > fka::kMaxVocab)
         return fail(FKA_ERR_UNSUPPORTED, "%d logits to a row exceed the limit of %d", desc->n_vocab, fka::kMaxVocab);
-    if (desc->n_rows > kMaxTrees) return fail(FKA_ERR_UNSUPPORTED, "%d rows exceed the limit of %d", desc->n_rows, kMaxTrees);
+    if (desc->n_rows > kMaxSampleRows) return fail(FKA_ERR_UNSUPPORTED, "%d rows exceed the limit of %d", desc->n_rows, kMaxSampleRows);
     REQUIRE(desc->logits_stride >= desc->n_vocab, "logits_stride (%lld) is less than n_vocab (%d)", (long long)desc->logits_stride,
             desc->n_vocab);
     if (desc->n_rows == 0) return ok();
@@ -2498,6 +2501,10 @@ fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const flo
     a.u = u;
     a.tokens = tokens;
     a.logprob = logprob;
+    const size_t tiles = R * ceil_div(desc->n_vocab, fka::kSampleTile);
+    a.tile_sum = static_cast<unsigned long long *>(workspace);
+    a.tile_max = reinterpret_cast<uint32_t *>(a.tile_sum + tiles);
+    a.group_max = a.tile_max + tiles;
     a.err = err;
     const hipError_t e = fka::launch_sample(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "sample kernel launch");

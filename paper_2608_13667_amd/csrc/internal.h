@@ -495,7 +495,9 @@ struct AcceptArgs {
     int32_t *err;                    // nullable
 };
 
-// The token that a row of logits gives (sample.h).
+// The token that a row of logits gives (sample.h): logits of a group and of a tile, of which the scan leaves maxima and sums.
+constexpr int kSampleGroup = 64;
+constexpr int kSampleTile = 4096;
 struct SampleArgs {
     const void *logits;      // [rows] of n_vocab fp32 or bf16, `stride` elements apart
     int64_t stride;
@@ -506,6 +508,9 @@ struct SampleArgs {
     const float *u;                            // [rows]
     int32_t *tokens;                           // [rows]
     float *logprob;                            // [rows], nullable
+    unsigned long long *tile_sum;              // [rows][tiles]
+    uint32_t *tile_max;                        // [rows][tiles]
+    uint32_t *group_max;                       // [rows][groups]
     int32_t *err;                              // nullable
 };
 constexpr int kMaxVocab = 1 << 18;

@@ -155,7 +155,7 @@ def _sample(fa, R=3, V=100, bf16=0, stride=100, work=1 << 20, **over):
 
 
 @pytest.mark.parametrize("over,status,needle", [
-    (dict(R=-1), -1, "n_rows"), (dict(V=0), -1, "n_vocab"), (dict(V=2**18 + 1, stride=2**19), -2, "logits"), (dict(R=2**20 + 1), -2, "rows"),
+    (dict(R=-1), -1, "n_rows"), (dict(V=0), -1, "n_vocab"), (dict(V=2**18 + 1, stride=2**19), -2, "logits"), (dict(R=2**17 + 1), -2, "rows"),
     (dict(bf16=2), -1, "bf16"), (dict(stride=99), -1, "logits_stride"), (dict(stride=-1), -1, "logits_stride"),
     (dict(logits=None), -1, "logits is null"), (dict(logits=ODD), -1, "logits is not 4-byte"), (dict(bf16=1, logits=C.c_void_p(4097)), -1, "2-byte"),
     (dict(u=None), -1, "u is null"), (dict(tokens=None), -1, "tokens"), (dict(temperature=ODD), -1, "temperature"), (dict(top_k=ODD), -1, "top_k"),
