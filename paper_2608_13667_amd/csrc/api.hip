@@ -2445,11 +2445,35 @@ fka_status fka_tree_accept_paged(const fka_accept_desc *desc, const int32_t *par
                       stream);
 }
 
+// Lays the workspace out (n_rows and n_vocab given); its bytes.
+static size_t sample_layout(fka::SampleArgs &a, char *at)
+{
+    const size_t R = a.n_rows, tiles = ceil_div(a.n_vocab, fka::kSampleTile), groups = ceil_div(a.n_vocab, fka::kSampleGroup);
+    a.max_left = std::min(a.n_rows, fka::kSampleMaxLeft);
+    a.shares = std::max(1, std::min((int32_t)tiles, 2048 / std::max(1, a.max_left)));
+    size_t bytes = 0;
+    auto take = [&](auto *&p, size_t n) {
+        using X = std::remove_reference_t<decltype(*p)>;
+        p = reinterpret_cast<X *>(at + bytes);
+        bytes += (n * sizeof(X) + 15) & ~size_t(15);
+    };
+    take(a.n_left, 1);
+    take(a.left, a.max_left);
+    take(a.list, (size_t)a.max_left * fka::kSampleList);
+    take(a.hist, (size_t)a.max_left * a.shares * fka::kSampleLeftBins);
+    take(a.tile_sum, R * tiles);
+    take(a.tile_max, R * tiles);
+    take(a.group_max, R * groups);
+    return bytes;
+}
+
 size_t fka_sample_bytes(int32_t n_rows, int32_t n_vocab)
 {
     if (n_rows < 0 || n_rows > kMaxSampleRows || n_vocab < 1 || n_vocab > fka::kMaxVocab) return 0;  // as fka_sample
-    const size_t tiles = ceil_div(n_vocab, fka::kSampleTile), groups = ceil_div(n_vocab, fka::kSampleGroup);
-    return std::max<size_t>(16, n_rows * (tiles * 12 + groups * 4));
+    fka::SampleArgs a{};
+    a.n_rows = n_rows;
+    a.n_vocab = n_vocab;
+    return sample_layout(a, nullptr);
 }
 
 fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const float *temperature, const int32_t *top_k,
@@ -2501,11 +2525,9 @@ fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const flo
     a.u = u;
     a.tokens = tokens;
     a.logprob = logprob;
-    const size_t tiles = R * ceil_div(desc->n_vocab, fka::kSampleTile);
-    a.tile_sum = static_cast<unsigned long long *>(workspace);
-    a.tile_max = reinterpret_cast<uint32_t *>(a.tile_sum + tiles);
-    a.group_max = a.tile_max + tiles;
     a.err = err;
+    sample_layout(a, static_cast<char *>(workspace));
+    if (!top_p) a.max_left = 0;
     const hipError_t e = fka::launch_sample(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "sample kernel launch");
     return ok();

@@ -498,6 +498,18 @@ struct AcceptArgs {
 // The token that a row of logits gives (sample.h): logits of a group and of a tile, of which the scan leaves maxima and sums.
 constexpr int kSampleGroup = 64;
 constexpr int kSampleTile = 4096;
+// Rows that several blocks share: most of them, bins of a histogram, entries of a list; the blocks of such a row are some
+// 2048 / rows, up to one to a tile.
+constexpr int kSampleMaxLeft = 1024;
+constexpr int kSampleLeftBins = 1024;
+constexpr int kSampleList = 2048;
+struct SampleLeft {
+    double limit;              // top-p's: what is in front of a kept logit is less
+    unsigned long long front;  // in front of the bin that holds the threshold
+    int32_t row;
+    uint32_t max_key;
+    int32_t count, unused;     // entries of the list
+};
 struct SampleArgs {
     const void *logits;      // [rows] of n_vocab fp32 or bf16, `stride` elements apart
     int64_t stride;
@@ -511,6 +523,11 @@ struct SampleArgs {
     unsigned long long *tile_sum;              // [rows][tiles]
     uint32_t *tile_max;                        // [rows][tiles]
     uint32_t *group_max;                       // [rows][groups]
+    int32_t max_left, shares;                  // rows that several blocks may share (0: none is left to them), their blocks
+    int32_t *n_left;
+    SampleLeft *left;                          // [max_left]
+    unsigned long long *list;                  // [max_left][kSampleList]
+    unsigned long long *hist;                  // [max_left][shares][kSampleLeftBins]
     int32_t *err;                              // nullable
 };
 constexpr int kMaxVocab = 1 << 18;

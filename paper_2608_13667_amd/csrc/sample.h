@@ -7,26 +7,32 @@
 // than p of their sum in front of them.  So what is kept is one logit value, the threshold, and a place: everything above the value,
 // and of its equals those up to the place.  min-p is a bound on w itself.
 //
-// Two kernels.  sample_scan_kernel reads the logits, all blocks at the rate of the memory: the largest of every 64 (a
-// group), and of every 4096 (a tile) also the sum of the weights against the tile's own largest, where the row needs a sum over all.
+// sample_scan_kernel reads the logits, all blocks at the rate of the memory: the largest of every 64 (a group), and of every 4096 (a
+// tile) also the sum of the weights against the tile's own largest, where the row needs a sum over all.
 // sample_row_kernel, a block to a row, then reads little more of it:
 //   * nothing filtered: the tiles' sums give the tile that the random number falls into, which is read;
 //   * otherwise the groups' maxima bound the threshold from below: the k-th largest of them is no larger than the k-th largest
-//     logit.  The groups that reach the bound are read and the logits above it listed, up to 2048, ranked, and filtered.  For top-p
-//     alone the bound is that of 256 groups, and the list will do if it has p of the sum;
-//   * where it does not, a histogram of the weights by (M - l) / t, then the list of the bin where the sum passes p;
-//   * where a list does not fit: the threshold digit by digit of the logit's bits (11, 11, 10 from the top, as unsigned numbers in the
-//     logits' order), a histogram of each digit's values among what agrees in the digits before.
+//     logit.  The groups that reach the bound are read and the logits above it listed, up to 2048, and filtered.  For top-p
+//     alone the bound is that of 128 groups, and the list will do if it has p of the sum;
+//   * where it has not, the row is left to three more kernels, in which many blocks share it: a histogram of the weights by
+//     (M - l) / t; the bin where their sum passes p, whose logits are listed, and the sums of each tile's logits above it; the draw;
+//   * where a list does not fit (thousands of equal logits, a k in the thousands), the block goes over the row by itself: the threshold
+//     digit by digit of the logit's bits (11, 11, 10 from the top, as unsigned numbers in the logits' order), a histogram of each
+//     digit's values among what agrees in the digits before.
 #pragma once
 
+#include <type_traits>
+
 #include "internal.h"
+#include "scan64.h"
 
 namespace fka {
 
-constexpr int kSampleThreads = 1024;
+constexpr int kSampleThreads = 512;
 constexpr int kSampleWaves = kSampleThreads / 64;
 constexpr int kSampleBins = 2048;
-constexpr int kSampleList = 2048;
+constexpr int kSampleFew = kSampleThreads / 4;
+constexpr int kSampleFirst = 128;  // groups whose maxima bound the list of top-p alone
 constexpr double kSampleUnit = 17592186044416.0;  // 2^44
 constexpr uint32_t kNoLogit = 0x007fffffu;        // the key of -inf (NaN counts as that)
 
@@ -64,30 +70,45 @@ __device__ inline float sample_logit(uint32_t key) { return __uint_as_float(key 
 struct SampleWeight {
     const double *table;  // kSampleTable, in LDS
     double max, step;     // M, 64 / (t ln 2)
-    uint32_t max_key;
 
-    __device__ inline SampleWeight(const double *table_, uint32_t max_key_, float t)
-        : table(table_), max((double)sample_logit(max_key_)), step(64 * 1.4426950408889634074 / (double)t), max_key(max_key_)
+    __device__ inline SampleWeight(const double *table_, uint32_t max_key, float t)
+        : table(table_), max((double)sample_logit(max_key)), step(64 * 1.4426950408889634074 / (double)t)
     {
+    }
+    // what exp is of, in units of ln 2 / 64; no less than `least`, as which NaN counts (an infinite M beside another logit)
+    __device__ inline double times64(float x, double least) const { return fmax(((double)x - max) * step, least); }
+    __device__ static inline double series(double r)  // 2^(r / 64)
+    {
+        constexpr double L = 0.69314718055994530942 / 64;
+        double p = __builtin_fma(r, L * L * L * L * L / 120, L * L * L * L / 24);
+        p = __builtin_fma(r, p, L * L * L / 6);
+        p = __builtin_fma(r, p, L * L / 2);
+        p = __builtin_fma(r, p, L);
+        return __builtin_fma(r, p, 1.0);
     }
     __device__ inline double exact(uint32_t key) const
     {
-        if (key == max_key) return kSampleUnit;
-        const double z = ((double)sample_logit(key) - max) * step;
-        if (!(z > -64.0 * 1000) || key == kNoLogit) return 0;  // (also infinities: -inf, or all but those of an infinite M)
-        const double n = rint(z), r = (z - n) * (0.69314718055994530942 / 64);
+        const float x = sample_logit(key);
+        if ((double)x == max) return kSampleUnit;
+        const double z = times64(x, -64.0 * 1000), n = rint(z);
         const int m = (int)n;
-        double p = __builtin_fma(r, 1.0 / 120, 1.0 / 24);
-        p = __builtin_fma(r, p, 1.0 / 6);
-        p = __builtin_fma(r, p, 0.5);
-        p = __builtin_fma(r, p, 1.0);
-        p = __builtin_fma(r, p, 1.0);
-        return ldexp(table[m & 63] * p, (m >> 6) + 44);
+        return ldexp(table[m & 63] * series(z - n), (m >> 6) + 44);
+    }
+    // The weight + kMark.  What is below 2^-60 of the largest rounds to 0.
+    static constexpr u64 kMark = 0x4330000000000000ull;
+    __device__ inline u64 marked(float x) const
+    {
+        const double z = times64(x, -64.0 * 60), n = rint(z), p = series(z - n);
+        const int m = (int)n;
+        const double y = table[m & 63] * p;
+        const u64 scaled = (u64)__double_as_longlong(y) + ((u64)(uint32_t)((m >> 6) + 44) << 52);
+        // 2^52 added rounds to a whole number in the lowest bits
+        return (u64)__double_as_longlong(__longlong_as_double((long long)scaled) + 4503599627370496.0);
     }
     __device__ inline u64 operator()(uint32_t key) const
     {
-        // 2^52 added rounds to a whole number in the lowest bits
-        return (u64)__double_as_longlong(exact(key) + 4503599627370496.0) & 0xfffffffffffffull;
+        const float x = sample_logit(key);
+        return (double)x == max ? (u64)kSampleUnit : marked(x) - kMark;
     }
 };
 
@@ -96,30 +117,47 @@ struct SampleRow;
 template <>
 struct SampleRow<float> {
     static constexpr int VEC = 4;
+    static constexpr uint32_t kNone = 0xff800000u;
     __device__ static float get(const uint32_t (&w)[4], int i) { return __uint_as_float(w[i]); }
     __device__ static float one(const float *p) { return *p; }
 };
 template <>
 struct SampleRow<uint16_t> {
     static constexpr int VEC = 8;
+    static constexpr uint32_t kNone = 0xff80ff80u;
     __device__ static float get(const uint32_t (&w)[4], int i) { return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16); }
     __device__ static float one(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
 };
 
-// The keys of the VEC logits from place i on (those past the row's end: kNoLogit).
+// The VEC logits from place i on, 16 bytes, as they lie in memory (rows may start anywhere); `whole`: none is past the row's end, otherwise those
+// that are count as -inf.
+template <class T>
+__device__ inline void sample_load(const T *row, int i, int n, bool whole, uint32_t (&w)[4])
+{
+    using R = SampleRow<T>;
+    if (whole || i + R::VEC <= n) {
+        __builtin_memcpy(w, row + i, 16);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            w[j] = R::kNone;
+            if constexpr (R::VEC == 4) {
+                if (i + j < n) w[j] = __float_as_uint(R::one(row + i + j));
+            } else {
+                if (i + 2 * j < n) w[j] = (R::kNone << 16) | row[i + 2 * j];
+                if (i + 2 * j + 1 < n) w[j] = (w[j] & 0xffffu) | (uint32_t)row[i + 2 * j + 1] << 16;
+            }
+        }
+    }
+}
+
 template <class T>
 __device__ inline void sample_keys(const T *row, int i, int n, uint32_t (&key)[SampleRow<T>::VEC])
 {
-    using R = SampleRow<T>;
-    if (i + R::VEC <= n) {
-        uint32_t w[4];
-        __builtin_memcpy(w, row + i, 16);  // rows may start anywhere
+    uint32_t w[4];
+    sample_load(row, i, n, false, w);
 #pragma unroll
-        for (int j = 0; j < R::VEC; ++j) key[j] = sample_key(R::get(w, j));
-    } else {
-#pragma unroll
-        for (int j = 0; j < R::VEC; ++j) key[j] = i + j < n ? sample_key(R::one(row + i + j)) : kNoLogit;
-    }
+    for (int j = 0; j < SampleRow<T>::VEC; ++j) key[j] = sample_key(SampleRow<T>::get(w, j));
 }
 
 __device__ inline bool sample_all(const SampleArgs &a, int r)  // whether row r needs the sum over all its logits
@@ -129,10 +167,51 @@ __device__ inline bool sample_all(const SampleArgs &a, int r)  // whether row r 
     return t > 0.f && !(k > 0 && k < a.n_vocab) && (p < 1.f || !(m > 0.f));
 }
 
+// Steps across lanes in the vector ALU (a shuffle is a round trip to LDS).
+template <int CTRL, int ROWS = 0xf>
+__device__ inline uint32_t sample_dpp(uint32_t x)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS = 0xf>
+__device__ inline u64 sample_dpp(u64 x)
+{
+    return (u64)sample_dpp<CTRL, ROWS>((uint32_t)(x >> 32)) << 32 | sample_dpp<CTRL, ROWS>((uint32_t)x);
+}
+// f over the lanes up to each (0 where f(0, x) = x): row shifts, then the rows' last lanes.
+template <class X, class F>
+__device__ inline X sample_wave_scan(X x, F &&f)
+{
+    x = f(sample_dpp<0x111>(x), x);
+    x = f(sample_dpp<0x112>(x), x);
+    x = f(sample_dpp<0x114>(x), x);
+    x = f(sample_dpp<0x118>(x), x);
+    x = f(sample_dpp<0x142, 0xa>(x), x);
+    return f(sample_dpp<0x143, 0xc>(x), x);
+}
+__device__ inline uint32_t sample_last(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)x, 63); }
+__device__ inline u64 sample_last(u64 x) { return (u64)sample_last((uint32_t)(x >> 32)) << 32 | sample_last((uint32_t)x); }
+template <class X>
+__device__ inline X sample_wave_max(X x)
+{
+    return sample_last(sample_wave_scan(x, [](X a, X b) { return a > b ? a : b; }));
+}
 __device__ inline u64 sample_wave_sum(u64 x)
 {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d);
+    return sample_last(sample_wave_scan(x, [](u64 a, u64 b) { return a + b; }));
+}
+
+// Largest of the lane's 16-byte neighbours in a group of 64 logits.
+template <int LANES>
+__device__ inline float sample_group_max(float x)
+{
+    auto step = [](float v, auto ctrl) {
+        return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true)));
+    };
+    x = step(x, std::integral_constant<int, 0xb1>{});  // quad_perm 1,0,3,2
+    x = step(x, std::integral_constant<int, 0x4e>{});  // quad_perm 2,3,0,1
+    x = step(x, std::integral_constant<int, 0x141>{});  // row_half_mirror
+    if constexpr (LANES == 16) x = step(x, std::integral_constant<int, 0x140>{});  // row_mirror
     return x;
 }
 
@@ -140,49 +219,63 @@ __device__ inline u64 sample_wave_sum(u64 x)
 template <class T>
 __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a)
 {
-    constexpr int VEC = SampleRow<T>::VEC, LOADS = kSampleTile / (256 * VEC), GL = kSampleGroup / VEC;  // lanes of a group
+    using R = SampleRow<T>;
+    constexpr int VEC = R::VEC, LOADS = kSampleTile / (256 * VEC), GL = kSampleGroup / VEC;  // lanes of a group
     __shared__ double table[64];
     __shared__ uint32_t top[4];
     __shared__ u64 part[4];
     const int tid = threadIdx.x, n = a.n_vocab;
     const int tiles = (n + kSampleTile - 1) / kSampleTile, groups = (n + kSampleGroup - 1) / kSampleGroup;
-    const int r = blockIdx.x / tiles, tile = blockIdx.x - r * tiles;
+    const int r = blockIdx.x / tiles, tile = blockIdx.x - r * tiles, i0 = tile * kSampleTile + tid * VEC;
     const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.stride;
-    uint32_t key[LOADS][VEC], most = 0;
+    if (blockIdx.x == 0 && tid == 0) *a.n_left = 0;
+    uint32_t w[LOADS][4];
+    if ((tile + 1) * kSampleTile <= n) {
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) sample_keys(row, tile * kSampleTile + j * 256 * VEC + tid * VEC, n, key[j]);
+        for (int j = 0; j < LOADS; ++j) sample_load(row, i0 + j * 256 * VEC, n, true, w[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) sample_load(row, i0 + j * 256 * VEC, n, false, w[j]);
+    }
     const bool all = sample_all(a, r);
     if (all && tid < 64) table[tid] = kSampleTable[tid];
+    float most = -INFINITY;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-        uint32_t m = key[j][0];
+        float m = -INFINITY;  // (fmaxf drops a NaN)
 #pragma unroll
-        for (int i = 1; i < VEC; ++i) m = max(m, key[j][i]);
-#pragma unroll
-        for (int d = 1; d < GL; d <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, d));
-        const int g = (tile * kSampleTile + j * 256 * VEC + tid * VEC) / kSampleGroup;
-        if (tid % GL == 0 && g < groups) a.group_max[(size_t)r * groups + g] = m;
-        most = max(most, m);
+        for (int i = 0; i < VEC; ++i) m = fmaxf(m, R::get(w[j], i));
+        m = sample_group_max<GL>(m);
+        const int g = (i0 + j * 256 * VEC) / kSampleGroup;
+        if (tid % GL == 0 && g < groups) a.group_max[(size_t)r * groups + g] = sample_key(m);
+        most = fmaxf(most, m);
     }
     if (!all) return;  // (uniform)
-#pragma unroll
-    for (int d = GL; d < 64; d <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, d));
-    if ((tid & 63) == 0) top[tid >> 6] = most;
+    const uint32_t wave_max = sample_wave_max(sample_key(most));
+    if ((tid & 63) == 0) top[tid >> 6] = wave_max;
     __syncthreads();
-    most = max(max(top[0], top[1]), max(top[2], top[3]));
+    const uint32_t max_key = max(max(top[0], top[1]), max(top[2], top[3]));
     u64 sum = 0;
-    if (most != kNoLogit) {
-        const SampleWeight weight(table, most, a.temperature ? a.temperature[r] : 1.f);
+    if (max_key != kNoLogit) {
+        const SampleWeight weight(table, max_key, a.temperature ? a.temperature[r] : 1.f);
+        if (sample_logit(max_key) < INFINITY) {
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j)
+            for (int j = 0; j < LOADS; ++j)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) sum += weight(key[j][i]);
+                for (int i = 0; i < VEC; ++i) sum += weight.marked(R::get(w[j], i));
+            sum -= LOADS * VEC * SampleWeight::kMark;
+        } else {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum += R::get(w[j], i) == INFINITY ? (u64)kSampleUnit : 0;
+        }
     }
     sum = sample_wave_sum(sum);
     if ((tid & 63) == 0) part[tid >> 6] = sum;
     __syncthreads();
     if (tid == 0) {
-        a.tile_max[(size_t)r * tiles + tile] = most;
+        a.tile_max[(size_t)r * tiles + tile] = max_key;
         a.tile_sum[(size_t)r * tiles + tile] = part[0] + part[1] + part[2] + part[3];
     }
 }
@@ -190,56 +283,61 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a)
 struct SampleShared {
     double table[64];
     u64 hist[kSampleBins];
-    u64 list[kSampleList], ranked[kSampleList];  // (key << 32 | ~place): a larger one comes first
+    u64 list[kSampleList], weight[kSampleList];  // (key << 32 | ~place): a larger one comes first
+    uint16_t few[kSampleFew];
     uint16_t groups[kMaxVocab / kSampleGroup];
-    u64 part[kSampleWaves];
-    u64 tile[kMaxVocab / kSampleTile];
+    u64 part[2 * kSampleWaves];
+    u64 tile[kMaxVocab / (kSampleThreads * 4)];
     u64 result[4];
-    int count;
+    int count, n_few;
 };
 
 // Sum over the block's threads before this one; `total` gets the sum of all.
-__device__ inline u64 sample_scan(u64 x, SampleShared &s, u64 &total)
+template <int WAVES = kSampleWaves>
+__device__ inline u64 sample_scan(u64 x, u64 *part, u64 &total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    u64 y = x;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const u64 z = __shfl_up(y, d);
-        if (lane >= d) y += z;
-    }
+    const u64 y = sample_wave_scan(x, [](u64 a, u64 b) { return a + b; });
     __syncthreads();
-    if (lane == 63) s.part[wave] = y;
+    if (lane == 63) part[wave] = y;
     __syncthreads();
     u64 before = 0;
     total = 0;
 #pragma unroll
-    for (int i = 0; i < kSampleWaves; ++i) {
+    for (int i = 0; i < WAVES; ++i) {
         if (i == wave) before = total;
-        total += s.part[i];
+        total += part[i];
     }
     return before + y - x;
 }
 
-// The last filled bin, from the top, with less than `limit` in front of it, and what is in front.
+// The last filled bin for whose front (`front`, and what is in the bins before it) takes(front) holds, and that front.  takes() holds up to
+// some sum and not past it, so this is the bin whose own content leads past it, or the last that is filled.
+template <int BINS, int THREADS, class F>
+__device__ inline int sample_bin(const u64 *hist, u64 *part, u64 *result, u64 front, u64 &before, F &&takes)
+{
+    constexpr int EACH = BINS / THREADS;
+    u64 x[EACH], sum = 0, total;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) sum += x[e] = hist[threadIdx.x * EACH + e];
+    u64 in_front = sample_scan<THREADS / 64>(sum, part, total) + front;
+    total += front;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const u64 next = in_front + x[e];
+        if (x[e] && takes(in_front) && (next == total || !takes(next))) {
+            result[0] = (u64)(threadIdx.x * EACH + e);
+            result[1] = in_front;
+        }
+        in_front = next;
+    }
+    __syncthreads();
+    before = result[1];
+    return (int)result[0];
+}
 __device__ inline int sample_bin(double limit, u64 front, SampleShared &s, u64 &before)
 {
-    static_assert(kSampleBins == 2 * kSampleThreads, "two bins a thread");
-    const int tid = threadIdx.x;
-    const u64 a = s.hist[2 * tid], b = s.hist[2 * tid + 1];
-    u64 total;
-    const u64 in_front = sample_scan(a + b, s, total) + front;
-    if (tid == 0) s.result[0] = 0;
-    __syncthreads();
-    u64 mine = 0;
-    if (a && (double)in_front < limit) mine = (u64)tid * 2 + 1;
-    if (b && (double)(in_front + a) < limit) mine = (u64)tid * 2 + 2;
-    if (mine) atomicMax(&s.result[0], mine);
-    __syncthreads();
-    if (mine && s.result[0] == mine) s.result[1] = (mine & 1) ? in_front : in_front + a;
-    __syncthreads();
-    before = s.result[1];
-    return (int)s.result[0] - 1;
+    return sample_bin<kSampleBins, kSampleThreads>(s.hist, s.part, s.result, front, before, [=](u64 x) { return (double)x < limit; });
 }
 
 __device__ inline void sample_clear(SampleShared &s)
@@ -306,7 +404,7 @@ __device__ inline int sample_place(const T *row, int n, uint32_t key, u64 r, Sam
 #pragma unroll
         for (int j = 0; j < VEC; ++j) here += i + j < n && k[j] == key;
         u64 total;
-        u64 rank = seen + sample_scan(here, s, total);
+        u64 rank = seen + sample_scan(here, s.part, total);
         if (seen + total >= r) {
 #pragma unroll
             for (int j = 0; j < VEC; ++j)
@@ -319,41 +417,119 @@ __device__ inline int sample_place(const T *row, int n, uint32_t key, u64 r, Sam
     return n;
 }
 
-// Appends the logits that take() accepts to the list; s.count counts them all, also those that do not fit.
-__device__ inline void sample_append(SampleShared &s, uint32_t key, int place)
+// The place of the last of the keys equal to `key` that top-p keeps, with `before` in front of the first: that one, and each further one
+// with less than `limit` in front of it.
+template <class T>
+__device__ inline int sample_mass_place(const T *row, int n, uint32_t key, u64 w, u64 before, double limit, SampleShared &s)
 {
-    const int at = atomicAdd(&s.count, 1);
-    if (at < kSampleList) s.list[at] = (u64)key << 32 | (uint32_t)~place;
+    u64 more = 1;
+    for (u64 by = (u64)1 << 18; by; by >>= 1)
+        if ((double)(before + (more + by - 1) * w) < limit) more += by;
+    return sample_place(row, n, key, more, s);
 }
 
-// s.ranked: the n entries of s.list in falling order (they differ, by their places).
-__device__ inline void sample_rank(SampleShared &s, int n)
+// Appends the logits that each lane takes, bit j of `take` for key[j] at place + j, a wave at once; `count` counts them all, also those
+// that do not fit.
+template <int N>
+__device__ inline void sample_append(u64 *list, int *count, uint32_t take, const uint32_t (&key)[N], int place)
+{
+    if (!__builtin_amdgcn_ballot_w64(take != 0)) return;
+    const int mine = __popc(take), up_to = scan64(mine);
+    int base = 0;
+    if ((threadIdx.x & 63) == 63) base = atomicAdd(count, up_to);
+    int at = __builtin_amdgcn_readlane(base, 63) + up_to - mine;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (take >> j & 1) {
+            if (at < kSampleList) list[at] = (u64)key[j] << 32 | (uint32_t)~(place + j);
+            ++at;
+        }
+}
+
+// The part where the sum of up to 128 parts' sums passes the mark, and what is left of the mark in it.
+struct SamplePart {
+    int part;
+    u64 mark, total;
+};
+template <class F>
+__device__ inline SamplePart sample_part(const u64 *sums, int parts, F &&mark_of)
+{
+    const int lane = threadIdx.x & 63;
+    const u64 a = 2 * lane < parts ? sums[2 * lane] : 0, b = 2 * lane + 1 < parts ? sums[2 * lane + 1] : 0;
+    const u64 up_to = sample_wave_scan(a + b, [](u64 x, u64 y) { return x + y; }), total = sample_last(up_to), mark = mark_of(total);
+    const int at = __builtin_ctzll(__builtin_amdgcn_ballot_w64(up_to > mark));
+    const u64 front = __shfl(up_to - a - b, at), first = __shfl(a, at);
+    const bool second = mark - front >= first;
+    return SamplePart{2 * at + (second ? 1 : 0), mark - front - (second ? first : 0), total};
+}
+
+// Of the n entries of s.list, those from `from` on in falling order (they differ, by their places): the last with less than `limit`
+// in front of it, in what q(i) says of entry i, on top of `front`.  A histogram by the entries' upper bits finds a bin; its entries, where they
+// are few, are compared with each other, otherwise their own range is cut into bins again.
+template <class Q>
+__device__ inline u64 sample_list_select(int n, u64 from, double limit, u64 front, SampleShared &s, Q &&q)
 {
     const int tid = threadIdx.x;
-    if (n <= 512) {  // an entry's rank is the number of those above it; the threads of an entry share the others
-        const int shares = n <= 64 ? 16 : n <= 128 ? 8 : n <= 256 ? 4 : 2;  // neighbouring lanes
-        const int i = tid / shares, share = tid % shares;
-        const u64 x = i < n ? s.list[i] : 0;
-        int above = 0;
-        for (int j = share; j < n; j += shares) above += s.list[j] > x;
-        for (int d = 1; d < shares; d <<= 1) above += __shfl_xor(above, d);
-        if (i < n && share == 0) s.ranked[above] = x;
-        __syncthreads();
-        return;
-    }
-    // a bitonic sort of 1024 or 2048 entries
-    const int size = n <= 1024 ? 1024 : 2048;
-    for (int i = tid; i < size; i += kSampleThreads) s.ranked[i] = i < n ? s.list[i] : 0;
-    __syncthreads();
-    for (int run = 2; run <= size; run <<= 1)
-        for (int d = run >> 1; d; d >>= 1) {
-            for (int e = tid; e < size / 2; e += kSampleThreads) {
-                const int lo = (e & ~(d - 1)) * 2 + (e & (d - 1)), hi = lo + d;
-                const u64 x = s.ranked[lo], y = s.ranked[hi];
-                if ((x < y) == ((lo & run) == 0)) s.ranked[lo] = y, s.ranked[hi] = x;
-            }
-            __syncthreads();
+    u64 low = 0, hi = 0;  // ~ the lowest, the highest
+    for (int i = tid; i < n; i += kSampleThreads) {
+        const u64 x = s.list[i];
+        if (x >= from) {
+            low = ~x > low ? ~x : low;
+            hi = x > hi ? x : hi;
         }
+    }
+    for (;;) {  // [~low, hi] holds the entry; each round keeps less than a 1024th of it
+        low = sample_wave_max(low);
+        hi = sample_wave_max(hi);
+        __syncthreads();
+        if ((tid & 63) == 0) {
+            s.part[tid >> 6] = hi;
+            s.part[kSampleWaves + (tid >> 6)] = low;
+        }
+        if (tid == 0) s.n_few = 0;
+        sample_clear(s);
+#pragma unroll
+        for (int i = 0; i < kSampleWaves; ++i) {
+            hi = s.part[i] > hi ? s.part[i] : hi;
+            low = s.part[kSampleWaves + i] > low ? s.part[kSampleWaves + i] : low;
+        }
+        const u64 top = hi, bottom = ~low, width = (top - bottom) >> 11;
+        const int shift = width ? 64 - __builtin_clzll(width) : 0;
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const u64 x = s.list[i];
+            if (x >= bottom && x <= top) {
+                const u64 add = q(i);
+                if (add) atomicAdd(&s.hist[(top - x) >> shift], add);
+            }
+        }
+        __syncthreads();
+        const u64 b = (u64)sample_bin(limit, front, s, front);
+        low = hi = 0;
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const u64 x = s.list[i];
+            if (x >= bottom && x <= top && (top - x) >> shift == b && q(i)) {
+                const int at = atomicAdd(&s.n_few, 1);
+                if (at < kSampleFew) s.few[at] = (uint16_t)i;
+                low = ~x > low ? ~x : low;
+                hi = x > hi ? x : hi;
+            }
+        }
+        if (tid == 0) s.result[3] = ~0ull;
+        __syncthreads();
+        if (s.n_few <= kSampleFew) break;
+    }
+    // four lanes an entry share the others
+    const int few = s.n_few, i = tid / 4;
+    if (i < few) {
+        const u64 x = s.list[s.few[i]];
+        u64 before = 0;
+        for (int j = tid % 4; j < few; j += 4) before += s.list[s.few[j]] > x ? q(s.few[j]) : 0;
+        before += __shfl_xor(before, 1);
+        before += __shfl_xor(before, 2);
+        if ((double)(front + before) < limit) atomicMin(&s.result[3], x);
+    }
+    __syncthreads();
+    return s.result[3];
 }
 
 // What is drawn from: the row's parameters.
@@ -361,6 +537,14 @@ struct SampleDraw {
     float t, p, u;
     int k;      // 0: no top-k
     u64 least;  // the smallest weight that min-p keeps
+
+    __device__ inline SampleDraw(const SampleArgs &a, int r)
+        : t(a.temperature ? a.temperature[r] : 1.f), p(a.top_p ? a.top_p[r] : 1.f), u(a.u[r]), k(a.top_k ? a.top_k[r] : 0)
+    {
+        if (k < 0 || k >= a.n_vocab) k = 0;
+        const float m = a.min_p ? a.min_p[r] : 0.f;
+        least = m > 0.f ? (u64)ceil(fmin((double)m, 1.0) * kSampleUnit) : 0;
+    }
     __device__ inline u64 mark(u64 total) const
     {
         const double at = floor((u > 0.f ? (double)u : 0.0) * (double)total);
@@ -375,48 +559,118 @@ __device__ inline void sample_answer(const SampleArgs &a, int r, int token, doub
     if (a.logprob) a.logprob[r] = (float)logprob;
 }
 
+// The same as sample_from_list for up to 64 entries, by one wave: an entry's rank is the number of those above it, and with the entries
+// in that order sums across lanes take the place of histograms.
+__device__ inline bool sample_from_few(const SampleArgs &a, int r, const SampleDraw &draw, const SampleWeight &weight, int n, double sum,
+                                       SampleShared &s)
+{
+    const int lane = threadIdx.x & 63;
+    u64 x = lane < n ? s.list[lane] : 0;
+    auto entry = [](u64 v, int i) {
+        return (u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+    };
+    int rank = lane < n ? 0 : lane;
+    for (int i = 0; i < n; ++i) rank += lane < n && entry(x, i) > x ? 1 : 0;
+    x = (u64)(uint32_t)__builtin_amdgcn_ds_permute(4 * rank, (int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_ds_permute(4 * rank, (int)x);
+    if (draw.k) n = min(n, draw.k);
+    auto add = [](u64 p, u64 q) { return p + q; };
+    u64 w = lane < n ? weight((uint32_t)(x >> 32)) : 0;
+    const u64 up_to = sample_wave_scan(w, add), total = sample_last(up_to);
+    bool in = w > 0 && w >= draw.least;
+    if (draw.p < 1.f) {
+        const double limit = fmax((double)draw.p * (draw.k ? (double)total : sum), 0.5);  // the first is always kept
+        if (!draw.k && (double)total < limit) return false;
+        in = in && (double)(up_to - w) < limit;
+    }
+    w = in ? w : 0;
+    const u64 kept = sample_wave_sum(w), mark = draw.mark(kept);
+    u64 before = 0;  // the kept weights of lower places
+    for (int i = 0; i < n; ++i) {
+        const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, i);  // ~place
+        before += at > (uint32_t)x ? entry(w, i) : 0;
+    }
+    if (w && mark >= before && mark < before + w) sample_answer(a, r, (int)~(uint32_t)x, log((double)w / (double)kept));
+    return true;
+}
+
 // Filters and draws from the n entries of s.list, which hold all that is kept.  `sum`: of all the row's weights, where the list is
 // not known to hold what top-p keeps; false if it does not.
 __device__ inline bool sample_from_list(const SampleArgs &a, int r, const SampleDraw &draw, const SampleWeight &weight, int n, double sum,
                                         SampleShared &s)
 {
     const int tid = threadIdx.x;
-    sample_rank(s, n);
-    if (draw.k) n = min(n, draw.k);
-    // two entries a thread, in order
-    u64 w[2], before[2], total;
-    for (int e = 0; e < 2; ++e) w[e] = 2 * tid + e < n ? weight((uint32_t)(s.ranked[2 * tid + e] >> 32)) : 0;
-    before[0] = sample_scan(w[0] + w[1], s, total);
-    before[1] = before[0] + w[0];
-    bool in[2];
-    const double limit = (double)draw.p * (draw.k ? (double)total : sum);
-    if (draw.p < 1.f && !draw.k && (double)total < limit) return false;  // (uniform)
-    u64 mine = 0;
-    for (int e = 0; e < 2; ++e) {
-        const int i = 2 * tid + e;
-        in[e] = i < n && (!(draw.p < 1.f) || i == 0 || (double)before[e] < limit) && w[e] >= draw.least && w[e] > 0;
-        mine += in[e] ? 1 : 0;
-    }
-    // in the vocabulary's order: the sums up to each kept entry (kept ones are the first `kept`)
-    u64 kept;
-    sample_scan(mine, s, kept);
-    for (int e = 0; e < 2; ++e)
-        if (in[e]) s.list[2 * tid + e] = w[e];
     __syncthreads();
-    u64 kept_sum;
-    sample_scan((in[0] ? w[0] : 0) + (in[1] ? w[1] : 0), s, kept_sum);
-    const u64 mark = draw.mark(kept_sum);
-    const int shares = kept <= 64 ? 16 : kept <= 128 ? 8 : kept <= 256 ? 4 : kept <= 512 ? 2 : 1;
-    for (int i = tid / shares; i < (int)kept; i += kSampleThreads / shares) {
-        const uint32_t at = (uint32_t)s.ranked[i];  // ~place
-        u64 front = 0;
-        for (int j = tid % shares; j < (int)kept; j += shares) front += (uint32_t)s.ranked[j] > at ? s.list[j] : 0;
-        for (int d = 1; d < shares; d <<= 1) front += __shfl_xor(front, d);
-        const u64 here = s.list[i];
-        if (tid % shares == 0 && mark >= front && mark < front + here)
-            sample_answer(a, r, (int)~at, log((double)here / (double)kept_sum));
+    for (int i = tid; i < n; i += kSampleThreads) s.weight[i] = weight((uint32_t)(s.list[i] >> 32));
+    __syncthreads();
+    u64 from = 0, total = 0;  // kept are the entries from `from` on
+    if (draw.k && draw.k < n) from = sample_list_select(n, 0, (double)draw.k, 0, s, [](int) { return (u64)1; });
+    if (draw.p < 1.f) {
+        u64 mine = 0;
+        for (int i = tid; i < n; i += kSampleThreads) mine += s.list[i] >= from ? s.weight[i] : 0;
+        sample_scan(mine, s.part, total);
+        const double limit = fmax((double)draw.p * (draw.k ? (double)total : sum), 0.5);  // the first is always kept
+        if (!draw.k && (double)total < limit) return false;  // (uniform)
+        from = sample_list_select(n, from, limit, 0, s, [&](int i) { return s.weight[i]; });
+    }
+    // in the vocabulary's order: the kept weights of equal stretches of it, the stretch where their sum passes the mark, its entries
+    const int width = (a.n_vocab - 1) >> 11, shift = width ? 32 - __builtin_clz(width) : 0;
+    auto kept = [&](int i) -> u64 { return s.list[i] >= from && s.weight[i] >= draw.least ? s.weight[i] : 0; };
+    sample_clear(s);
+    u64 mine = 0;
+    for (int i = tid; i < n; i += kSampleThreads) {
+        const u64 w = kept(i);
+        mine += w;
+        if (w) atomicAdd(&s.hist[~(uint32_t)s.list[i] >> shift], w);
+    }
+    if (tid == 0) s.n_few = 0;
+    sample_scan(mine, s.part, total);
+    const u64 mark = draw.mark(total);
+    u64 front;
+    const uint32_t stretch = (uint32_t)sample_bin<kSampleBins, kSampleThreads>(s.hist, s.part, s.result, 0, front, [=](u64 x) { return x <= mark; });
+    for (int i = tid; i < n; i += kSampleThreads)
+        if (kept(i) && ~(uint32_t)s.list[i] >> shift == stretch) s.few[atomicAdd(&s.n_few, 1)] = (uint16_t)i;
+    __syncthreads();
+    static_assert(kSampleFew >= kMaxVocab / kSampleBins, "a stretch's entries");
+    const int few = s.n_few, e = tid / 4;
+    if (e < few) {
+        const uint32_t at = (uint32_t)s.list[s.few[e]];  // ~place
+        u64 before = 0;
+        for (int j = tid % 4; j < few; j += 4) before += (uint32_t)s.list[s.few[j]] > at ? s.weight[s.few[j]] : 0;
+        before += __shfl_xor(before, 1);
+        before += __shfl_xor(before, 2);
+        const u64 here = s.weight[s.few[e]];
+        if (tid % 4 == 0 && mark >= front + before && mark < front + before + here)
+            sample_answer(a, r, (int)~at, log((double)here / (double)total));
     }
     return true;
+}
+
+// The place where the sum of the kept weights of COUNT logits, `first` on, passes the mark.
+template <int COUNT, class T>
+__device__ inline void sample_from_part(const SampleArgs &a, int r, const T *row, int first, u64 mark, double total, SampleShared &s,
+                                        const SampleDraw &draw, const SampleKept &kept, const SampleWeight &weight)
+{
+    constexpr int EACH = COUNT / kSampleThreads;
+    const int i = first + (int)threadIdx.x * EACH;
+    u64 w[EACH], sum = 0, unused;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        w[j] = 0;
+        if (i + j < a.n_vocab) {
+            const uint32_t key = sample_key(SampleRow<T>::one(row + i + j));
+            const u64 x = kept(key, i + j) ? weight(key) : 0;
+            w[j] = x >= draw.least ? x : 0;
+        }
+        sum += w[j];
+    }
+    u64 before = sample_scan(sum, s.part, unused);
+    if (mark >= before && mark < before + sum) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+            if (mark >= before && mark < before + w[j]) sample_answer(a, r, i + j, log((double)w[j] / total));
+            before += w[j];
+        }
+    }
 }
 
 // Draws from all that the threshold and min-p keep: the kept weights of each part of the row, then the part, the thread and the place
@@ -430,41 +684,22 @@ __device__ inline void sample_from_row(const SampleArgs &a, int r, const T *row,
     __syncthreads();
     if (tid < parts) s.tile[tid] = 0;
     __syncthreads();
-    auto kept_weight = [&](uint32_t key, int i) -> u64 {
-        if (i >= n || !kept(key, i)) return 0;
-        const u64 w = weight(key);
-        return w >= draw.least ? w : 0;
-    };
     for (int part = 0; part < parts; ++part) {
         const int i = part * PART + tid * VEC;
         uint32_t x[VEC];
         sample_keys(row, i, n, x);
         u64 sum = 0;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) sum += kept_weight(x[j], i + j);
+        for (int j = 0; j < VEC; ++j) {
+            const u64 w = i + j < n && kept(x[j], i + j) ? weight(x[j]) : 0;
+            sum += w >= draw.least ? w : 0;
+        }
         sum = sample_wave_sum(sum);
         if ((tid & 63) == 0 && sum) atomicAdd(&s.tile[part], sum);
     }
     __syncthreads();
-    u64 total = 0;
-    for (int i = 0; i < parts; ++i) total += s.tile[i];
-    u64 mark = draw.mark(total);
-    int part = 0;
-    while (mark >= s.tile[part]) mark -= s.tile[part++];
-    const int i = part * PART + tid * VEC;
-    uint32_t x[VEC];
-    sample_keys(row, i, n, x);
-    u64 w[VEC], sum = 0, unused;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) sum += w[j] = kept_weight(x[j], i + j);
-    u64 before = sample_scan(sum, s, unused);
-    if (mark >= before && mark < before + sum) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            if (mark >= before && mark < before + w[j]) sample_answer(a, r, i + j, log((double)w[j] / (double)total));
-            before += w[j];
-        }
-    }
+    const SamplePart at = sample_part(s.tile, parts, [&](u64 total) { return draw.mark(total); });
+    sample_from_part<PART>(a, r, row, at.part * PART, at.mark, (double)at.total, s, draw, kept, weight);
 }
 
 // Lane i: tile i's share of the sum of all weights, in units of the largest one's 2^-44.
@@ -480,7 +715,7 @@ template <class T>
 __device__ inline void sample_from_tiles(const SampleArgs &a, int r, const T *row, const SampleDraw &draw, const SampleWeight &against,
                                          SampleShared &s)
 {
-    const int n = a.n_vocab, tid = threadIdx.x, lane = tid & 63, tiles = (n + kSampleTile - 1) / kSampleTile;
+    const int n = a.n_vocab, lane = threadIdx.x & 63, tiles = (n + kSampleTile - 1) / kSampleTile;
     const double sum = sample_tile_sum(a, r, against);
     double up_to = sum;  // the sums up to the lane's tile
 #pragma unroll
@@ -493,139 +728,74 @@ __device__ inline void sample_from_tiles(const SampleArgs &a, int r, const T *ro
     const int tile = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
     const double here = __shfl(sum, tile), front = __shfl(up_to, tile) - here;
     const uint32_t tile_key = a.tile_max[(size_t)r * tiles + tile];
-    const double unit = against.exact(tile_key) / kSampleUnit;
-    const SampleWeight weight(s.table, tile_key, draw.t);
-    const int i = tile * kSampleTile + tid * 4;
-    u64 w[4], mine = 0, all;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) mine += w[j] = i + j < n ? weight(sample_key(SampleRow<T>::one(row + i + j))) : 0;
-    u64 before = sample_scan(mine, s, all);
+    const u64 all = a.tile_sum[(size_t)r * tiles + tile];
     const u64 at = min((u64)(fmin(fmax((mark - front) / here, 0.0), 1.0) * (double)all), all - 1);
-    if (at >= before && at < before + mine) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (at >= before && at < before + w[j]) sample_answer(a, r, i + j, log((double)w[j] * unit / total));
-            before += w[j];
-        }
-    }
+    sample_from_part<kSampleTile>(a, r, row, tile * kSampleTile, at, total * kSampleUnit / against.exact(tile_key), s, draw,
+                                  SampleKept{0, n}, SampleWeight(s.table, tile_key, draw.t));
 }
 
-// The threshold of top-p alone: the bin of (M - l) / t in which the sum passes the limit, and in it the last logit with less than the limit
-// in front.
+// Top-k, and top-p behind it or alone, over the whole row.  limit: top-p's, where it is alone.
 template <class T>
-__device__ inline SampleKept sample_nucleus(const T *row, int n, const SampleWeight &weight, float t, double limit, SampleShared &s)
-{
-    const int tid = threadIdx.x;
-    const float max = sample_logit(weight.max_key), step = 64.f / t;
-    auto bin = [&](uint32_t k) -> int {
-        return k == weight.max_key ? 0 : (int)fminf((max - sample_logit(k)) * step, (float)(kSampleBins - 1));
-    };
-    sample_clear(s);
-    sample_each(row, n, [&](uint32_t k, int) {
-        const u64 w = weight(k);
-        if (w) atomicAdd(&s.hist[bin(k)], w);
-    });
-    __syncthreads();
-    u64 front;
-    const int b = sample_bin(limit, 0, s, front);
-    if (tid == 0) s.count = 0;
-    __syncthreads();
-    sample_each(row, n, [&](uint32_t k, int i) {
-        if (bin(k) == b) sample_append(s, k, i);
-    });
-    __syncthreads();
-    const int count = s.count;
-    if (count <= kSampleList) {
-        sample_rank(s, count);
-        u64 w[2], unused;
-        for (int e = 0; e < 2; ++e) w[e] = 2 * tid + e < count ? weight((uint32_t)(s.ranked[2 * tid + e] >> 32)) : 0;
-        const u64 before = front + sample_scan(w[0] + w[1], s, unused);
-        // the last with less than the limit in front; the bin's first has
-        if (tid == 0) s.result[3] = 0;
-        __syncthreads();
-        u64 mine = 0;
-        if (w[0] && (double)before < limit) mine = 2 * tid;
-        if (w[1] && (double)(before + w[0]) < limit) mine = 2 * tid + 1;
-        if (mine) atomicMax(&s.result[3], mine);
-        __syncthreads();
-        const u64 last = s.ranked[s.result[3]];
-        return SampleKept{(uint32_t)(last >> 32), (int)~(uint32_t)last};
-    }
-    SampleKept kept{0, n};
-    uint32_t key;
-    u64 before;
-    sample_select<true>(row, n, kept, weight, limit, s, key, before);
-    // of its equals those with less than the limit in front: one, and each further one
-    const u64 w = weight(key);
-    u64 more = 1;
-    for (u64 by = (u64)1 << 18; by; by >>= 1)
-        if ((double)(before + (more + by - 1) * w) < limit) more += by;
-    return SampleKept{key, sample_place(row, n, key, more, s)};
-}
-
-// Top-k, and top-p behind it, over the whole row.
-template <class T>
-__device__ inline SampleKept sample_first_k(const T *row, int n, const SampleWeight &weight, int k, float p, SampleShared &s)
+__device__ inline SampleKept sample_whole_row(const T *row, int n, const SampleWeight &weight, const SampleDraw &draw, double limit,
+                                              SampleShared &s)
 {
     SampleKept kept{0, n};
     uint32_t key;
     u64 before;
-    sample_select<false>(row, n, kept, weight, (double)k, s, key, before);
-    kept.last = sample_place(row, n, key, (u64)k - before, s);
-    kept.key = key;
-    if (!(p < 1.f)) return kept;
-    u64 sum = 0, total;
-    sample_each(row, n, [&](uint32_t x, int i) { sum += kept(x, i) ? weight(x) : 0; });
-    sample_scan(sum, s, total);
-    const double limit = fmax((double)p * (double)total, 0.5);  // the first is always kept
+    if (draw.k) {
+        sample_select<false>(row, n, kept, weight, (double)draw.k, s, key, before);
+        kept.last = sample_place(row, n, key, (u64)draw.k - before, s);
+        kept.key = key;
+    }
+    if (!(draw.p < 1.f)) return kept;
+    if (draw.k) {
+        u64 sum = 0, total;
+        sample_each(row, n, [&](uint32_t x, int i) { sum += kept(x, i) ? weight(x) : 0; });
+        sample_scan(sum, s.part, total);
+        limit = fmax((double)draw.p * (double)total, 0.5);  // the first is always kept
+    }
     sample_select<true>(row, n, kept, weight, limit, s, key, before);
-    const u64 w = weight(key);
-    u64 more = 1;
-    for (u64 by = (u64)1 << 18; by; by >>= 1)
-        if ((double)(before + (more + by - 1) * w) < limit) more += by;
-    const int last = sample_place(row, n, key, more, s);
+    const int last = sample_mass_place(row, n, key, weight(key), before, limit, s);
     return SampleKept{key, key == kept.key ? min(kept.last, last) : last};
 }
 
 template <class T>
 __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a)
 {
-    constexpr int VEC = SampleRow<T>::VEC, GL = kSampleGroup / VEC, EACH = kMaxVocab / kSampleGroup / kSampleThreads;
+    constexpr int VEC = SampleRow<T>::VEC, GL = kSampleGroup / VEC, EACH = kMaxVocab / kSampleGroup / kSampleThreads, AHEAD = 4;
     __shared__ SampleShared s;
     const int r = blockIdx.x, n = a.n_vocab, tid = threadIdx.x, groups = (n + kSampleGroup - 1) / kSampleGroup;
     const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.stride;
     if (tid < 64) s.table[tid] = kSampleTable[tid];
+    const SampleDraw draw(a, r);
 
     // the groups' maxima; the largest, in the first group that has it, and the lowest that is a number
-    uint32_t most[EACH], low = ~0u;
+    uint32_t most[EACH], low = 0;  // ~ the lowest
     u64 best = 0;
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
         const int g = tid + e * kSampleThreads;
         most[e] = g < groups ? a.group_max[(size_t)r * groups + g] : kNoLogit;
-        const u64 x = (u64)most[e] << 32 | (uint32_t)~g;
-        best = x > best ? x : best;
-        if (most[e] > kNoLogit) low = min(low, most[e]);
     }
 #pragma unroll
-    for (int d = 32; d; d >>= 1) {
-        const u64 x = __shfl_xor(best, d);
+    for (int e = 0; e < EACH; ++e) {
+        const u64 x = (u64)most[e] << 32 | (uint32_t)~(tid + e * kSampleThreads);
         best = x > best ? x : best;
-        low = min(low, (uint32_t)__shfl_xor((int)low, d));
+        if (most[e] > kNoLogit) low = max(low, ~most[e]);
     }
+    best = sample_wave_max(best);
+    low = sample_wave_max(low);
     if ((tid & 63) == 0) {
         s.part[tid >> 6] = best;
-        s.tile[tid >> 6] = low;
+        s.part[kSampleWaves + (tid >> 6)] = low;
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kSampleWaves; ++i) {
         best = s.part[i] > best ? s.part[i] : best;
-        low = min(low, (uint32_t)s.tile[i]);
+        low = max(low, (uint32_t)s.part[kSampleWaves + i]);
     }
     const uint32_t max_key = (uint32_t)(best >> 32);
-    SampleDraw draw;
-    draw.t = a.temperature ? a.temperature[r] : 1.f;
     if (max_key == kNoLogit || !(draw.t > 0.f)) {
         if (max_key == kNoLogit) {
             if (tid == 0) {
@@ -640,12 +810,6 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
         return;
     }
     const SampleWeight weight(s.table, max_key, draw.t);
-    const float min_p = a.min_p ? a.min_p[r] : 0.f;
-    draw.p = a.top_p ? a.top_p[r] : 1.f;
-    draw.u = a.u[r];
-    draw.k = a.top_k ? a.top_k[r] : 0;
-    if (draw.k < 0 || draw.k >= n) draw.k = 0;
-    draw.least = min_p > 0.f ? (u64)ceil(fmin((double)min_p, 1.0) * kSampleUnit) : 0;
     const bool nucleus = draw.p < 1.f && !draw.k;
     if (!draw.k && !nucleus && !draw.least) {
         sample_from_tiles(a, r, row, draw, weight, s);
@@ -654,16 +818,20 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
 
     // the list of the logits above a bound that is below the threshold
     double sum = nucleus ? sample_tile_sum(a, r, weight) : 0;
+    if (nucleus) {
 #pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    const float max = sample_logit(max_key), range = max - sample_logit(low);
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    }
+    const double limit = fmax((double)draw.p * sum, 0.5);
+    const float top = sample_logit(max_key), range = top - sample_logit(~low);
     const bool by_rank = draw.k || nucleus;
     int bound = 0;
     const float step = range > 0.f ? (kSampleBins - 1) / range : 0.f;
-    auto bin = [&](uint32_t k) -> int { return (int)fminf((max - sample_logit(k)) * step, (float)(kSampleBins - 1)); };
+    auto bin = [&](uint32_t k) -> int { return (int)fminf((top - sample_logit(k)) * step, (float)(kSampleBins - 1)); };
     auto above = [&](uint32_t k) -> bool { return k > kNoLogit && (by_rank ? bin(k) <= bound : weight(k) >= draw.least); };
-    bool listed = !by_rank || (range < 3e38f && step < 3e38f && draw.k <= groups);  // (uniform)
+    const bool listed = !by_rank || (range < 3e38f && step < 3e38f && draw.k <= groups);  // (uniform)
     if (listed) {
+        if (tid == 0) s.count = s.n_few = 0;
         if (by_rank) {
             sample_clear(s);
 #pragma unroll
@@ -671,51 +839,244 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
                 if (most[e] > kNoLogit) atomicAdd(&s.hist[bin(most[e])], 1ull);
             __syncthreads();
             u64 unused;
-            bound = sample_bin((double)(draw.k ? draw.k : 256), 0, s, unused);
+            bound = sample_bin((double)(draw.k ? draw.k : kSampleFirst), 0, s, unused);
+        } else {
+            __syncthreads();
         }
-        if (tid == 0) s.count = 0;
-        __syncthreads();
 #pragma unroll
         for (int e = 0; e < EACH; ++e)
-            if (above(most[e])) s.groups[atomicAdd(&s.count, 1)] = (uint16_t)(tid + e * kSampleThreads);
+            if (above(most[e])) s.groups[atomicAdd(&s.n_few, 1)] = (uint16_t)(tid + e * kSampleThreads);
         __syncthreads();
-        const int picked = s.count;
-        __syncthreads();
-        if (tid == 0) s.count = 0;
-        __syncthreads();
-        for (int e = tid; e < picked * GL; e += kSampleThreads) {
-            const int i = s.groups[e / GL] * kSampleGroup + e % GL * VEC;
-            uint32_t x[VEC];
-            sample_keys(row, i, n, x);
+        const int picked = s.n_few;
+        for (int e0 = 0; e0 < picked * GL; e0 += AHEAD * kSampleThreads) {  // AHEAD loads of a thread on their way
+            uint32_t w[AHEAD][4];
+            int place[AHEAD];
 #pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (above(x[j])) sample_append(s, x[j], i + j);  // (past the row's end: kNoLogit)
+            for (int e = 0; e < AHEAD; ++e) {
+                const int at = e0 + e * kSampleThreads + tid;
+                place[e] = at < picked * GL ? s.groups[at / GL] * kSampleGroup + at % GL * VEC : n;
+                sample_load(row, max(0, min(place[e], n - VEC)), n, n >= VEC, w[e]);
+            }
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                if (place[e] + VEC > n) sample_load(row, place[e], n, false, w[e]);
+                uint32_t x[VEC], take = 0;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    x[j] = sample_key(SampleRow<T>::get(w[e], j));
+                    take |= above(x[j]) ? 1u << j : 0;  // (past the row's end: kNoLogit)
+                }
+                sample_append(s.list, &s.count, take, x, place[e]);
+            }
         }
         __syncthreads();
         const int count = s.count;
         // (fewer groups than k: a logit below all of them may be among the first k)
-        if (picked >= draw.k && count <= kSampleList && sample_from_list(a, r, draw, weight, count, sum, s)) return;
+        if (picked >= draw.k && count <= kSampleList &&
+            (count <= 64 ? sample_from_few(a, r, draw, weight, count, sum, s) : sample_from_list(a, r, draw, weight, count, sum, s)))
+            return;
         __syncthreads();
     }
-    SampleKept kept{0, n};
-    if (draw.k)
-        kept = sample_first_k(row, n, weight, draw.k, draw.p, s);
-    else if (nucleus)
-        kept = sample_nucleus(row, n, weight, draw.t, fmax((double)draw.p * sum, 0.5), s);
+    if (nucleus && a.max_left > 0) {  // to be shared by many blocks, where there is a place left
+        if (tid == 0) {
+            const int at = atomicAdd(a.n_left, 1);
+            s.count = at;
+            if (at < a.max_left) a.left[at] = SampleLeft{limit, 0, r, max_key, 0, 0};
+        }
+        __syncthreads();
+        if (s.count < a.max_left) return;
+        __syncthreads();
+    }
+    const SampleKept kept = by_rank ? sample_whole_row(row, n, weight, draw, limit, s) : SampleKept{0, n};
     sample_from_row(a, r, row, draw, kept, weight, s);
+}
+
+// The rows that are left: block c of the a.shares of a row takes every a.shares-th tile of it.
+struct SampleShare {
+    const SampleLeft *left;
+    int share;
+    bool on;
+    __device__ inline explicit SampleShare(const SampleArgs &a)
+    {
+        const int at = (int)blockIdx.x / a.shares;
+        share = (int)blockIdx.x - at * a.shares;
+        on = at < min(*a.n_left, a.max_left);
+        left = a.left + at;
+    }
+};
+
+// (M - l) / t in bins of 1/32 (a weight of more than 2^-45 is in the first 999).
+struct SampleNucleusBin {
+    float max, step;
+    __device__ inline SampleNucleusBin(uint32_t max_key, float t) : max(sample_logit(max_key)), step(32.f / t) {}
+    __device__ inline int operator()(float x) const { return x == max ? 0 : (int)fminf((max - x) * step, (float)(kSampleLeftBins - 1)); }
+};
+
+// f(logits, place of the first) for the tiles of a share, all of a wave's lanes at once (those past the row's end: -inf).
+template <class T, class F, class G>
+__device__ inline void sample_share_tiles(const SampleArgs &a, int r, int share, F &&f, G &&after)
+{
+    using R = SampleRow<T>;
+    constexpr int VEC = R::VEC, LOADS = kSampleTile / (256 * VEC);
+    const int n = a.n_vocab, tiles = (n + kSampleTile - 1) / kSampleTile;
+    const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.stride;
+    for (int tile = share; tile < tiles; tile += a.shares) {
+        const int i0 = tile * kSampleTile + (int)threadIdx.x * VEC;
+        uint32_t w[LOADS][4];
+        if ((tile + 1) * kSampleTile <= n) {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) sample_load(row, i0 + j * 256 * VEC, n, true, w[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) sample_load(row, i0 + j * 256 * VEC, n, false, w[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            float x[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[i] = R::get(w[j], i);
+            f(x, i0 + j * 256 * VEC);
+        }
+        after(tile);
+    }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void sample_hist_kernel(SampleArgs a)
+{
+    constexpr int VEC = SampleRow<T>::VEC;
+    __shared__ double table[64];
+    __shared__ u64 hist[kSampleLeftBins];
+    const SampleShare mine(a);
+    if (!mine.on) return;
+    const int tid = threadIdx.x, r = mine.left->row;
+    const uint32_t max_key = mine.left->max_key;
+    if (tid < 64) table[tid] = kSampleTable[tid];
+    for (int i = tid; i < kSampleLeftBins; i += 256) hist[i] = 0;
+    __syncthreads();
+    const float t = a.temperature ? a.temperature[r] : 1.f;
+    const SampleWeight weight(table, max_key, t);
+    const SampleNucleusBin bin(max_key, t);
+    const float max = sample_logit(max_key);
+    sample_share_tiles<T>(
+        a, r, mine.share,
+        [&](const float(&x)[VEC], int) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const u64 w = x[j] == max ? (u64)kSampleUnit : weight.marked(x[j]) - SampleWeight::kMark;
+                if (w) atomicAdd(&hist[bin(x[j])], w);
+            }
+        },
+        [](int) {});
+    __syncthreads();
+    for (int i = tid; i < kSampleLeftBins; i += 256) a.hist[(size_t)blockIdx.x * kSampleLeftBins + i] = hist[i];
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a)
+{
+    constexpr int VEC = SampleRow<T>::VEC;
+    __shared__ double table[64];
+    __shared__ u64 hist[kSampleLeftBins];
+    __shared__ u64 part[4], result[2];
+    const SampleShare mine(a);
+    if (!mine.on) return;
+    const int tid = threadIdx.x, at = mine.left - a.left, r = mine.left->row, tiles = (a.n_vocab + kSampleTile - 1) / kSampleTile;
+    const uint32_t max_key = mine.left->max_key;
+    const double limit = mine.left->limit;
+    if (tid < 64) table[tid] = kSampleTable[tid];
+    for (int i = tid; i < kSampleLeftBins; i += 256) {
+        u64 sum = 0;
+        for (int c = 0; c < a.shares; ++c) sum += a.hist[((size_t)at * a.shares + c) * kSampleLeftBins + i];
+        hist[i] = sum;
+    }
+    __syncthreads();
+    u64 front;
+    const int border =
+        sample_bin<kSampleLeftBins, 256>(hist, part, result, 0, front, [=](u64 x) { return (double)x < limit; });
+    if (mine.share == 0 && tid == 0) a.left[at].front = front;
+    const SampleDraw draw(a, r);
+    const SampleWeight weight(table, max_key, draw.t);
+    const SampleNucleusBin bin(max_key, draw.t);
+    const float max = sample_logit(max_key);
+    u64 sum = 0;
+    sample_share_tiles<T>(
+        a, r, mine.share,
+        [&](const float(&x)[VEC], int i) {
+            uint32_t key[VEC], take = 0;
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const int b = bin(fmaxf(x[j], -INFINITY));  // (fmaxf drops a NaN)
+                if (b < border) {
+                    const u64 w = x[j] == max ? (u64)kSampleUnit : weight.marked(x[j]) - SampleWeight::kMark;
+                    sum += w >= draw.least ? w : 0;
+                }
+                take |= b == border ? 1u << j : 0;
+                key[j] = sample_key(x[j]);
+            }
+            sample_append(a.list + (size_t)at * kSampleList, &a.left[at].count, take, key, i);
+        },
+        [&](int tile) {
+            sum = sample_wave_sum(sum);
+            __syncthreads();
+            if ((tid & 63) == 0) part[tid >> 6] = sum;
+            __syncthreads();
+            if (tid == 0) a.tile_sum[(size_t)r * tiles + tile] = part[0] + part[1] + part[2] + part[3];
+            sum = 0;
+        });
+}
+
+template <class T>
+__global__ __launch_bounds__(kSampleThreads) void sample_left_kernel(SampleArgs a)
+{
+    __shared__ SampleShared s;
+    const int at = blockIdx.x, tid = threadIdx.x, n = a.n_vocab, tiles = (n + kSampleTile - 1) / kSampleTile;
+    if (at >= min(*a.n_left, a.max_left)) return;
+    const SampleLeft left = a.left[at];
+    const int r = left.row, count = left.count;
+    const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.stride;
+    if (tid < 64) s.table[tid] = kSampleTable[tid];
+    if (tid < tiles) s.tile[tid] = a.tile_sum[(size_t)r * tiles + tid];
+    __syncthreads();
+    const SampleDraw draw(a, r);
+    const SampleWeight weight(s.table, left.max_key, draw.t);
+    if (count > kSampleList) {
+        sample_from_row(a, r, row, draw, sample_whole_row(row, n, weight, draw, left.limit, s), weight, s);
+        return;
+    }
+    for (int i = tid; i < count; i += kSampleThreads) {
+        s.list[i] = a.list[(size_t)at * kSampleList + i];
+        s.weight[i] = weight((uint32_t)(s.list[i] >> 32));
+    }
+    __syncthreads();
+    const u64 last = sample_list_select(count, 0, left.limit, left.front, s, [&](int i) { return s.weight[i]; });
+    for (int i = tid; i < count; i += kSampleThreads)
+        if (s.list[i] >= last && s.weight[i] >= draw.least) atomicAdd(&s.tile[~(uint32_t)s.list[i] / kSampleTile], s.weight[i]);
+    __syncthreads();
+    const SamplePart in = sample_part(s.tile, tiles, [&](u64 total) { return draw.mark(total); });
+    sample_from_part<kSampleTile>(a, r, row, in.part * kSampleTile, in.mark, (double)in.total, s, draw,
+                                  SampleKept{(uint32_t)(last >> 32), (int)~(uint32_t)last}, weight);
+}
+
+template <class T>
+void launch_sample_type(const SampleArgs &a, hipStream_t s)
+{
+    const unsigned tiles = (a.n_vocab + kSampleTile - 1) / kSampleTile;
+    sample_scan_kernel<T><<<dim3(a.n_rows * tiles), dim3(256), 0, s>>>(a);
+    sample_row_kernel<T><<<dim3(a.n_rows), dim3(kSampleThreads), 0, s>>>(a);
+    if (a.max_left == 0) return;
+    sample_hist_kernel<T><<<dim3(a.max_left * a.shares), dim3(256), 0, s>>>(a);
+    sample_cut_kernel<T><<<dim3(a.max_left * a.shares), dim3(256), 0, s>>>(a);
+    sample_left_kernel<T><<<dim3(a.max_left), dim3(kSampleThreads), 0, s>>>(a);
 }
 
 inline hipError_t launch_sample_kernels(const SampleArgs &a, hipStream_t s)
 {
     if (a.n_rows <= 0) return hipSuccess;
-    const unsigned tiles = (a.n_vocab + kSampleTile - 1) / kSampleTile;
-    if (a.bf16) {
-        sample_scan_kernel<uint16_t><<<dim3(a.n_rows * tiles), dim3(256), 0, s>>>(a);
-        sample_row_kernel<uint16_t><<<dim3(a.n_rows), dim3(kSampleThreads), 0, s>>>(a);
-    } else {
-        sample_scan_kernel<float><<<dim3(a.n_rows * tiles), dim3(256), 0, s>>>(a);
-        sample_row_kernel<float><<<dim3(a.n_rows), dim3(kSampleThreads), 0, s>>>(a);
-    }
+    if (a.bf16)
+        launch_sample_type<uint16_t>(a, s);
+    else
+        launch_sample_type<float>(a, s);
     return hipGetLastError();
 }
 
