@@ -2448,9 +2448,9 @@ fka_status fka_tree_accept_paged(const fka_accept_desc *desc, const int32_t *par
 // Lays the workspace out (n_rows and n_vocab given); its bytes.
 static size_t sample_layout(fka::SampleArgs &a, char *at)
 {
-    const size_t R = a.n_rows, tiles = ceil_div(a.n_vocab, fka::kSampleTile), groups = ceil_div(a.n_vocab, fka::kSampleGroup);
+    const size_t R = a.n_rows, tiles = ceil_div(a.n_vocab, fka::kSampleTile), groups = ceil_div(a.n_vocab, fka::sample_group_of(a.n_vocab));
     a.max_left = std::min(a.n_rows, fka::kSampleMaxLeft);
-    a.shares = std::max(1, std::min((int32_t)tiles, 2048 / std::max(1, a.max_left)));
+    a.shares = std::max(1, std::min((int32_t)tiles, 4096 / std::max(1, a.max_left)));
     size_t bytes = 0;
     auto take = [&](auto *&p, size_t n) {
         using X = std::remove_reference_t<decltype(*p)>;
@@ -2527,7 +2527,7 @@ fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const flo
     a.logprob = logprob;
     a.err = err;
     sample_layout(a, static_cast<char *>(workspace));
-    if (!top_p) a.max_left = 0;
+    if (!top_p && !top_k && !min_p) a.max_left = 0;
     const hipError_t e = fka::launch_sample(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "sample kernel launch");
     return ok();

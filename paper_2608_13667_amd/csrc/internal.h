@@ -495,11 +495,13 @@ struct AcceptArgs {
     int32_t *err;                    // nullable
 };
 
-// The token that a row of logits gives (sample.h): logits of a group and of a tile, of which the scan leaves maxima and sums.
-constexpr int kSampleGroup = 64;
+// The token that a row of logits gives (sample.h): logits of a group and of a tile, of which the scan leaves maxima and sums, and the most
+// groups of a row.
 constexpr int kSampleTile = 4096;
+constexpr int kSampleGroups = 4096;
+__host__ __device__ inline int sample_group_of(int n_vocab) { return n_vocab <= 16 * kSampleGroups ? 16 : 64; }
 // Rows that several blocks share: most of them, bins of a histogram, entries of a list; the blocks of such a row are some
-// 2048 / rows, up to one to a tile.
+// 4096 / rows, up to one to a tile.
 constexpr int kSampleMaxLeft = 1024;
 constexpr int kSampleLeftBins = 1024;
 constexpr int kSampleList = 2048;
@@ -508,7 +510,11 @@ struct SampleLeft {
     unsigned long long front;  // in front of the bin that holds the threshold
     int32_t row;
     uint32_t max_key;
-    int32_t count, unused;     // entries of the list
+    int32_t count;             // entries of the list
+    // what is shared: the search of top-p's threshold, with min-p alone all logits, or the list of those with (M - l) step of at most `bound`
+    static constexpr int32_t kNucleus = -1, kAll = -2;
+    int32_t bound;
+    float step;
 };
 struct SampleArgs {
     const void *logits;      // [rows] of n_vocab fp32 or bf16, `stride` elements apart

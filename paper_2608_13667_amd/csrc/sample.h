@@ -7,7 +7,7 @@
 // than p of their sum in front of them.  So what is kept is one logit value, the threshold, and a place: everything above the value,
 // and of its equals those up to the place.  min-p is a bound on w itself.
 //
-// sample_scan_kernel reads the logits, all blocks at the rate of the memory: the largest of every 64 (a group), and of every 4096 (a
+// sample_scan_kernel reads the logits, all blocks at the rate of the memory: the largest of every 64 or 16 (a group), and of every 4096 (a
 // tile) also the sum of the weights against the tile's own largest, where the row needs a sum over all.
 // sample_row_kernel, a block to a row, then reads little more of it:
 //   * nothing filtered: the tiles' sums give the tile that the random number falls into, which is read;
@@ -15,7 +15,8 @@
 //     logit.  The groups that reach the bound are read and the logits above it listed, up to 2048, and filtered.  For top-p
 //     alone the bound is that of 128 groups, and the list will do if it has p of the sum;
 //   * where it has not, the row is left to three more kernels, in which many blocks share it: a histogram of the weights by
-//     (M - l) / t; the bin where their sum passes p, whose logits are listed, and the sums of each tile's logits above it; the draw;
+//     (M - l) / t; the bin where their sum passes p, whose logits are listed, and the sums of each tile's logits above it; the draw.
+//     So are rows of which more than 256 groups have to be read, for the list or, with min-p alone, the draw;
 //   * where a list does not fit (thousands of equal logits, a k in the thousands), the block goes over the row by itself: the threshold
 //     digit by digit of the logit's bits (11, 11, 10 from the top, as unsigned numbers in the logits' order), a histogram of each
 //     digit's values among what agrees in the digits before.
@@ -201,7 +202,7 @@ __device__ inline u64 sample_wave_sum(u64 x)
     return sample_last(sample_wave_scan(x, [](u64 a, u64 b) { return a + b; }));
 }
 
-// Largest of the lane's 16-byte neighbours in a group of 64 logits.
+// Largest over the LANES lanes of a group.
 template <int LANES>
 __device__ inline float sample_group_max(float x)
 {
@@ -209,23 +210,23 @@ __device__ inline float sample_group_max(float x)
         return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xf, 0xf, true)));
     };
     x = step(x, std::integral_constant<int, 0xb1>{});  // quad_perm 1,0,3,2
-    x = step(x, std::integral_constant<int, 0x4e>{});  // quad_perm 2,3,0,1
-    x = step(x, std::integral_constant<int, 0x141>{});  // row_half_mirror
+    if constexpr (LANES >= 4) x = step(x, std::integral_constant<int, 0x4e>{});  // quad_perm 2,3,0,1
+    if constexpr (LANES >= 8) x = step(x, std::integral_constant<int, 0x141>{});  // row_half_mirror
     if constexpr (LANES == 16) x = step(x, std::integral_constant<int, 0x140>{});  // row_mirror
     return x;
 }
 
 // A block takes a tile: its groups' maxima, its maximum and its sum.
-template <class T>
+template <class T, int GROUP>
 __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a)
 {
     using R = SampleRow<T>;
-    constexpr int VEC = R::VEC, LOADS = kSampleTile / (256 * VEC), GL = kSampleGroup / VEC;  // lanes of a group
+    constexpr int VEC = R::VEC, LOADS = kSampleTile / (256 * VEC), GL = GROUP / VEC;  // lanes of a group
     __shared__ double table[64];
     __shared__ uint32_t top[4];
     __shared__ u64 part[4];
     const int tid = threadIdx.x, n = a.n_vocab;
-    const int tiles = (n + kSampleTile - 1) / kSampleTile, groups = (n + kSampleGroup - 1) / kSampleGroup;
+    const int tiles = (n + kSampleTile - 1) / kSampleTile, groups = (n + GROUP - 1) / GROUP;
     const int r = blockIdx.x / tiles, tile = blockIdx.x - r * tiles, i0 = tile * kSampleTile + tid * VEC;
     const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.stride;
     if (blockIdx.x == 0 && tid == 0) *a.n_left = 0;
@@ -246,7 +247,7 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) m = fmaxf(m, R::get(w[j], i));
         m = sample_group_max<GL>(m);
-        const int g = (i0 + j * 256 * VEC) / kSampleGroup;
+        const int g = (i0 + j * 256 * VEC) / GROUP;
         if (tid % GL == 0 && g < groups) a.group_max[(size_t)r * groups + g] = sample_key(m);
         most = fmaxf(most, m);
     }
@@ -285,7 +286,7 @@ struct SampleShared {
     u64 hist[kSampleBins];
     u64 list[kSampleList], weight[kSampleList];  // (key << 32 | ~place): a larger one comes first
     uint16_t few[kSampleFew];
-    uint16_t groups[kMaxVocab / kSampleGroup];
+    uint16_t groups[kSampleGroups];
     u64 part[2 * kSampleWaves];
     u64 tile[kMaxVocab / (kSampleThreads * 4)];
     u64 result[4];
@@ -354,18 +355,12 @@ struct SampleKept {
     __device__ inline bool operator()(uint32_t k, int i) const { return k > key || (k == key && i <= last); }
 };
 
-// f(key, place) for every logit of the row.
+// f(key, place) for every logit of the row.  (One to a load: this is the way of rare rows, and wide loads make its code eight times as long.)
 template <class T, class F>
 __device__ inline void sample_each(const T *row, int n, F &&f)
 {
-    constexpr int VEC = SampleRow<T>::VEC;
-    for (int i = threadIdx.x * VEC; i < n; i += kSampleThreads * VEC) {
-        uint32_t k[VEC];
-        sample_keys(row, i, n, k);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            if (i + j < n) f(k[j], i + j);
-    }
+#pragma unroll 2
+    for (int i = threadIdx.x; i < n; i += kSampleThreads) f(sample_key(SampleRow<T>::one(row + i)), i);
 }
 
 // The last group of equal keys, among those that `kept` keeps, with less than `limit` in front of it (counts, or the sum of
@@ -394,21 +389,14 @@ __device__ inline void sample_select(const T *row, int n, const SampleKept &kept
 template <class T>
 __device__ inline int sample_place(const T *row, int n, uint32_t key, u64 r, SampleShared &s)
 {
-    constexpr int VEC = SampleRow<T>::VEC;
     u64 seen = 0;
-    for (int at = 0; at < n; at += kSampleThreads * VEC) {
-        const int i = at + threadIdx.x * VEC;
-        uint32_t k[VEC];
-        sample_keys(row, i, n, k);
-        u64 here = 0;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) here += i + j < n && k[j] == key;
+    for (int at = 0; at < n; at += kSampleThreads) {
+        const int i = at + threadIdx.x;
+        const bool here = i < n && sample_key(SampleRow<T>::one(row + i)) == key;
         u64 total;
-        u64 rank = seen + sample_scan(here, s.part, total);
+        const u64 rank = seen + sample_scan((u64)here, s.part, total);
         if (seen + total >= r) {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j)
-                if (i + j < n && k[j] == key && ++rank == r) s.result[2] = (u64)(i + j);
+            if (here && rank + 1 == r) s.result[2] = (u64)i;
             __syncthreads();
             return (int)s.result[2];
         }
@@ -679,19 +667,17 @@ template <class T>
 __device__ inline void sample_from_row(const SampleArgs &a, int r, const T *row, const SampleDraw &draw, const SampleKept &kept,
                                        const SampleWeight &weight, SampleShared &s)
 {
-    constexpr int VEC = SampleRow<T>::VEC, PART = kSampleThreads * VEC;
+    constexpr int PART = kSampleThreads * 4;
     const int n = a.n_vocab, tid = threadIdx.x, parts = (n + PART - 1) / PART;
     __syncthreads();
     if (tid < parts) s.tile[tid] = 0;
     __syncthreads();
     for (int part = 0; part < parts; ++part) {
-        const int i = part * PART + tid * VEC;
-        uint32_t x[VEC];
-        sample_keys(row, i, n, x);
         u64 sum = 0;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const u64 w = i + j < n && kept(x[j], i + j) ? weight(x[j]) : 0;
+#pragma unroll 1
+        for (int i = part * PART + tid; i < min(n, (part + 1) * PART); i += kSampleThreads) {
+            const uint32_t key = sample_key(SampleRow<T>::one(row + i));
+            const u64 w = kept(key, i) ? weight(key) : 0;
             sum += w >= draw.least ? w : 0;
         }
         sum = sample_wave_sum(sum);
@@ -759,12 +745,26 @@ __device__ inline SampleKept sample_whole_row(const T *row, int n, const SampleW
     return SampleKept{key, key == kept.key ? min(kept.last, last) : last};
 }
 
-template <class T>
+// Leaves the row to many blocks, where there is a place.
+__device__ inline bool sample_leave(const SampleArgs &a, SampleShared &s, const SampleLeft &left)
+{
+    if (a.max_left == 0) return false;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int at = atomicAdd(a.n_left, 1);
+        s.result[0] = (u64)(at < a.max_left);
+        if (at < a.max_left) a.left[at] = left;
+    }
+    __syncthreads();
+    return s.result[0] != 0;
+}
+
+template <class T, int GROUP>
 __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a)
 {
-    constexpr int VEC = SampleRow<T>::VEC, GL = kSampleGroup / VEC, EACH = kMaxVocab / kSampleGroup / kSampleThreads, AHEAD = 4;
+    constexpr int VEC = SampleRow<T>::VEC, GL = GROUP / VEC, EACH = kSampleGroups / kSampleThreads, AHEAD = 4;
     __shared__ SampleShared s;
-    const int r = blockIdx.x, n = a.n_vocab, tid = threadIdx.x, groups = (n + kSampleGroup - 1) / kSampleGroup;
+    const int r = blockIdx.x, n = a.n_vocab, tid = threadIdx.x, groups = (n + GROUP - 1) / GROUP;
     const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.stride;
     if (tid < 64) s.table[tid] = kSampleTable[tid];
     const SampleDraw draw(a, r);
@@ -803,8 +803,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
                 if (a.err) atomicOr(a.err, kErrNoToken);
             }
         } else if (tid < 64) {
-            const int i = (int)~(uint32_t)best * kSampleGroup + tid;
-            const u64 equal = __builtin_amdgcn_ballot_w64(i < n && sample_key(SampleRow<T>::one(row + min(i, n - 1))) == max_key);
+            const int i = (int)~(uint32_t)best * GROUP + tid;
+            const u64 equal = __builtin_amdgcn_ballot_w64(tid < GROUP && i < n && sample_key(SampleRow<T>::one(row + min(i, n - 1))) == max_key);
             if (tid == 0) sample_answer(a, r, i + __builtin_ctzll(equal), 0.0);
         }
         return;
@@ -848,13 +848,16 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
             if (above(most[e])) s.groups[atomicAdd(&s.n_few, 1)] = (uint16_t)(tid + e * kSampleThreads);
         __syncthreads();
         const int picked = s.n_few;
+        if (picked > kSampleFirst * 2 && !nucleus && picked >= draw.k &&
+            sample_leave(a, s, SampleLeft{limit, 0, r, max_key, 0, by_rank ? bound : SampleLeft::kAll, step}))
+            return;
         for (int e0 = 0; e0 < picked * GL; e0 += AHEAD * kSampleThreads) {  // AHEAD loads of a thread on their way
             uint32_t w[AHEAD][4];
             int place[AHEAD];
 #pragma unroll
             for (int e = 0; e < AHEAD; ++e) {
                 const int at = e0 + e * kSampleThreads + tid;
-                place[e] = at < picked * GL ? s.groups[at / GL] * kSampleGroup + at % GL * VEC : n;
+                place[e] = at < picked * GL ? s.groups[at / GL] * GROUP + at % GL * VEC : n;
                 sample_load(row, max(0, min(place[e], n - VEC)), n, n >= VEC, w[e]);
             }
 #pragma unroll
@@ -877,16 +880,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
             return;
         __syncthreads();
     }
-    if (nucleus && a.max_left > 0) {  // to be shared by many blocks, where there is a place left
-        if (tid == 0) {
-            const int at = atomicAdd(a.n_left, 1);
-            s.count = at;
-            if (at < a.max_left) a.left[at] = SampleLeft{limit, 0, r, max_key, 0, 0};
-        }
-        __syncthreads();
-        if (s.count < a.max_left) return;
-        __syncthreads();
-    }
+    if (nucleus && sample_leave(a, s, SampleLeft{limit, 0, r, max_key, 0, SampleLeft::kNucleus, 0.f})) return;
     const SampleKept kept = by_rank ? sample_whole_row(row, n, weight, draw, limit, s) : SampleKept{0, n};
     sample_from_row(a, r, row, draw, kept, weight, s);
 }
@@ -948,7 +942,7 @@ __global__ __launch_bounds__(256) void sample_hist_kernel(SampleArgs a)
     __shared__ double table[64];
     __shared__ u64 hist[kSampleLeftBins];
     const SampleShare mine(a);
-    if (!mine.on) return;
+    if (!mine.on || mine.left->bound != SampleLeft::kNucleus) return;
     const int tid = threadIdx.x, r = mine.left->row;
     const uint32_t max_key = mine.left->max_key;
     if (tid < 64) table[tid] = kSampleTable[tid];
@@ -978,22 +972,54 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a)
     constexpr int VEC = SampleRow<T>::VEC;
     __shared__ double table[64];
     __shared__ u64 hist[kSampleLeftBins];
-    __shared__ u64 part[4], result[2];
+    __shared__ u64 part[4], result[2], list[kSampleList];
+    __shared__ int count, base;
     const SampleShare mine(a);
     if (!mine.on) return;
     const int tid = threadIdx.x, at = mine.left - a.left, r = mine.left->row, tiles = (a.n_vocab + kSampleTile - 1) / kSampleTile;
     const uint32_t max_key = mine.left->max_key;
     const double limit = mine.left->limit;
+    const int bound = mine.left->bound;
+    if (tid == 0) count = 0;
+    auto pass_on = [&]() {
+        __syncthreads();
+        if (tid == 0) base = atomicAdd(&a.left[at].count, count);  // (one to a block: a wave's would be a round trip to memory each)
+        __syncthreads();
+        for (int i = tid; i < min(count, kSampleList); i += 256)
+            if (base + i < kSampleList) a.list[(size_t)at * kSampleList + base + i] = list[i];
+    };
+    if (bound >= 0) {  // the list of the logits up to a bound, as sample_row_kernel makes it
+        const float top = sample_logit(max_key), step = mine.left->step;
+        __syncthreads();
+        sample_share_tiles<T>(
+            a, r, mine.share,
+            [&](const float(&x)[VEC], int i) {
+                uint32_t key[VEC], take = 0;
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    key[j] = sample_key(x[j]);
+                    take |= key[j] > kNoLogit && (int)fminf((top - x[j]) * step, (float)(kSampleBins - 1)) <= bound ? 1u << j : 0;
+                }
+                sample_append(list, &count, take, key, i);
+            },
+            [](int) {});
+        pass_on();
+        return;
+    }
     if (tid < 64) table[tid] = kSampleTable[tid];
-    for (int i = tid; i < kSampleLeftBins; i += 256) {
-        u64 sum = 0;
-        for (int c = 0; c < a.shares; ++c) sum += a.hist[((size_t)at * a.shares + c) * kSampleLeftBins + i];
-        hist[i] = sum;
+    int border = kSampleLeftBins;
+    u64 front = 0;
+    if (bound == SampleLeft::kNucleus) {
+        for (int i = tid; i < kSampleLeftBins; i += 256) {
+            u64 sum = 0;
+#pragma unroll 8
+            for (int c = 0; c < a.shares; ++c) sum += a.hist[((size_t)at * a.shares + c) * kSampleLeftBins + i];
+            hist[i] = sum;
+        }
+        __syncthreads();
+        border = sample_bin<kSampleLeftBins, 256>(hist, part, result, 0, front, [=](u64 x) { return (double)x < limit; });
     }
     __syncthreads();
-    u64 front;
-    const int border =
-        sample_bin<kSampleLeftBins, 256>(hist, part, result, 0, front, [=](u64 x) { return (double)x < limit; });
     if (mine.share == 0 && tid == 0) a.left[at].front = front;
     const SampleDraw draw(a, r);
     const SampleWeight weight(table, max_key, draw.t);
@@ -1014,7 +1040,7 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a)
                 take |= b == border ? 1u << j : 0;
                 key[j] = sample_key(x[j]);
             }
-            sample_append(a.list + (size_t)at * kSampleList, &a.left[at].count, take, key, i);
+            sample_append(list, &count, take, key, i);
         },
         [&](int tile) {
             sum = sample_wave_sum(sum);
@@ -1024,6 +1050,7 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a)
             if (tid == 0) a.tile_sum[(size_t)r * tiles + tile] = part[0] + part[1] + part[2] + part[3];
             sum = 0;
         });
+    pass_on();
 }
 
 template <class T>
@@ -1036,11 +1063,11 @@ __global__ __launch_bounds__(kSampleThreads) void sample_left_kernel(SampleArgs 
     const int r = left.row, count = left.count;
     const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.stride;
     if (tid < 64) s.table[tid] = kSampleTable[tid];
-    if (tid < tiles) s.tile[tid] = a.tile_sum[(size_t)r * tiles + tid];
+    if (tid < tiles && left.bound < 0) s.tile[tid] = a.tile_sum[(size_t)r * tiles + tid];
     __syncthreads();
     const SampleDraw draw(a, r);
     const SampleWeight weight(s.table, left.max_key, draw.t);
-    if (count > kSampleList) {
+    if (count > kSampleList) {  // (not min-p alone)
         sample_from_row(a, r, row, draw, sample_whole_row(row, n, weight, draw, left.limit, s), weight, s);
         return;
     }
@@ -1048,8 +1075,14 @@ __global__ __launch_bounds__(kSampleThreads) void sample_left_kernel(SampleArgs 
         s.list[i] = a.list[(size_t)at * kSampleList + i];
         s.weight[i] = weight((uint32_t)(s.list[i] >> 32));
     }
+    if (left.bound >= 0) {
+        (void)sample_from_list(a, r, draw, weight, count, 0, s);  // (top-k: it holds all that is kept)
+        return;
+    }
     __syncthreads();
-    const u64 last = sample_list_select(count, 0, left.limit, left.front, s, [&](int i) { return s.weight[i]; });
+    u64 last = 0;  // (nothing listed: min-p alone)
+    if (left.bound == SampleLeft::kNucleus)
+        last = sample_list_select(count, 0, left.limit, left.front, s, [&](int i) { return s.weight[i]; });
     for (int i = tid; i < count; i += kSampleThreads)
         if (s.list[i] >= last && s.weight[i] >= draw.least) atomicAdd(&s.tile[~(uint32_t)s.list[i] / kSampleTile], s.weight[i]);
     __syncthreads();
@@ -1058,12 +1091,21 @@ __global__ __launch_bounds__(kSampleThreads) void sample_left_kernel(SampleArgs 
                                   SampleKept{(uint32_t)(last >> 32), (int)~(uint32_t)last}, weight);
 }
 
+template <class T, int GROUP>
+void launch_sample_group(const SampleArgs &a, hipStream_t s)
+{
+    const unsigned tiles = (a.n_vocab + kSampleTile - 1) / kSampleTile;
+    sample_scan_kernel<T, GROUP><<<dim3(a.n_rows * tiles), dim3(256), 0, s>>>(a);
+    sample_row_kernel<T, GROUP><<<dim3(a.n_rows), dim3(kSampleThreads), 0, s>>>(a);
+}
+
 template <class T>
 void launch_sample_type(const SampleArgs &a, hipStream_t s)
 {
-    const unsigned tiles = (a.n_vocab + kSampleTile - 1) / kSampleTile;
-    sample_scan_kernel<T><<<dim3(a.n_rows * tiles), dim3(256), 0, s>>>(a);
-    sample_row_kernel<T><<<dim3(a.n_rows), dim3(kSampleThreads), 0, s>>>(a);
+    if (sample_group_of(a.n_vocab) == 16)
+        launch_sample_group<T, 16>(a, s);
+    else
+        launch_sample_group<T, 64>(a, s);
     if (a.max_left == 0) return;
     sample_hist_kernel<T><<<dim3(a.max_left * a.shares), dim3(256), 0, s>>>(a);
     sample_cut_kernel<T><<<dim3(a.max_left * a.shares), dim3(256), 0, s>>>(a);
