@@ -667,17 +667,19 @@ template <class T>
 __device__ inline void sample_from_row(const SampleArgs &a, int r, const T *row, const SampleDraw &draw, const SampleKept &kept,
                                        const SampleWeight &weight, SampleShared &s)
 {
-    constexpr int PART = kSampleThreads * 4;
+    constexpr int VEC = SampleRow<T>::VEC, PART = kSampleThreads * VEC;
     const int n = a.n_vocab, tid = threadIdx.x, parts = (n + PART - 1) / PART;
     __syncthreads();
     if (tid < parts) s.tile[tid] = 0;
     __syncthreads();
     for (int part = 0; part < parts; ++part) {
+        const int i = part * PART + tid * VEC;
+        uint32_t x[VEC];
+        sample_keys(row, i, n, x);
         u64 sum = 0;
-#pragma unroll 1
-        for (int i = part * PART + tid; i < min(n, (part + 1) * PART); i += kSampleThreads) {
-            const uint32_t key = sample_key(SampleRow<T>::one(row + i));
-            const u64 w = kept(key, i) ? weight(key) : 0;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const u64 w = i + j < n && kept(x[j], i + j) ? weight(x[j]) : 0;
             sum += w >= draw.least ? w : 0;
         }
         sum = sample_wave_sum(sum);
@@ -718,6 +720,54 @@ __device__ inline void sample_from_tiles(const SampleArgs &a, int r, const T *ro
     const u64 at = min((u64)(fmin(fmax((mark - front) / here, 0.0), 1.0) * (double)all), all - 1);
     sample_from_part<kSampleTile>(a, r, row, tile * kSampleTile, at, total * kSampleUnit / against.exact(tile_key), s, draw,
                                   SampleKept{0, n}, SampleWeight(s.table, tile_key, draw.t));
+}
+
+// (M - l) / t in bins of 1/32 (a weight of more than 2^-45 is in the first 999).
+struct SampleNucleusBin {
+    float max, step;
+    __device__ inline SampleNucleusBin(uint32_t max_key, float t) : max(sample_logit(max_key)), step(32.f / t) {}
+    __device__ inline int operator()(float x) const { return x == max ? 0 : (int)fminf((max - x) * step, (float)(kSampleLeftBins - 1)); }
+};
+
+// The threshold of top-p alone, by one block: the histogram of the weights, the list of the bin where their sum passes the limit; false where
+// that does not fit.
+template <class T>
+__device__ inline bool sample_nucleus(const T *row, int n, const SampleWeight &weight, uint32_t max_key, float t, double limit,
+                                      SampleShared &s, SampleKept &kept)
+{
+    constexpr int VEC = SampleRow<T>::VEC, STEP = kSampleThreads * VEC;
+    const int tid = threadIdx.x;
+    const SampleNucleusBin bin(max_key, t);
+    sample_clear(s);
+    if (tid == 0) s.count = 0;
+    for (int i = tid * VEC; i < n; i += STEP) {
+        uint32_t x[VEC];
+        sample_keys(row, i, n, x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const u64 w = weight(x[j]);
+            if (w) atomicAdd(&s.hist[bin(sample_logit(x[j]))], w);
+        }
+    }
+    __syncthreads();
+    u64 front;
+    const int border = sample_bin(limit, 0, s, front);
+    for (int i0 = 0; i0 < n; i0 += STEP) {
+        const int i = i0 + tid * VEC;
+        uint32_t x[VEC], take = 0;
+        sample_keys(row, i, n, x);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) take |= x[j] > kNoLogit && bin(sample_logit(x[j])) == border ? 1u << j : 0;
+        sample_append(s.list, &s.count, take, x, i);
+    }
+    __syncthreads();
+    const int count = s.count;
+    if (count > kSampleList) return false;  // (uniform)
+    for (int i = tid; i < count; i += kSampleThreads) s.weight[i] = weight((uint32_t)(s.list[i] >> 32));
+    __syncthreads();
+    const u64 last = sample_list_select(count, 0, limit, front, s, [&](int i) { return s.weight[i]; });
+    kept = SampleKept{(uint32_t)(last >> 32), (int)~(uint32_t)last};
+    return true;
 }
 
 // Top-k, and top-p behind it or alone, over the whole row.  limit: top-p's, where it is alone.
@@ -848,7 +898,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
             if (above(most[e])) s.groups[atomicAdd(&s.n_few, 1)] = (uint16_t)(tid + e * kSampleThreads);
         __syncthreads();
         const int picked = s.n_few;
-        if (picked > kSampleFirst * 2 && !nucleus && picked >= draw.k &&
+        if (picked > 256 && !nucleus && picked >= draw.k &&
             sample_leave(a, s, SampleLeft{limit, 0, r, max_key, 0, by_rank ? bound : SampleLeft::kAll, step}))
             return;
         for (int e0 = 0; e0 < picked * GL; e0 += AHEAD * kSampleThreads) {  // AHEAD loads of a thread on their way
@@ -881,7 +931,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
         __syncthreads();
     }
     if (nucleus && sample_leave(a, s, SampleLeft{limit, 0, r, max_key, 0, SampleLeft::kNucleus, 0.f})) return;
-    const SampleKept kept = by_rank ? sample_whole_row(row, n, weight, draw, limit, s) : SampleKept{0, n};
+    SampleKept kept{0, n};
+    if (by_rank && !(nucleus && sample_nucleus(row, n, weight, max_key, draw.t, limit, s, kept)))
+        kept = sample_whole_row(row, n, weight, draw, limit, s);
     sample_from_row(a, r, row, draw, kept, weight, s);
 }
 
@@ -897,13 +949,6 @@ struct SampleShare {
         on = at < min(*a.n_left, a.max_left);
         left = a.left + at;
     }
-};
-
-// (M - l) / t in bins of 1/32 (a weight of more than 2^-45 is in the first 999).
-struct SampleNucleusBin {
-    float max, step;
-    __device__ inline SampleNucleusBin(uint32_t max_key, float t) : max(sample_logit(max_key)), step(32.f / t) {}
-    __device__ inline int operator()(float x) const { return x == max ? 0 : (int)fminf((max - x) * step, (float)(kSampleLeftBins - 1)); }
 };
 
 // f(logits, place of the first) for the tiles of a share, all of a wave's lanes at once (those past the row's end: -inf).
