@@ -1055,12 +1055,17 @@ __global__ __launch_bounds__(256) void sample_cut_kernel(SampleArgs a)
     int border = kSampleLeftBins;
     u64 front = 0;
     if (bound == SampleLeft::kNucleus) {
-        for (int i = tid; i < kSampleLeftBins; i += 256) {
-            u64 sum = 0;
+        // four bins a thread, the loads of several shares on their way at a time
+        static_assert(kSampleLeftBins == 4 * 256, "four bins a thread");
+        ulonglong2 sum[2] = {};
+        const ulonglong2 *from = reinterpret_cast<const ulonglong2 *>(a.hist + (size_t)at * a.shares * kSampleLeftBins) + 2 * tid;
 #pragma unroll 8
-            for (int c = 0; c < a.shares; ++c) sum += a.hist[((size_t)at * a.shares + c) * kSampleLeftBins + i];
-            hist[i] = sum;
+        for (int c = 0; c < a.shares; ++c) {
+            const ulonglong2 x = from[0], y = from[1];
+            from += kSampleLeftBins / 2;
+            sum[0].x += x.x, sum[0].y += x.y, sum[1].x += y.x, sum[1].y += y.y;
         }
+        hist[4 * tid] = sum[0].x, hist[4 * tid + 1] = sum[0].y, hist[4 * tid + 2] = sum[1].x, hist[4 * tid + 3] = sum[1].y;
         __syncthreads();
         border = sample_bin<kSampleLeftBins, 256>(hist, part, result, 0, front, [=](u64 x) { return (double)x < limit; });
     }
