@@ -96,6 +96,8 @@ def parse():
     ap.add_argument("--prefill-tokens", default="1,16,64", help="instruction tokens per branch to time")
     ap.add_argument("--lifecycle", action="store_true",
                     help="also time the fork lifecycle on the page pool (contiguous workloads' shapes)")
+    ap.add_argument("--draft", default="", help="also time steps with drafted trees of these many nodes a branch, such as 4,16,64 "
+                                                "(contiguous workloads' shapes)")
     return ap.parse_args()
 
 
@@ -336,6 +338,73 @@ def cpu_oracle(oracle, w, n_seq, hq, seconds):
     return {"value": v, "unit": "steps/s", "cores": cores, "kind": "oracle",
             "sample": f"{n} full decode steps (all {n_seq} x {hq} rows) at the initial lengths, fp64 on the host",
             "single_thread": {"value": v1, "unit": "steps/s", "cores": 1, "sample": f"{n1} full decode steps"}}
+
+
+def draft_timing(fa, torch, b, node_counts, trials, vocab=32000):
+    """One step with drafted trees at the workload's shape, for each count of nodes a branch: the layout, the nodes' rotation and
+    store, their attention over the prefix and suffixes, the choice of a token behind each node (top-k 50, top-p 0.9 over bf16 logits of
+    `vocab` words) and the acceptance, in one layer (the projections between them are the caller's model); and the attention by
+    itself.  HIP graphs over the workload's layer replicas, HIP events on the launch stream, the median of the trials."""
+    spec, w = b.spec, b.w
+    N, Hq, Hkv, d = w.n_branches, spec.n_q_heads, spec.n_kv_heads, spec.head_dim
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    freq = 1e6 ** (-torch.arange(0, d, 2, dtype=torch.float64, device="cuda") / d)
+    found = {}
+    for n in node_counts:
+        cap = int(w.suffix_len.max()) + n
+        parents = torch.tensor([[-1] + [max(0, i - 3) for i in range(1, n)]] * N, dtype=torch.int32, device="cuda")
+        masks, positions = torch.empty(N, n, dtype=torch.int64, device="cuda"), torch.empty(N, n, dtype=torch.int32, device="cuda")
+        rows = torch.randn(N, n, (Hq + 2 * Hkv) * d, generator=gen, device="cuda", dtype=torch.bfloat16)
+        q, k, v = (rows[..., a * d: z * d].unflatten(-1, (z - a, d)) for a, z in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+        q_out = torch.empty(N, n, Hq, d, dtype=torch.bfloat16, device="cuda")
+        suffixes = [tuple(torch.cat([r[x][:, :, :cap - n], torch.zeros(N, Hkv, n, d, dtype=torch.bfloat16, device="cuda")], 2).contiguous()
+                          for x in ("suffix_k", "suffix_v")) for r in b.reps]
+        lens, base = b.len0.clone(), b.len0 + w.prefix_len
+        plan = fa.Plan.tree_plan(Hq, Hkv, d, N, n, w.prefix_len, cap, cap)
+        out, lse = torch.empty(N, n, Hq, d, device="cuda"), torch.empty(N, n, Hq, device="cuda")
+        logits = torch.randn(N * n, vocab, generator=gen, device="cuda", dtype=torch.bfloat16) * 4
+        u = torch.rand(N * n, generator=gen, device="cuda")
+        top_k, top_p = torch.full((N * n,), 50, dtype=torch.int32, device="cuda"), torch.full((N * n,), 0.9, device="cuda")
+        drafted = torch.randint(vocab, (N, n), generator=gen, device="cuda", dtype=torch.int32)
+        targets, path = torch.empty(N * n, dtype=torch.int32, device="cuda"), torch.empty(N, n, dtype=torch.int32, device="cuda")
+        count, pending = (torch.empty(N, dtype=torch.int32, device="cuda") for _ in "cp")
+        work = fa.sample_workspace(N * n, vocab)
+
+        def attend(i):
+            r = b.reps[i]
+            plan.tree_attend(q_out, r["prefix_k"], r["prefix_v"], *suffixes[i], lens, masks, out, lse)
+
+        def step(i):
+            fa.tree_layout(parents, base, masks, positions)
+            fa.rotate_append(q, k, v, positions, freq, q_out, *suffixes[i], lens)
+            attend(i)
+            fa.sample(logits, u, targets, top_k=top_k, top_p=top_p, workspace=work)
+            fa.tree_accept(parents, masks, drafted, targets.view(N, n), *suffixes[i], lens, path, count, pending, advance=False)
+
+        def timed(call):
+            for i in range(b.R):
+                call(i)
+            torch.cuda.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                for i in range(b.R):
+                    call(i)
+            graph.replay()
+            us = []
+            for _ in range(trials):
+                t0, t1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+                t0.record()
+                for _ in range(20):
+                    graph.replay()
+                t1.record()
+                torch.cuda.synchronize()
+                us.append(t0.elapsed_time(t1) * 1e3 / (20 * b.R))
+            return float(np.median(us))
+
+        found[str(n)] = {"us_per_step": timed(step), "us_attention": timed(attend), "vocab": vocab}
+        log(f"[bench] drafted trees of {n}: {found[str(n)]['us_per_step']:.1f} us a step, attention {found[str(n)]['us_attention']:.1f}")
+        plan.close()
+    return found
 
 
 def lifecycle_timing(fa, torch, w):
@@ -606,6 +675,9 @@ def main():
     lifecycle = None
     if args.lifecycle and not main_b.paged:
         lifecycle = lifecycle_timing(fa, torch, main_b.w)
+    draft = None
+    if args.draft and not main_b.paged:
+        draft = draft_timing(fa, torch, main_b, [int(x) for x in args.draft.split(",")], args.trials)
     main_b.release()
 
     subs = {}
@@ -660,6 +732,8 @@ def main():
         res["instruction_prefill"] = prefill
     if lifecycle:
         res["lifecycle"] = lifecycle
+    if draft:
+        res["draft"] = draft
     print(json.dumps(res), flush=True)
 
 
