@@ -243,9 +243,9 @@ __global__ __launch_bounds__(256) void sample_scan_kernel(SampleArgs a)
     float most = -INFINITY;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-        float m = -INFINITY;  // (fmaxf drops a NaN)
+        float m = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) m = fmaxf(m, R::get(w[j], i));
+        for (int i = 0; i < VEC; ++i) m = fmaxf(m, __builtin_canonicalizef(R::get(w[j], i)));  // (drops a quiet NaN; a signalling one wins)
         m = sample_group_max<GL>(m);
         const int g = (i0 + j * 256 * VEC) / GROUP;
         if (tid % GL == 0 && g < groups) a.group_max[(size_t)r * groups + g] = sample_key(m);

@@ -230,7 +230,7 @@ class Plan:
         self.paged = paged
         self.heads = heads
         self.n_seqs = n_seqs
-        self._tree = None  # of a tree plan: the shapes of q and of the masks
+        self._tree = None  # of a tree plan: the shapes of a call's tensors
         self._mx = None  # of a plan over 4-bit tiles: the pool's shape, entries of the tile table
 
     @classmethod
@@ -300,7 +300,9 @@ class Plan:
         out = _vp()
         _check(_lib.fka_plan_create_tree(C.byref(h), C.byref(d), C.byref(out)))
         plan = cls(out.value, False, h, n_branches * n_nodes)
-        plan._tree = (n_branches, n_nodes, n_q_heads, head_dim)
+        plan._tree_shapes(n_branches, n_nodes)
+        cache = (n_branches, n_kv_heads, suffix_cap, head_dim)
+        plan._tree += ((n_kv_heads, prefix_len, head_dim),) * 2 + (cache, cache)
         return plan
 
     @classmethod
@@ -312,18 +314,30 @@ class Plan:
         out = _vp()
         _check(_lib.fka_plan_create_tree_paged(C.byref(h), C.byref(d), C.byref(out)))
         plan = cls(out.value, True, h, n_branches * n_nodes)
-        plan._tree = (n_branches, n_nodes, n_q_heads, head_dim)
+        plan._tree_shapes(n_branches, n_nodes)
+        pool = (n_pool_pages, n_kv_heads, page_size, head_dim)
+        plan._tree += (pool, pool, (n_branches, max_pages_per_seq))
         return plan
 
-    def _tree_shapes(self, q, masks):
-        if self._tree is None:
+    def _tree_shapes(self, n_branches, n_nodes):
+        q = (n_branches, n_nodes, self.heads.n_q_heads, self.heads.head_dim)
+        self._tree = q, q[:2], q[:1], q, q[:3]
+
+    def _tree_check(self, q, masks, suffix_len, out, out_lse, *cache):
+        want = self._tree
+        if want is None:
             return  # refused by the call
-        if q.shape != self._tree or masks.shape != self._tree[:2]:
-            raise ValueError(f"q must be {list(self._tree)}, masks int64 {list(self._tree[:2])}, as the plan was made")
+        got = (q.shape, masks.shape, suffix_len.shape, out.shape, want[4] if out_lse is None else out_lse.shape) + tuple(
+            w if t is None and not w[1] else t.shape for t, w in zip(cache, want[5:]))  # (no prefix: its tensors may be None)
+        if got != want:
+            names = ("q", "masks", "suffix_len", "out", "out_lse") + (
+                ("k_pool", "v_pool", "page_table") if self.paged else ("prefix_k", "prefix_v", "suffix_k", "suffix_v"))
+            raise ValueError("the plan was made for " + ", ".join(f"{n} {list(w)} (got {list(g)})" for n, g, w in zip(names, got, want)
+                                                                  if g != w))
 
     def tree_attend(self, q, prefix_k, prefix_v, suffix_k, suffix_v, suffix_len, masks, out, out_lse=None, stream=None):
         """fka_tree_attend: q bf16 [N][n][Hq][d], masks int64 [N][n] (the bits of tree_layout) -> out fp32 [N][n][Hq][d]."""
-        self._tree_shapes(q, masks)
+        self._tree_check(q, masks, suffix_len, out, out_lse, prefix_k, prefix_v, suffix_k, suffix_v)
         d = self.device
         _check(_lib.fka_tree_attend(self._h, _p(q, "bf16", d), _p(prefix_k, "bf16", d), _p(prefix_v, "bf16", d),
                                     _p(suffix_k, "bf16", d), _p(suffix_v, "bf16", d), _p(suffix_len, "i32", d), _p(masks, "i64", d),
@@ -331,7 +345,7 @@ class Plan:
 
     def tree_attend_paged(self, q, k_pool, v_pool, page_table, suffix_len, masks, out, out_lse=None, stream=None):
         """fka_tree_attend_paged: the same over the page pool."""
-        self._tree_shapes(q, masks)
+        self._tree_check(q, masks, suffix_len, out, out_lse, k_pool, v_pool, page_table)
         d = self.device
         _check(_lib.fka_tree_attend_paged(self._h, _p(q, "bf16", d), _p(k_pool, "bf16", d), _p(v_pool, "bf16", d),
                                           _p(page_table, "i32", d), _p(suffix_len, "i32", d), _p(masks, "i64", d), _p(out, "f32", d),

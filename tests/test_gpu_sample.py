@@ -192,9 +192,10 @@ def test_every_token_can_come(fa):
     assert (np.abs(np.bincount(got, minlength=5) - 4096 * w / w.sum()) <= 1).all()
 
 
-def test_graph_replays(fa):
+@pytest.mark.parametrize("V", [20000, 50000])
+def test_graph_replays(fa, V):
     rng = np.random.default_rng(5)
-    R, V = 40, 20000
+    R = 40
     x = _logits(rng, R, V, True).cuda()
     f32 = lambda a: torch.tensor(np.asarray(a, np.float32), device="cuda")  # noqa: E731
     u, t, p = f32(rng.random(R)), f32(rng.choice([0.0, 0.7, 1.2], R)), f32(rng.choice([1.0, 0.9], R))
@@ -215,6 +216,66 @@ def test_graph_replays(fa):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(tokens, want[0]) and torch.equal(logprob.view(torch.int32), want[1].view(torch.int32))
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V", [32768, 32769, 65536, 65537, 100001])
+def test_rows_that_many_blocks_share(fa, V, bf16):
+    """Wide nuclei, large k and flat min-p, from where rows are shared on."""
+    rng = np.random.default_rng(V)
+    picks = [(1.5, 0, 0.95, 0.0), (3.0, 0, 0.5, 0.0), (1.0, 1000, 1.0, 0.0), (1.0, 600, 0.9, 0.0), (4.0, 0, 1.0, 0.01), (1.5, 0, 0.99, 0.001),
+             (1.0, 2000, 0.999, 0.0), (2.0, 0, 1.0 - 2.0 ** -24, 0.0), (1.0, 300, 0.0, 0.0), (1.0, 20, 0.9, 0.0), (0.0, 0, 0.9, 0.0)]
+    t, k, p, m = (np.array(c) for c in zip(*picks))
+    _check(fa, _logits(rng, len(picks), V, bf16), t, k, p, m, rng.random(len(picks)))
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_equal_logits_of_large_rows(fa, bf16):
+    """More equals than any list holds, in rows that many blocks share."""
+    V, rng = 50000, np.random.default_rng(7)
+    x = np.zeros((8, V), np.float32)
+    x[4:] = rng.integers(0, 3, (4, V))
+    x = torch.from_numpy(x)
+    k, p, m = [0, 1000, 3000, 0] * 2, [0.5, 1.0, 0.5, 1.0] * 2, [0.0, 0.0, 0.0, 0.2] * 2
+    _check(fa, x.bfloat16() if bf16 else x, [1.0] * 8, k, p, m, rng.random(8))
+
+
+def test_few_finite_logits(fa):
+    """Fewer groups with a logit than top-k wants, and logits below every group's largest among the first k."""
+    x = np.full((4, 3000), -np.inf, np.float32)
+    x[0, [0, 1, 2, 700, 701, 2999]] = [1, 0, -5, 3, -9, 2]
+    x[1, :200] = np.random.default_rng(0).standard_normal(200)
+    x[2, 1500] = 0
+    x[3, :40] = np.arange(40)
+    for k in (2, 5, 50, 150, 187, 188):
+        _check(fa, torch.from_numpy(x), [1.0] * 4, [k] * 4, [1.0, 0.9, 0.5, 0.999], [0.0] * 4, [0.99, 0.4, 0.7, 0.1])
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_signalling_nan(fa, bf16):
+    x = np.random.default_rng(1).standard_normal((3, 500)).astype(np.float32)
+    bits = torch.from_numpy(x)
+    bits = (bits.bfloat16().view(torch.int16) if bf16 else bits.view(torch.int32)).clone()
+    bits[:, 3::7] = 0x7f81 if bf16 else 0x7f800001
+    bits[1, 4::7] = -0x7f if bf16 else -0x7fffff  # negative, all exponent bits set
+    x = bits.view(torch.bfloat16 if bf16 else torch.float32)
+    assert torch.isnan(x[:, 3]).all() and torch.isnan(x[1, 4])
+    for k, p in ((0, 1.0), (10, 1.0), (0, 0.8)):
+        _check(fa, x, [1.0, 0.0, 0.5], [k] * 3, [p] * 3, [0.0] * 3, [0.1, 0.5, 0.9])
+
+
+def test_more_rows_than_places_to_share(fa):
+    """1100 rows with a wide nucleus: the later ones are searched by their own block, with the same result."""
+    V, rng = 40000, np.random.default_rng(9)
+    x = _logits(rng, 2, V, True)
+    u = rng.random(2)
+    _, want, _ = _check(fa, x, [2.0] * 2, None, [0.9] * 2, None, u)
+    R = 1100
+    big = x.cuda()[torch.arange(R, device="cuda") % 2].contiguous()
+    f32 = lambda v: torch.tensor(np.resize(np.asarray(v, np.float32), R), device="cuda")  # noqa: E731
+    tokens = torch.empty(R, dtype=torch.int32, device="cuda")
+    fa.sample(big, f32(u), tokens, temperature=f32([2.0]), top_p=f32([0.9]), workspace=fa.sample_workspace(R, V))
+    assert tokens.view(-1, 2).eq(want).all()
 
 
 def test_no_rows(fa):

@@ -332,6 +332,62 @@ def test_attend_scale_and_more_than_64_branches(fa):
     _close(t, t.want())
 
 
+def test_plans_take_their_own_calls_only(fa):
+    t = Tree(8, 2, 64, 4, 20, [10, 20], _trees(1, 2, 4), seed=3)
+    t.place()
+    plan, prefill = t.plan(fa), fa.Plan.prefill_plan(8, 2, 64, 2, 4, 20, t.cap, t.cap)
+    with pytest.raises(fa.FkaError, match="fka_tree_attend"):
+        plan.prefill(t.dq, *t.cache, t.lens, t.out)
+    with pytest.raises(fa.FkaError, match="not a tree plan"):
+        prefill.tree_attend(t.dq, *t.cache, t.lens, t.dmasks, t.out)
+    with pytest.raises(fa.FkaError, match="not a paged tree plan"):
+        fa._check(fa.raw_call("fka_tree_attend_paged", plan.handle, *[None] * 9))
+    with pytest.raises(fa.FkaError, match="instruction-prefill"):
+        plan.decode(t.dq, *t.cache, t.lens, t.out)
+    p = Tree(8, 2, 64, 4, 20, [10, 20], _trees(1, 2, 4), paged=True, seed=3)
+    p.place()
+    paged = p.plan(fa)
+    with pytest.raises(fa.FkaError, match="fka_tree_attend_paged"):
+        paged.prefill_paged(p.dq, *p.cache, p.lens, p.out)
+    with pytest.raises(fa.FkaError, match="contiguous buffers"):
+        fa._check(fa.raw_call("fka_tree_attend", paged.handle, *[None] * 10))
+    # tensors of other sizes than the plan's
+    for bad, name in ((dict(dq=t.dq[:1]), "q"), (dict(dmasks=t.dmasks[:, :3]), "masks"), (dict(lens=t.lens[:1]), "suffix_len"),
+                      (dict(out=t.out[:1]), "out"), (dict(lse=t.lse[:1]), "out_lse"), (dict(cache=[c[:, :1] for c in t.cache]), "prefix_k")):
+        was = {key: getattr(t, key) for key in bad}
+        t.__dict__.update(bad)
+        with pytest.raises(ValueError, match=name):
+            t.call(plan)
+        t.__dict__.update(was)
+    t.dmasks = t.dmasks.int()
+    with pytest.raises(ValueError, match="i64"):
+        t.call(plan)
+
+
+def test_attend_without_a_prefix_takes_none_for_it(fa):
+    t = Tree(4, 2, 64, 5, 0, [3, 9], _trees(2, 2, 5), seed=2)
+    t.place()
+    t.cache[:2] = None, None
+    t.call(t.plan(fa))
+    _close(t, t.want())
+
+
+def test_attend_on_another_stream_and_two_plans_at_once(fa):
+    made = [Tree(8, 2, 128, 7, 600 + i, [30, 10], _trees(i, 2, 7), seed=i) for i in range(2)]
+    plans, streams = [], [torch.cuda.Stream() for _ in made]
+    for t in made:
+        t.place()
+        plans.append(t.plan(fa))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for t, plan, stream in zip(made, plans, streams):
+            with torch.cuda.stream(stream):
+                t.call(plan)
+    torch.cuda.synchronize()
+    for t in made:
+        _close(t, t.want())
+
+
 # ------------------------------------------------------------------------------------------------- accept
 
 def _accept(parents, masks, tokens, targets):
