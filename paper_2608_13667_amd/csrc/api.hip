@@ -29,6 +29,7 @@ struct fka_plan {
     // those with prefix tiles), whole prefix tiles of 64 keys
     bool prefill_tiles = false;
     bool tree = false;          // attention of drafted trees (tokens are nodes), on the tiled kernel
+    bool tree_halves = false;   // ... with two waves to a unit
     int32_t tile_unit_groups = 0, tile_ranges = 0, tile_prefix_ranges = 0, tile_prefix = 0;
     fka::TileSplit tile_split{};
     int32_t max_suffix_len = 0;
@@ -495,7 +496,7 @@ fka_status run_prefill(const fka_plan *p, const fka::AttnArgs &a, float *out, fl
         t.prefix_tiles = p->tile_prefix;
         t.split = p->tile_split;
         t.scale_log2 = p->scale * 1.4426950408889634f;
-        e = p->tree ? fka::launch_tree_tiles(t, p->n_blocks, p->d, s) : fka::launch_prefill_tiles(t, p->n_blocks, p->d, s);
+        e = p->tree ? fka::launch_tree_tiles(t, p->tree_halves, p->n_blocks, p->d, s) : fka::launch_prefill_tiles(t, p->n_blocks, p->d, s);
         if (e != hipSuccess) return hip_fail(e, "prefill kernel launch");
         fka::MergeArgs m{};
         m.part_o = p->part_o;
@@ -504,7 +505,7 @@ fka_status run_prefill(const fka_plan *p, const fka::AttnArgs &a, float *out, fl
         m.out_lse = out_lse;
         m.rows = p->n_seqs * p->Hq;
         m.n_q_heads = p->Hq;
-        m.n_parts = p->tile_ranges;
+        m.n_parts = p->n_slots;
         m.plan = 0;
         m.err = p->err;
         e = fka::launch_merge(m, p->d, s);
@@ -705,7 +706,10 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
         p->prefill_groups = tile_waves;
         p->n_blocks = (int32_t)(base * R);
         p->rounds = 1;
-        p->n_slots = (int32_t)R;
+        // Up to four units, two waves to each: us a call of 5 branches over 32k keys (40 / 8 heads), one wave to a unit / two: 1 unit
+        // 42.3 / 39.0, 2 units 43.6 / 41.2, 3 46.7 / 45.6, 4 51.5 / 51.2.  (Only trees have it so far.)
+        p->tree_halves = tree && U <= tile_waves / 2;
+        p->n_slots = (int32_t)R * (p->tree_halves ? 2 : 1);
         fka_status st = finish_plan(p);
         if (st != FKA_OK) return bail(st);
         *out = p;

@@ -567,7 +567,8 @@ int prefill_tiles_unit_rows();
 int prefill_tiles_waves();
 int prefill_tiles_blocks_per_cu(int head_dim, bool paged, bool tree = false);
 hipError_t launch_prefill_tiles(const PrefillArgs &a, int n_blocks, int head_dim, hipStream_t s);
-hipError_t launch_tree_tiles(const TreeArgs &a, int n_blocks, int head_dim, hipStream_t s);
+// halves: a range has two parts, 2 r and 2 r + 1 (at most four units a block).
+hipError_t launch_tree_tiles(const TreeArgs &a, bool halves, int n_blocks, int head_dim, hipStream_t s);
 hipError_t launch_append(const AppendArgs &a, int n_seqs, hipStream_t s);
 hipError_t launch_gather(const GatherArgs &a, hipStream_t s);
 hipError_t launch_scatter(const ScatterArgs &a, hipStream_t s);

@@ -316,7 +316,9 @@ struct MatrixPlan {
 //
 // With TreeArgs the tokens of a branch are the nodes of a tree: a row reads its branch's whole suffix and, of the nodes' keys
 // behind it, those of its mask's bits.  A row's keys of a tail tile are then bits too, eight to each of the lane's groups.
-template <int HD, bool PAGED, class Args>
+//
+// HALVES: up to four units a block.  Waves 2 u and 2 u + 1 share unit u, each takes half of a tile's keys and writes a part of its own.
+template <int HD, bool PAGED, bool HALVES, class Args>
 __device__ INLINE inline void prefill_tiles(const Args &a)
 {
     constexpr bool TREE = std::is_same<Args, TreeArgs>::value;
@@ -324,8 +326,9 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
     constexpr int CPR = HD / 8;             // 16-byte chunks per key row
     constexpr int NC = HD / 32;             // k-steps of the q.k product
     constexpr int NE = HD / 16;             // 16-wide d tiles of the output
-    constexpr int MT = KT / 16;             // 16-key score tiles per prefix tile
-    constexpr int KS = KT / 32;             // 32-key k-steps of p.v per prefix tile
+    constexpr int WK = HALVES ? KT / 2 : KT;  // keys that a wave takes of a tile
+    constexpr int MT = WK / 16;             // 16-key score tiles of those
+    constexpr int KS = WK / 32;             // 32-key k-steps of p.v
     constexpr int EG = 2;                   // d tiles per group of V operands
     constexpr int KBYTES = KT * ROWB;       // K (or V) of one prefix tile
     constexpr int V_LDS = STAGES * KBYTES;  // K buffers first, then V buffers
@@ -363,7 +366,8 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
     // stream its tiles at the same pace, so each tile is fetched once into the XCD's L2 for all
     const int unit_a = ug * a.split.units_each + min(ug, a.split.units_more);
     const int unit_z = unit_a + a.split.units_each + (ug < a.split.units_more ? 1 : 0);
-    const int u = unit_a + wave;
+    const int half = HALVES ? wave & 1 : 0;
+    const int u = unit_a + (HALVES ? wave >> 1 : wave);
     const bool active = u < unit_z;
     const int R = a.ranges, RP = a.prefix_ranges;
     const int PT = a.prefix_tiles;
@@ -471,13 +475,14 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
     }
 
     if (nmain > 1) issue_prefix(s0 + 1, 1);
+    if (HALVES && nmain > 2) issue_prefix(s0 + 2, 2);
 
     // ---- per-lane constants
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&lds[0];
     // K A-operand reads: row 16 i + l16 (i = M tile, an immediate), chunk 4 c + q4
     uint32_t kaddr[NC];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) kaddr[c] = lds0 + l16 * ROWB + 16 * ((4 * c + q4) ^ swz_k(l16));
+    for (int c = 0; c < NC; ++c) kaddr[c] = lds0 + half * (KT / 2 * ROWB) + l16 * ROWB + 16 * ((4 * c + q4) ^ swz_k(l16));
     // V^T reads (transposed): lane (q4, l16) addresses row 4 q4 + l16 / 4, d = 16 e + 4 (l16 % 4); rows
     // 16 m further are an immediate away with the same swizzle
     uint32_t vaddr[NE];
@@ -485,7 +490,7 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
         const int m4 = l16 & 3, T = 4 * q4 + (l16 >> 2);
 #pragma unroll
         for (int e = 0; e < NE; ++e)
-            vaddr[e] = lds0 + V_LDS + T * ROWB + 16 * ((2 * e + (m4 >> 1)) ^ swz_v(T)) + (m4 & 1) * 8;
+            vaddr[e] = lds0 + V_LDS + half * (KT / 2 * ROWB) + T * ROWB + 16 * ((2 * e + (m4 >> 1)) ^ swz_v(T)) + (m4 & 1) * 8;
     }
 
     // Tail tile j: this wave loads group 8 j + wave of the tail and leaves the group's branch (-1: the
@@ -776,7 +781,7 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
     // A lane's four keys of score tile i are keys 4 (q4 mod 2) + j of group 2 i + q4 / 2.
     bool use = true, tail = false;
     [[maybe_unused]] int lim[2][MT];  // row t reads the keys k <= lim[t][i] of group 2 i + q4 / 2
-    static_assert(!TREE || MT * GRP == 32, "a row's keys of the lane's groups are the bits of a word");
+    static_assert(!TREE || MT * GRP <= 32, "a row's keys of the lane's groups are bits of a word");
     [[maybe_unused]] uint32_t vis[2] = {~0u, ~0u};  // a tree's row t reads key k of group 2 i + q4 / 2 where bit 8 i + k is set
     uint32_t suffix_groups = 0;  // bit i: that group holds suffix keys (not the prefix's, which every row reads)
 #pragma unroll
@@ -794,7 +799,7 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
         if constexpr (TREE)  // (only this wave reads them, behind these writes; the four lanes of a row write the same)
             ds_write_b64(mask_at() + 128 * t, lr < rows_head ? a.masks[lr / a.split.group] & ~0ull >> (64 - n) : 0);
     }
-    const uint32_t grp0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&s_grp[0][0] + 8 * (q4 >> 1);
+    const uint32_t grp0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)&s_grp[0][0] + 8 * (q4 >> 1) + half * (NW / 2 * 8);
     auto any_qk = [&](int i) INLINE {
         use = true;
         tail = i >= nmain;
@@ -995,13 +1000,36 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
         for (; i < nmain; ++i) whole_step(i, LEADc);
         for (; i <= ntot; ++i) any_step(i, LEADc);
     };
+    // HALVES: few rows wait for a tile's loads and for a wave's own chain from q.k to p.v.  So three tiles load while one is read, half a tile is
+    // the chain, its steps one after the other, and no phase waits for another wave's.  25 rows over 32k keys: a step takes 1.32 us,
+    // 6.35 TB/s over all blocks (1.48 with both halves on one SIMD; its own work 1.1), 16 of 18; the start 5.5.
+    [[maybe_unused]] auto stream = [&]() INLINE {
+        for (int i = 0; i < ntot; ++i) {
+            if (i + 2 < ntot)
+                wait_vm<4 * DMAS>();
+            else if (i + 1 < ntot)
+                wait_vm<2 * DMAS>();
+            else
+                wait_vm<0>();
+            lds_barrier();  // tile i is in LDS; every wave is done with tile i - 1
+            if (i + 3 < ntot) issue(i + 3);
+            if (!active) continue;
+            any_qk(i);
+            any_sm(i);
+            any_pv(i);
+        }
+    };
     if (ntot > 0) {
         if (nmain < 1) issue(0);
         if (nmain < 2 && ntot > 1) issue(1);
-        if (wave < 4)
+        if constexpr (HALVES) {
+            if (nmain < 3 && ntot > 2) issue(2);
+            stream();
+        } else if (wave < 4) {
             run(std::true_type{});
-        else
+        } else {
             run(std::false_type{});
+        }
     }
     if (PAGED && __builtin_amdgcn_ballot_w64(bad_page) != 0 && lane == 0) atomicOr(a.err, kErrBadPage);
 
@@ -1066,7 +1094,7 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
         const int lr = u * 32 + 16 * t + l16c;
         if (lr >= rows_head) continue;
         const int s = lr / a.split.group, h = g * G + lr - s * G;
-        const size_t orow = (size_t)r * rows_total + (size_t)s * Hq + h;
+        const size_t orow = (size_t)(HALVES ? 2 * r + half : r) * rows_total + (size_t)s * Hq + h;
         // a row with no keys in this range: lse = -inf (the merge takes nothing of its o)
         const bool empty = !(l > 0.f) && !(l != l);
         if (q4c == 0) a.part_lse[orow] = empty ? -INFINITY : (__log2f(l) - nm[t]) * kLn2;
@@ -1081,25 +1109,25 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
 template <bool PAGED>  // head_dim 128
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void prefill_tiles_kernel(PrefillArgs a)
 {
-    prefill_tiles<128, PAGED>(a);
+    prefill_tiles<128, PAGED, false>(a);
 }
 
-template <bool PAGED>  // head_dim 128
+template <bool PAGED, bool HALVES>  // head_dim 128
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void tree_tiles_kernel(TreeArgs a)
 {
-    prefill_tiles<128, PAGED>(a);
+    prefill_tiles<128, PAGED, HALVES>(a);
 }
 
-template <bool PAGED>  // head_dim 64
+template <bool PAGED, bool HALVES>  // head_dim 64
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void tree_tiles_d64_kernel(TreeArgs a)
 {
-    prefill_tiles<64, PAGED>(a);
+    prefill_tiles<64, PAGED, HALVES>(a);
 }
 
 template <bool PAGED>  // head_dim 64
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void prefill_tiles_d64_kernel(PrefillArgs a)
 {
-    prefill_tiles<64, PAGED>(a);
+    prefill_tiles<64, PAGED, false>(a);
 }
 
 }  // namespace
@@ -1111,10 +1139,11 @@ int prefill_tiles_blocks_per_cu(int head_dim, bool paged, bool tree)
 {
     const void *f = nullptr;
     if (tree && head_dim == 128)
-        f = paged ? reinterpret_cast<const void *>(&tree_tiles_kernel<true>) : reinterpret_cast<const void *>(&tree_tiles_kernel<false>);
+        f = paged ? reinterpret_cast<const void *>(&tree_tiles_kernel<true, false>)
+                  : reinterpret_cast<const void *>(&tree_tiles_kernel<false, false>);
     else if (tree && head_dim == 64)
-        f = paged ? reinterpret_cast<const void *>(&tree_tiles_d64_kernel<true>)
-                  : reinterpret_cast<const void *>(&tree_tiles_d64_kernel<false>);
+        f = paged ? reinterpret_cast<const void *>(&tree_tiles_d64_kernel<true, false>)
+                  : reinterpret_cast<const void *>(&tree_tiles_d64_kernel<false, false>);
     else if (head_dim == 128)
         f = paged ? reinterpret_cast<const void *>(&prefill_tiles_kernel<true>)
                   : reinterpret_cast<const void *>(&prefill_tiles_kernel<false>);
@@ -1145,23 +1174,29 @@ hipError_t launch_prefill_tiles(const PrefillArgs &a, int n_blocks, int head_dim
     return hipGetLastError();
 }
 
-hipError_t launch_tree_tiles(const TreeArgs &a, int n_blocks, int head_dim, hipStream_t s)
+template <bool HALVES>
+static hipError_t launch_tree_tiles(const TreeArgs &a, int n_blocks, int head_dim, hipStream_t s)
 {
-    if (n_blocks <= 0) return hipSuccess;
     if (head_dim == 128) {
         if (a.paged)
-            tree_tiles_kernel<true><<<n_blocks, 64 * NW, 0, s>>>(a);
+            tree_tiles_kernel<true, HALVES><<<n_blocks, 64 * NW, 0, s>>>(a);
         else
-            tree_tiles_kernel<false><<<n_blocks, 64 * NW, 0, s>>>(a);
+            tree_tiles_kernel<false, HALVES><<<n_blocks, 64 * NW, 0, s>>>(a);
     } else if (head_dim == 64) {
         if (a.paged)
-            tree_tiles_d64_kernel<true><<<n_blocks, 64 * NW, 0, s>>>(a);
+            tree_tiles_d64_kernel<true, HALVES><<<n_blocks, 64 * NW, 0, s>>>(a);
         else
-            tree_tiles_d64_kernel<false><<<n_blocks, 64 * NW, 0, s>>>(a);
+            tree_tiles_d64_kernel<false, HALVES><<<n_blocks, 64 * NW, 0, s>>>(a);
     } else {
         return hipErrorInvalidValue;
     }
     return hipGetLastError();
+}
+
+hipError_t launch_tree_tiles(const TreeArgs &a, bool halves, int n_blocks, int head_dim, hipStream_t s)
+{
+    if (n_blocks <= 0) return hipSuccess;
+    return halves ? launch_tree_tiles<true>(a, n_blocks, head_dim, s) : launch_tree_tiles<false>(a, n_blocks, head_dim, s);
 }
 
 }  // namespace fka

@@ -20,7 +20,7 @@ def test_every_xdl_result_read_is_padded_in_the_tree_kernels():
         asm = X.compile_asm(hipcc, os.path.join(ROOT, "paper_2608_13667_amd", "csrc", "prefill.hip"),
                             os.path.join(ROOT, "include"), os.path.join(d, "prefill.s"))
     kernels = X.kernels(asm, "tree_tiles")
-    assert len(kernels) == 4
+    assert len(kernels) == 8
     for k in kernels:
         pairs = X.scan(asm, k)
         assert pairs, k
