@@ -907,11 +907,13 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
 #pragma unroll
             for (int e = 0; e < AHEAD; ++e) {
                 const int at = e0 + e * kSampleThreads + tid;
+                if (at - tid >= picked * GL) break;  // (uniform)
                 place[e] = at < picked * GL ? s.groups[at / GL] * GROUP + at % GL * VEC : n;
                 sample_load(row, max(0, min(place[e], n - VEC)), n, n >= VEC, w[e]);
             }
 #pragma unroll
             for (int e = 0; e < AHEAD; ++e) {
+                if (e0 + e * kSampleThreads >= picked * GL) break;
                 if (place[e] + VEC > n) sample_load(row, place[e], n, false, w[e]);
                 uint32_t x[VEC], take = 0;
 #pragma unroll
