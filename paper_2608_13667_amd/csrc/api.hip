@@ -29,7 +29,7 @@ struct fka_plan {
     // those with prefix tiles), whole prefix tiles of 64 keys
     bool prefill_tiles = false;
     bool tree = false;          // attention of drafted trees (tokens are nodes), on the tiled kernel
-    bool tree_halves = false;   // ... with two waves to a unit
+    fka::TreeKind tree_kind = fka::TreeKind::kPhases;
     int32_t tile_unit_groups = 0, tile_ranges = 0, tile_prefix_ranges = 0, tile_prefix = 0;
     fka::TileSplit tile_split{};
     int32_t max_suffix_len = 0;
@@ -496,7 +496,7 @@ fka_status run_prefill(const fka_plan *p, const fka::AttnArgs &a, float *out, fl
         t.prefix_tiles = p->tile_prefix;
         t.split = p->tile_split;
         t.scale_log2 = p->scale * 1.4426950408889634f;
-        e = p->tree ? fka::launch_tree_tiles(t, p->tree_halves, p->n_blocks, p->d, s) : fka::launch_prefill_tiles(t, p->n_blocks, p->d, s);
+        e = p->tree ? fka::launch_tree_tiles(t, p->tree_kind, p->n_blocks, p->d, s) : fka::launch_prefill_tiles(t, p->n_blocks, p->d, s);
         if (e != hipSuccess) return hip_fail(e, "prefill kernel launch");
         fka::MergeArgs m{};
         m.part_o = p->part_o;
@@ -644,7 +644,7 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
     if (tree || use_prefill_tiles(p)) {
         // The tiled kernel: units of 32 consecutive rows of a KV head, eight per block (one per
         // wave) over one of R ranges of the keys, R such that the blocks fill the device.
-        const int per_cu = fka::prefill_tiles_blocks_per_cu(p->d, lay.paged, tree);
+        const int per_cu = fka::prefill_tiles_blocks_per_cu(p->d, lay.paged);
         if (per_cu <= 0) return bail(fail(FKA_ERR_HIP, "occupancy query of the prefill kernel failed"));
         const int64_t rows_head = S * G;
         const int32_t U = (int32_t)ceil_div(rows_head, tile_rows);
@@ -708,8 +708,11 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
         p->rounds = 1;
         // Up to four units, two waves to each: us a call of 5 branches over 32k keys (40 / 8 heads), one wave to a unit / two: 1 unit
         // 42.3 / 39.0, 2 units 43.6 / 41.2, 3 46.7 / 45.6, 4 51.5 / 51.2.  (Only trees have it so far.)
-        p->tree_halves = tree && U <= tile_waves / 2;
-        p->n_slots = (int32_t)R * (p->tree_halves ? 2 : 1);
+        if (tree && U <= tile_waves / 2)
+            p->tree_kind = fka::TreeKind::kHalves;
+        else if (tree && (int64_t)Lp + max_suffix_len <= 20480)
+            p->tree_kind = fka::TreeKind::kStream;
+        p->n_slots = (int32_t)R * (p->tree_kind == fka::TreeKind::kHalves ? 2 : 1);
         fka_status st = finish_plan(p);
         if (st != FKA_OK) return bail(st);
         *out = p;

@@ -361,7 +361,7 @@ struct PrefillArgs {
     TileSplit split;
 };
 
-// Attention of drafted trees (prefill.hip): token t of a branch is node t of its tree, whose key is at suffix position L_b + t.  A node
+// Attention of drafted trees (tree_attend.h): token t of a branch is node t of its tree, whose key is at suffix position L_b + t.  A node
 // reads the prefix, its branch's suffix and node j's key where its mask has bit j.
 struct TreeArgs : PrefillArgs {
     const uint64_t *masks;  // [N][n], n <= 64
@@ -565,10 +565,11 @@ hipError_t launch_merge(const MergeArgs &a, int head_dim, hipStream_t s);
 // so units) per block, resident blocks per compute unit, and the launch.
 int prefill_tiles_unit_rows();
 int prefill_tiles_waves();
-int prefill_tiles_blocks_per_cu(int head_dim, bool paged, bool tree = false);
+int prefill_tiles_blocks_per_cu(int head_dim, bool paged);
 hipError_t launch_prefill_tiles(const PrefillArgs &a, int n_blocks, int head_dim, hipStream_t s);
-// halves: a range has two parts, 2 r and 2 r + 1 (at most four units a block).
-hipError_t launch_tree_tiles(const TreeArgs &a, bool halves, int n_blocks, int head_dim, hipStream_t s);
+// kHalves: a range has two parts, 2 r and 2 r + 1 (at most four units a block).
+enum class TreeKind { kPhases, kStream, kHalves };
+hipError_t launch_tree_tiles(const TreeArgs &a, TreeKind kind, int n_blocks, int head_dim, hipStream_t s);
 hipError_t launch_append(const AppendArgs &a, int n_seqs, hipStream_t s);
 hipError_t launch_gather(const GatherArgs &a, hipStream_t s);
 hipError_t launch_scatter(const ScatterArgs &a, hipStream_t s);

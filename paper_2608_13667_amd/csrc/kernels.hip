@@ -5,7 +5,7 @@
 // append_kernel / gather_kernel: suffix append and paged gather (data movement).
 // The operators around a snapshot's cache are in headers of their own: rotate.h (norm, rotation and store of new
 // tokens), mx_tiles.h (4-bit tiles), mx_attend.h (decode over them), evict.h (key weights, shortening); tree.h has the layout and the
-// acceptance of drafted trees (their attention is in prefill.hip), sample.h the choice of tokens.
+// acceptance of drafted trees, tree_attend.h their attention (the tiles of the instruction prefill), sample.h the choice of tokens.
 #include "evict.h"
 #include "internal.h"
 #include "merge_row.h"
@@ -14,6 +14,7 @@
 #include "rotate.h"
 #include "sample.h"
 #include "tree.h"
+#include "tree_attend.h"
 
 namespace fka {
 namespace {
@@ -421,6 +422,11 @@ hipError_t launch_mx_partials(const MxArgs &a, int n_jobs, int head_dim, int row
 hipError_t launch_key_weights(const WeightsArgs &a, int head_dim, hipStream_t s) { return launch_key_weights_kernel(a, head_dim, s); }
 
 hipError_t launch_evict(const EvictArgs &a, hipStream_t s) { return launch_evict_kernels(a, s); }
+
+hipError_t launch_tree_tiles(const TreeArgs &a, TreeKind kind, int n_blocks, int head_dim, hipStream_t s)
+{
+    return launch_tree_kernels(a, kind, n_blocks, head_dim, s);
+}
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s) { return launch_sample_kernels(a, s); }
 

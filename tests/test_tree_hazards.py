@@ -17,10 +17,10 @@ def test_every_xdl_result_read_is_padded_in_the_tree_kernels():
     if hipcc is None:
         pytest.skip("hipcc not found")
     with tempfile.TemporaryDirectory() as d:
-        asm = X.compile_asm(hipcc, os.path.join(ROOT, "paper_2608_13667_amd", "csrc", "prefill.hip"),
-                            os.path.join(ROOT, "include"), os.path.join(d, "prefill.s"))
+        asm = X.compile_asm(hipcc, os.path.join(ROOT, "paper_2608_13667_amd", "csrc", "kernels.hip"),
+                            os.path.join(ROOT, "include"), os.path.join(d, "kernels.s"))
     kernels = X.kernels(asm, "tree_tiles")
-    assert len(kernels) == 8
+    assert len(kernels) == 12
     for k in kernels:
         pairs = X.scan(asm, k)
         assert pairs, k
