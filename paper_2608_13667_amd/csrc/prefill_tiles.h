@@ -334,11 +334,9 @@ struct MatrixPlan {
 // With TreeArgs the tokens of a branch are the nodes of a tree: a row reads its branch's whole suffix and, of the nodes' keys
 // behind it, those of its mask's bits.  A row's keys of a tail tile are then bits too, eight to each of the lane's groups.
 //
-//
-// KIND kStream: the tiles one after the other, without the two phases (see stream below), and p in three bf16 terms, exact to 2^-27 (a
-// result is then as near to the 64-bit one as fp32 sums are: 4e-7 of it over 500 keys, where two terms leave 1.9e-6; over 30000 the sums alone leave as
-// much).  kHalves: the same for up to four units a block: waves 2 u and 2 u + 1 share unit u, each takes half of a tile's keys and
-// writes a part of its own.
+// KIND kStream: the tiles one after the other, without the two phases (see stream below), and p in three bf16 terms, to 2^-27 of it, so that a
+// result is as near to the 64-bit one as fp32 sums are (2.9e-7 of it over 500 keys, where two terms leave 1.9e-6).  kHalves: the same for
+// up to four units a block: waves 2 u and 2 u + 1 share unit u, each takes half of a tile's keys and writes a part of its own.
 enum { kPhases, kStream, kHalves };
 
 template <int HD, bool PAGED, int KIND, class Args>

@@ -278,6 +278,21 @@ def test_more_rows_than_places_to_share(fa):
     assert tokens.view(-1, 2).eq(want).all()
 
 
+def test_logits_past_four_gib(fa):
+    """The last rows of 4.6 GB of logits, with rows of many blocks among them, give what they give by themselves."""
+    R, V = 17500, 65536
+    x = torch.empty(R, V, device="cuda")
+    x.fill_(-1.0)
+    x[-3:] = _logits(np.random.default_rng(11), 3, V, False).cuda()
+    f32 = lambda v: torch.tensor(np.asarray(v, np.float32), device="cuda")  # noqa: E731
+    u, t, p = f32([0.2, 0.5, 0.9]), f32([1.0, 1.5, 0.0]), f32([1.0, 0.95, 1.0])
+    want, got = torch.empty(3, dtype=torch.int32, device="cuda"), torch.empty(R, dtype=torch.int32, device="cuda")
+    fa.sample(x[-3:], u, want, temperature=t, top_p=p, workspace=fa.sample_workspace(3, V))
+    fill = lambda last, value: torch.cat([torch.full((R - 3,), value, device="cuda"), last])  # noqa: E731
+    fa.sample(x, fill(u, 0.0), got, temperature=fill(t, 0.0), top_p=fill(p, 1.0), workspace=fa.sample_workspace(R, V))
+    assert torch.equal(got[-3:], want) and (got[:-3] == 0).all()
+
+
 def test_no_rows(fa):
     empty = torch.empty(0, dtype=torch.int32, device="cuda")
     fa.sample(torch.empty(0, 10, device="cuda"), torch.empty(0, device="cuda"), empty, workspace=fa.sample_workspace(0, 10))

@@ -204,6 +204,68 @@ def test_attend_over_a_long_prefix(fa, paged):
     _close(t, t.want())
 
 
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_many_rows_over_many_keys(fa, d, paged):
+    """400 rows of a KV head over 8200 keys: the kernel in two phases to a tile, with two terms of p."""
+    t = Tree(10, 2, d, 16, 8200 + 5, [100, 0, 33, 64, 7], _trees(5, 5, 16), paged, seed=d)
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    want = t.want()
+    _close(t, want)
+    first = t.out.clone()
+    t.out.zero_()
+    t.call(plan)
+    assert torch.equal(first, t.out)
+
+
+# few rows (two waves to a unit), a few units (tiles one after the other), many rows over many keys (two phases to a tile)
+KINDS = [(8, 2, 3, 4, 300), (10, 2, 4, 12, 300), (10, 2, 5, 16, 8192)]
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("kind", KINDS, ids=["halves", "stream", "phases"])
+def test_attend_infinite_prefix_values(fa, kind, paged):
+    """In the prefix, which every row reads, an infinity stays in its channel and is that infinity; both signs, or a NaN, are NaN there."""
+    hq, hkv, N, n, prefix = kind
+    t = Tree(hq, hkv, 128, n, prefix, [5] * N, _trees(3, N, n), paged, seed=1)
+    inf, nan = float("inf"), float("nan")
+    t.pv[0, 17, 3], t.pv[0, prefix - 1, 9], t.pv[0, 200, 20], t.pv[0, 40, 20] = inf, -inf, inf, -inf
+    t.pv[1, 250, 100], t.pv[1, 63, 64], t.pv[1, 64, 64] = nan, inf, inf
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    got = t.out.cpu()
+    a, z = got[:, :, : hq // 2], got[:, :, hq // 2:]
+    assert (a[..., 3] == inf).all() and (a[..., 9] == -inf).all() and torch.isnan(a[..., 20]).all()
+    assert torch.isnan(z[..., 100]).all() and (z[..., 64] == inf).all()
+    t.pv.nan_to_num_(0, 0, 0)
+    out, lse, tol, tol_lse = t.want()
+    rest = np.ones(got.shape, bool)
+    rest[:, :, : hq // 2, [3, 9, 20]] = False
+    rest[:, :, hq // 2:, [100, 64]] = False
+    assert (np.abs(got.double().numpy() - out)[rest] <= tol[rest]).all()
+
+
+@pytest.mark.parametrize("kind", KINDS, ids=["halves", "stream", "phases"])
+def test_attend_tree_edges_in_every_kernel(fa, kind):
+    """A hidden NaN node, a NaN that some rows read, an empty mask, and rows far apart in size, in each of the kernels."""
+    hq, hkv, N, n, prefix = kind
+    masks = _trees(7, N, n)
+    masks[0][1] = 0
+    masks = [[m & ~(1 << (n - 1)) for m in row] for row in masks]
+    t = Tree(hq, hkv, 64, n, prefix, [40] + [3] * (N - 1), masks, seed=4)
+    t.q[0] *= 30  # the scores of one branch rise far past the others'
+    for b, length in enumerate(t.suffix):
+        t.sk[b, :, length + n - 1] = float("nan")
+        t.sv[b, :, length + n - 1] = float("inf")
+    t.place()
+    t.call(t.plan(fa))
+    t.sk.nan_to_num_(0, 0, 0), t.sv.nan_to_num_(0, 0, 0)
+    _close(t, t.want())
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_attend_any_set_of_nodes(fa, d):
     """Masks that no tree gives: nothing, later nodes, not the node itself, bits past the nodes."""
@@ -510,3 +572,22 @@ def test_accept_from_a_graph(fa):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(state + (path, count, nxt), want))
+
+
+def test_accept_past_four_gib(fa):
+    """Rows behind 2^32 bytes of a cache."""
+    n, hkv, d, cap = 6, 4, 128, 2_200_000
+    k = torch.empty(2, hkv, cap, d, dtype=torch.bfloat16, device="cuda")
+    v = torch.empty_like(k)
+    lens = [cap - 10, cap - n]
+    parents, tokens, targets = [[-1, 0, 0, 2, 3, 4]] * 2, [[9, 1, 2, 3, 4, 5]] * 2, [[2, 0, 3, 4, 5, 6]] * 2
+    want = []
+    for b, length in enumerate(lens):
+        for c in (k, v):
+            c[b, :, length: length + n] = torch.randn(hkv, n, d, device="cuda")
+            want.append(c[b, :, [length + i for i in (0, 2, 3, 4, 5)]].clone())
+    dlens, (path, count, nxt) = _i32(lens), (torch.empty(s, dtype=torch.int32, device="cuda") for s in ((2, n), (2,), (2,)))
+    fa.tree_accept(_i32(parents), _i64([_masks(p) for p in parents]), _i32(tokens), _i32(targets), k, v, dlens, path, count, nxt)
+    assert count.tolist() == [5, 5] and nxt.tolist() == [6, 6]
+    got = [c[b, :, length: length + 5] for b, length in enumerate(lens) for c in (k, v)]
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
