@@ -466,6 +466,8 @@ size_t fka_sample_bytes(int32_t n_rows, int32_t n_vocab);
  *   min-p  of those, the ones with w >= min_p 2^44 (min_p <= 0 or NaN: all; more than 1 counts as 1)
  * and the token is the first place, in the order of the vocabulary, up to which the kept weights sum to more than floor(u S), S their
  * sum.  The products and comparisons of sums with p and u are in fp64.
+ * Where nothing is filtered, S, and with top-p alone the sum that p is of, are sums of stretches of 4096 logits, each in units of 2^-44 of its own
+ * largest weight: up to 2^-27 of the sum from the one above (some 1e-13 of it for the logits of a model).
  * A temperature of 0 (or less, or NaN) chooses the first of the largest logits.  A NaN logit counts as -inf, which is never chosen; beside a logit of +inf
  * the others have no weight.  A row without any logit above -inf gets the token -1 and bit 32 in *err.
  *   logits                     [n_rows] rows of n_vocab

@@ -633,14 +633,14 @@ __device__ inline bool sample_from_list(const SampleArgs &a, int r, const Sample
     return true;
 }
 
-// The place where the sum of the kept weights of COUNT logits, `first` on, passes the mark.
-template <int COUNT, class T>
-__device__ inline void sample_from_part(const SampleArgs &a, int r, const T *row, int first, u64 mark, double total, SampleShared &s,
+// The place where the sum of the kept weights of COUNT logits, `first` on, passes mark_of(their sum).
+template <int COUNT, class T, class F>
+__device__ inline void sample_from_part(const SampleArgs &a, int r, const T *row, int first, F &&mark_of, double total, SampleShared &s,
                                         const SampleDraw &draw, const SampleKept &kept, const SampleWeight &weight)
 {
     constexpr int EACH = COUNT / kSampleThreads;
     const int i = first + (int)threadIdx.x * EACH;
-    u64 w[EACH], sum = 0, unused;
+    u64 w[EACH], sum = 0, here;
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
         w[j] = 0;
@@ -651,7 +651,8 @@ __device__ inline void sample_from_part(const SampleArgs &a, int r, const T *row
         }
         sum += w[j];
     }
-    u64 before = sample_scan(sum, s.part, unused);
+    u64 before = sample_scan(sum, s.part, here);
+    const u64 mark = mark_of(here);
     if (mark >= before && mark < before + sum) {
 #pragma unroll
         for (int j = 0; j < EACH; ++j) {
@@ -687,24 +688,26 @@ __device__ inline void sample_from_row(const SampleArgs &a, int r, const T *row,
     }
     __syncthreads();
     const SamplePart at = sample_part(s.tile, parts, [&](u64 total) { return draw.mark(total); });
-    sample_from_part<PART>(a, r, row, at.part * PART, at.mark, (double)at.total, s, draw, kept, weight);
+    sample_from_part<PART>(a, r, row, at.part * PART, [&](u64) { return at.mark; }, (double)at.total, s, draw, kept, weight);
 }
 
-// Lane i: tile i's share of the sum of all weights, in units of the largest one's 2^-44.
+// Lane i: tile i's share of the sum of all weights, in units of the largest one's 2^-44: 0 for a tile whose largest rounds to 0 there.
 __device__ inline double sample_tile_sum(const SampleArgs &a, int r, const SampleWeight &weight)
 {
     const int tiles = (a.n_vocab + kSampleTile - 1) / kSampleTile, lane = threadIdx.x & 63;
     if (lane >= tiles) return 0;
-    return (double)a.tile_sum[(size_t)r * tiles + lane] * (weight.exact(a.tile_max[(size_t)r * tiles + lane]) / kSampleUnit);
+    const uint32_t key = a.tile_max[(size_t)r * tiles + lane];
+    return weight(key) ? (double)a.tile_sum[(size_t)r * tiles + lane] * (weight.exact(key) / kSampleUnit) : 0;
 }
 
-// Nothing filtered: the tile that the random number falls into, by the tiles' sums, and the place in it.
+// Nothing filtered: the tile that the random number falls into, by the tiles' sums, and the place in it by the weights against M (in a tile
+// with a share one at least is no 0).
 template <class T>
-__device__ inline void sample_from_tiles(const SampleArgs &a, int r, const T *row, const SampleDraw &draw, const SampleWeight &against,
+__device__ inline void sample_from_tiles(const SampleArgs &a, int r, const T *row, const SampleDraw &draw, const SampleWeight &weight,
                                          SampleShared &s)
 {
-    const int n = a.n_vocab, lane = threadIdx.x & 63, tiles = (n + kSampleTile - 1) / kSampleTile;
-    const double sum = sample_tile_sum(a, r, against);
+    const int n = a.n_vocab, lane = threadIdx.x & 63;
+    const double sum = sample_tile_sum(a, r, weight);
     double up_to = sum;  // the sums up to the lane's tile
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
@@ -715,11 +718,10 @@ __device__ inline void sample_from_tiles(const SampleArgs &a, int r, const T *ro
     const u64 past = __builtin_amdgcn_ballot_w64(sum > 0 && up_to > mark), any = __builtin_amdgcn_ballot_w64(sum > 0);
     const int tile = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
     const double here = __shfl(sum, tile), front = __shfl(up_to, tile) - here;
-    const uint32_t tile_key = a.tile_max[(size_t)r * tiles + tile];
-    const u64 all = a.tile_sum[(size_t)r * tiles + tile];
-    const u64 at = min((u64)(fmin(fmax((mark - front) / here, 0.0), 1.0) * (double)all), all - 1);
-    sample_from_part<kSampleTile>(a, r, row, tile * kSampleTile, at, total * kSampleUnit / against.exact(tile_key), s, draw,
-                                  SampleKept{0, n}, SampleWeight(s.table, tile_key, draw.t));
+    const double part = fmin(fmax((mark - front) / here, 0.0), 1.0);
+    sample_from_part<kSampleTile>(
+        a, r, row, tile * kSampleTile, [=](u64 all) { return min((u64)(part * (double)all), all - 1); }, total, s, draw,
+        SampleKept{0, n}, weight);
 }
 
 // (M - l) / t in bins of 1/32 (a weight of more than 2^-45 is in the first 999).
@@ -1139,7 +1141,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_left_kernel(SampleArgs 
         if (s.list[i] >= last && s.weight[i] >= draw.least) atomicAdd(&s.tile[~(uint32_t)s.list[i] / kSampleTile], s.weight[i]);
     __syncthreads();
     const SamplePart in = sample_part(s.tile, tiles, [&](u64 total) { return draw.mark(total); });
-    sample_from_part<kSampleTile>(a, r, row, in.part * kSampleTile, in.mark, (double)in.total, s, draw,
+    sample_from_part<kSampleTile>(a, r, row, in.part * kSampleTile, [&](u64) { return in.mark; }, (double)in.total, s, draw,
                                   SampleKept{(uint32_t)(last >> 32), (int)~(uint32_t)last}, weight);
 }
 

@@ -293,6 +293,20 @@ def test_logits_past_four_gib(fa):
     assert torch.equal(got[-3:], want) and (got[:-3] == 0).all()
 
 
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_what_rounds_to_no_weight_does_not_come(fa, bf16):
+    """Logits of the type's lowest value, and some whose weight rounds to 0, in front of those that have one, at the smallest random
+    numbers: no stretch of 4096 without a weight, and no such logit of a stretch with one, is drawn from."""
+    kind = torch.bfloat16 if bf16 else torch.float32
+    V = 5 * 4096
+    x = torch.full((4, V), torch.finfo(kind).min, dtype=kind)
+    x[:, 4096: 8192] = -40.0  # 2^-57.7 of the largest
+    x[:, 8192: 9000] = -33.0  # 2^-47.6
+    x[:, 9000] = -26.0        # 2^-37.5: 90 units
+    x[:, 3 * 4096:] = 0.0
+    _check(fa, x, None, None, None, None, [0.0, 1e-20, 0.3, 1.0])
+
+
 def test_no_rows(fa):
     empty = torch.empty(0, dtype=torch.int32, device="cuda")
     fa.sample(torch.empty(0, 10, device="cuda"), torch.empty(0, device="cuda"), empty, workspace=fa.sample_workspace(0, 10))
