@@ -499,6 +499,8 @@ struct AcceptArgs {
 // groups of a row.
 constexpr int kSampleTile = 4096;
 constexpr int kSampleGroups = 4096;
+// Groups of 16 where they fit: a row's block reads a quarter of the logits that groups of 64 make it read.  16 / 64, us a call of 5 rows of
+// 32000 bf16: k 20 13.5 / 12.7, 400 18.9 / 25.0, 1000 24.8 / 84; 65536 fp32 k 20 18.0 / 17.0, 1000 26.4 / 153.
 __host__ __device__ inline int sample_group_of(int n_vocab) { return n_vocab <= 16 * kSampleGroups ? 16 : 64; }
 // Rows that several blocks share: most of them, bins of a histogram, entries of a list; the blocks of such a row are some
 // 4096 / rows, up to one to a tile.

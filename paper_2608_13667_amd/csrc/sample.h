@@ -11,15 +11,21 @@
 // tile) also the sum of the weights against the tile's own largest, where the row needs a sum over all.
 // sample_row_kernel, a block to a row, then reads little more of it:
 //   * nothing filtered: the tiles' sums give the tile that the random number falls into, which is read;
-//   * otherwise the groups' maxima bound the threshold from below: the k-th largest of them is no larger than the k-th largest
-//     logit.  The groups that reach the bound are read and the logits above it listed, up to 2048, and filtered.  For top-p
+//   * otherwise the groups' maxima (for a large k the logits themselves, counted) bound the threshold from below: the k-th largest of them
+//     is no larger than the k-th largest logit.  The groups that reach the bound are read and the logits above it listed, up to 2048, and filtered.  For top-p
 //     alone the bound is that of 128 groups, and the list will do if it has p of the sum;
 //   * where it has not, the row is left to three more kernels, in which many blocks share it: a histogram of the weights by
 //     (M - l) / t; the bin where their sum passes p, whose logits are listed, and the sums of each tile's logits above it; the draw.
 //     So are rows of which more than 256 groups have to be read, for the list or, with min-p alone, the draw;
-//   * where a list does not fit (thousands of equal logits, a k in the thousands), the block goes over the row by itself: the threshold
+//   * where a list does not fit (thousands of equal logits, a k of some 2000 or more), the block goes over the row by itself: the threshold
 //     digit by digit of the logit's bits (11, 11, 10 from the top, as unsigned numbers in the logits' order), a histogram of each
 //     digit's values among what agrees in the digits before.
+//
+// One block to a row for all of it, by digits from memory, took 64 us for 5 rows of 32000 bf16, 556 for 320 of 128000 fp32 (a quarter of them
+// top-p alone) and 111 for 80 of 200003 bf16, nothing filtered.  Now 20 to 32 (a row with k = 1000 is the
+// slowest of such a call), 103 and 23.7.  The scan is bound by memory (164 MB in 28 us, 5.9 TB/s) or, with sums, by fp64 exponentials (16 million
+// in 18 us); the row kernel by latency, some twenty steps between barriers (7 us where nothing is filtered, 14 with k = 50 and p,
+// 20 over 320 rows); the three kernels behind it by their start, their loads and the list's (12, 23 and 17).
 #pragma once
 
 #include <type_traits>
@@ -33,7 +39,9 @@ constexpr int kSampleThreads = 512;
 constexpr int kSampleWaves = kSampleThreads / 64;
 constexpr int kSampleBins = 2048;
 constexpr int kSampleFew = kSampleThreads / 4;
-constexpr int kSampleFirst = 128;  // groups whose maxima bound the list of top-p alone
+// Groups whose maxima bound the list of top-p alone.  (48 made no difference: a row whose kept logits are few is done either way, and one of thousands
+// is left to many blocks or read by its own.)
+constexpr int kSampleFirst = 128;
 constexpr double kSampleUnit = 17592186044416.0;  // 2^44
 constexpr uint32_t kNoLogit = 0x007fffffu;        // the key of -inf (NaN counts as that)
 
@@ -159,6 +167,31 @@ __device__ inline void sample_keys(const T *row, int i, int n, uint32_t (&key)[S
     sample_load(row, i, n, false, w);
 #pragma unroll
     for (int j = 0; j < SampleRow<T>::VEC; ++j) key[j] = sample_key(SampleRow<T>::get(w, j));
+}
+
+// f(keys, place of the first) for the row, the block's threads side by side, all lanes of a wave at once (past the row's end: kNoLogit), and the loads of
+// several steps on their way.
+constexpr int kSampleAhead = 4;
+template <class T, class F>
+__device__ inline void sample_walk(const T *row, int n, F &&f)
+{
+    constexpr int VEC = SampleRow<T>::VEC, STEP = kSampleThreads * VEC;
+    for (int i0 = 0; i0 < n; i0 += kSampleAhead * STEP) {
+        const int at = i0 + (int)threadIdx.x * VEC;
+        uint32_t w[kSampleAhead][4];
+#pragma unroll
+        for (int e = 0; e < kSampleAhead; ++e) sample_load(row, max(0, min(at + e * STEP, n - VEC)), n, n >= VEC, w[e]);
+#pragma unroll
+        for (int e = 0; e < kSampleAhead; ++e) {
+            if (i0 + e * STEP >= n) break;  // (uniform)
+            const int i = at + e * STEP;
+            if (i + VEC > n) sample_load(row, i, n, false, w[e]);
+            uint32_t key[VEC];
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) key[j] = sample_key(SampleRow<T>::get(w[e], j));
+            f(key, i);
+        }
+    }
 }
 
 __device__ inline bool sample_all(const SampleArgs &a, int r)  // whether row r needs the sum over all its logits
@@ -673,10 +706,7 @@ __device__ inline void sample_from_row(const SampleArgs &a, int r, const T *row,
     __syncthreads();
     if (tid < parts) s.tile[tid] = 0;
     __syncthreads();
-    for (int part = 0; part < parts; ++part) {
-        const int i = part * PART + tid * VEC;
-        uint32_t x[VEC];
-        sample_keys(row, i, n, x);
+    sample_walk(row, n, [&](const uint32_t(&x)[VEC], int i) {
         u64 sum = 0;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
@@ -684,8 +714,8 @@ __device__ inline void sample_from_row(const SampleArgs &a, int r, const T *row,
             sum += w >= draw.least ? w : 0;
         }
         sum = sample_wave_sum(sum);
-        if ((tid & 63) == 0 && sum) atomicAdd(&s.tile[part], sum);
-    }
+        if ((tid & 63) == 0 && sum) atomicAdd(&s.tile[i / PART], sum);
+    });
     __syncthreads();
     const SamplePart at = sample_part(s.tile, parts, [&](u64 total) { return draw.mark(total); });
     sample_from_part<PART>(a, r, row, at.part * PART, [&](u64) { return at.mark; }, (double)at.total, s, draw, kept, weight);
@@ -737,31 +767,27 @@ template <class T>
 __device__ inline bool sample_nucleus(const T *row, int n, const SampleWeight &weight, uint32_t max_key, float t, double limit,
                                       SampleShared &s, SampleKept &kept)
 {
-    constexpr int VEC = SampleRow<T>::VEC, STEP = kSampleThreads * VEC;
+    constexpr int VEC = SampleRow<T>::VEC;
     const int tid = threadIdx.x;
     const SampleNucleusBin bin(max_key, t);
     sample_clear(s);
     if (tid == 0) s.count = 0;
-    for (int i = tid * VEC; i < n; i += STEP) {
-        uint32_t x[VEC];
-        sample_keys(row, i, n, x);
+    sample_walk(row, n, [&](const uint32_t(&x)[VEC], int) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
             const u64 w = weight(x[j]);
             if (w) atomicAdd(&s.hist[bin(sample_logit(x[j]))], w);
         }
-    }
+    });
     __syncthreads();
     u64 front;
     const int border = sample_bin(limit, 0, s, front);
-    for (int i0 = 0; i0 < n; i0 += STEP) {
-        const int i = i0 + tid * VEC;
-        uint32_t x[VEC], take = 0;
-        sample_keys(row, i, n, x);
+    sample_walk(row, n, [&](const uint32_t(&x)[VEC], int i) {
+        uint32_t take = 0;
 #pragma unroll
         for (int j = 0; j < VEC; ++j) take |= x[j] > kNoLogit && bin(sample_logit(x[j])) == border ? 1u << j : 0;
         sample_append(s.list, &s.count, take, x, i);
-    }
+    });
     __syncthreads();
     const int count = s.count;
     if (count > kSampleList) return false;  // (uniform)
@@ -877,18 +903,30 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
     const double limit = fmax((double)draw.p * sum, 0.5);
     const float top = sample_logit(max_key), range = top - sample_logit(~low);
     const bool by_rank = draw.k || nucleus;
+    // k so large that the groups' maxima say little about the k-th logit: the bins count the logits themselves (over twice the maxima's range; what
+    // is below is in the last one).  us a call of 5 rows, maxima / logits: 17000 (1063 groups of 16) k 300 17.4 / 21.1, 600 20.8 / 22.6, 1000
+    // 60 / 25; 24000 k 600 20.2 / 24.2, 1000 24.9 / 26.6; 32000 k 1000 24.1 / 28.3, 1500 158 / 35; 128000 (groups of 64) k 1500 506 / 55.
+    const bool ranks = draw.k > groups / 2;
     int bound = 0;
-    const float step = range > 0.f ? (kSampleBins - 1) / range : 0.f;
+    const float step = range > 0.f ? (kSampleBins - 1) / (ranks ? 2 * range : range) : 0.f;
     auto bin = [&](uint32_t k) -> int { return (int)fminf((top - sample_logit(k)) * step, (float)(kSampleBins - 1)); };
     auto above = [&](uint32_t k) -> bool { return k > kNoLogit && (by_rank ? bin(k) <= bound : weight(k) >= draw.least); };
-    const bool listed = !by_rank || (range < 3e38f && step < 3e38f && draw.k <= groups);  // (uniform)
+    const bool listed = !by_rank || (range < 1.5e38f && step < 3e38f);  // (uniform)
     if (listed) {
         if (tid == 0) s.count = s.n_few = 0;
         if (by_rank) {
             sample_clear(s);
+            if (ranks) {
+                sample_walk(row, n, [&](const uint32_t(&x)[VEC], int) {
 #pragma unroll
-            for (int e = 0; e < EACH; ++e)
-                if (most[e] > kNoLogit) atomicAdd(&s.hist[bin(most[e])], 1ull);
+                    for (int j = 0; j < VEC; ++j)
+                        if (x[j] > kNoLogit) atomicAdd(&s.hist[bin(x[j])], 1ull);
+                });
+            } else {
+#pragma unroll
+                for (int e = 0; e < EACH; ++e)
+                    if (most[e] > kNoLogit) atomicAdd(&s.hist[bin(most[e])], 1ull);
+            }
             __syncthreads();
             u64 unused;
             bound = sample_bin((double)(draw.k ? draw.k : kSampleFirst), 0, s, unused);
@@ -900,7 +938,10 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
             if (above(most[e])) s.groups[atomicAdd(&s.n_few, 1)] = (uint16_t)(tid + e * kSampleThreads);
         __syncthreads();
         const int picked = s.n_few;
-        if (picked > 256 && !nucleus && picked >= draw.k &&
+        // Shared by many blocks / read by this one, us a call, fp32, all rows with the same k: 5 rows of 128000 k 100 22.3 / 25.4, 400 23.5 / 31, 1000
+        // 26.9 / 48; 40 rows k 300 30.0 / 30.0, 600 31.2 / 38.9; 320 rows k 100 76 / 50, 400 80 / 61, 1000 87 / 83; 5 rows of 65536 (groups of
+        // 16) k 100 22.5 / 20.5, 1000 26.4 / 29.0.  Where only some of many rows share, theirs cost less.
+        if (picked > 256 && !nucleus && (ranks || picked >= draw.k) &&
             sample_leave(a, s, SampleLeft{limit, 0, r, max_key, 0, by_rank ? bound : SampleLeft::kAll, step}))
             return;
         for (int e0 = 0; e0 < picked * GL; e0 += AHEAD * kSampleThreads) {  // AHEAD loads of a thread on their way
@@ -929,7 +970,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
         __syncthreads();
         const int count = s.count;
         // (fewer groups than k: a logit below all of them may be among the first k)
-        if (picked >= draw.k && count <= kSampleList &&
+        if ((ranks || picked >= draw.k) && count <= kSampleList &&
             (count <= 64 ? sample_from_few(a, r, draw, weight, count, sum, s) : sample_from_list(a, r, draw, weight, count, sum, s)))
             return;
         __syncthreads();

@@ -2,7 +2,8 @@
 //
 // tree_layout: with a(i) the parent of node i, a(i) < i, the nodes that node i reads are itself, a(i), a(a(i)), .. to the
 // root.  One wave takes a tree, lane i node i.  Six doublings replace up to 63 steps: with m_i the nodes found so far
-// and r_i the node behind them, m_i |= m[r_i], r_i = r[r_i].  Bound by the launch: 512 trees of 64 nodes 4.6 us.
+// and r_i the node behind them, m_i |= m[r_i], r_i = r[r_i].  Bound by the launch: the kernel takes 1.9 us for 5 trees of 16 nodes and 2.4 us
+// for 512 of 64, a call from Python 6.
 //
 // tree_accept: node i is right where its token is the one chosen behind its parent, and no node before it has the same parent
 // and token.  It is accepted where all the nodes that it reads are right: one comparison of bit sets a lane.  The
@@ -10,7 +11,8 @@
 // row L + i_j to row L + j.  i_j >= j, so a wave that moves a head's rows in ascending chunks, each read whole before it is
 // written, never writes a row that is still to be read.
 // One block takes a branch, so that the length is written behind every read of it; its waves share the K and V heads.  Bound by
-// latency: the tree, the pages, the rows, one after the other.
+// latency: the tree, the pages, the rows, one after the other.  3.9 us for 5 branches of 16 nodes, 8 KV heads of 128; 7.2 us for 80 of 64 nodes
+// in pages (12 MB at the copy rate would be 2.4).
 #pragma once
 
 #include "internal.h"

@@ -307,6 +307,23 @@ def test_what_rounds_to_no_weight_does_not_come(fa, bf16):
     _check(fa, x, None, None, None, None, [0.0, 1e-20, 0.3, 1.0])
 
 
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("V", [100, 2047, 2049, 5000, 17000, 40001, 70001])
+def test_large_k(fa, V, bf16):
+    """k around half of the groups and past them, around the list's length, and just below the vocabulary's; flat rows, outliers far
+    below, the type's lowest values, a single value."""
+    rng = np.random.default_rng(V + 7)
+    groups = -(-V // (16 if V <= 65536 else 64))
+    ks = sorted({k for k in (groups // 2, groups // 2 + 1, groups, groups + 1, 1000, 2047, 2048, 2049, V // 2, V - 1) if 0 < k < V})
+    x = _logits(rng, 5 * len(ks), V, False)
+    x[1::5] *= 0.01
+    x[2::5, ::3] = -1e4
+    x[3::5, V // 5:] = torch.finfo(torch.float32 if not bf16 else torch.bfloat16).min
+    x[4::5] = 1.5
+    R = len(x)
+    _check(fa, x.bfloat16() if bf16 else x, 0.5 + rng.random(R), np.repeat(ks, 5), rng.choice([1.0, 0.9, 0.999], R), rng.choice([0.0, 0.01], R), rng.random(R))
+
+
 def test_no_rows(fa):
     empty = torch.empty(0, dtype=torch.int32, device="cuda")
     fa.sample(torch.empty(0, 10, device="cuda"), torch.empty(0, device="cuda"), empty, workspace=fa.sample_workspace(0, 10))
