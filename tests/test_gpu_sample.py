@@ -324,6 +324,27 @@ def test_large_k(fa, V, bf16):
     _check(fa, x.bfloat16() if bf16 else x, 0.5 + rng.random(R), np.repeat(ks, 5), rng.choice([1.0, 0.9, 0.999], R), rng.choice([0.0, 0.01], R), rng.random(R))
 
 
+def test_two_streams_at_once(fa):
+    """Calls on two streams, each with a workspace of its own, and the stream given as an argument."""
+    R, V = 40, 70001
+    rng = np.random.default_rng(3)
+    x = _logits(rng, 2 * R, V, True).cuda()
+    f32 = lambda v: torch.tensor(np.asarray(v, np.float32), device="cuda")  # noqa: E731
+    u, p = f32(rng.random(2 * R)), f32(rng.choice([0.5, 0.95], 2 * R))
+    k = torch.tensor(rng.choice([0, 50, 400], 2 * R), dtype=torch.int32, device="cuda")
+    want, got = (torch.empty(2 * R, dtype=torch.int32, device="cuda") for _ in "wg")
+    fa.sample(x, u, want, top_k=k, top_p=p, workspace=fa.sample_workspace(2 * R, V))
+    works = [fa.sample_workspace(R, V) for _ in "ab"]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in "ab"]
+    for _ in range(5):
+        for i, (st, work) in enumerate(zip(streams, works)):
+            part = slice(i * R, (i + 1) * R)
+            fa.sample(x[part], u[part], got[part], top_k=k[part], top_p=p[part], workspace=work, stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
 def test_no_rows(fa):
     empty = torch.empty(0, dtype=torch.int32, device="cuda")
     fa.sample(torch.empty(0, 10, device="cuda"), torch.empty(0, device="cuda"), empty, workspace=fa.sample_workspace(0, 10))

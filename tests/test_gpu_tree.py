@@ -591,3 +591,38 @@ def test_accept_past_four_gib(fa):
     assert count.tolist() == [5, 5] and nxt.tolist() == [6, 6]
     got = [c[b, :, length: length + 5] for b, length in enumerate(lens) for c in (k, v)]
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("hq,n", [(4, 3), (32, 20)], ids=["halves", "phases"])
+def test_attend_past_four_gib(fa, hq, n, paged):
+    """The keys that count are behind 2^32 bytes of a prefix; those in front have less than 2^-90 of their weight."""
+    near, L = 300, 4_200_003
+    t = Tree(hq, 4, 128, n, near, [5], _trees(3, 1, n), scale=1.0, junk=0.0)
+    t.q[..., 0] = 8
+    t.pk[..., 0] = t.sk[..., 0] = 0
+    t.place()
+    if paged:
+        shared = -(-L // 16)
+        cache = []
+        for pre, suf in ((t.cache[0], t.cache[2]), (t.cache[1], t.cache[3])):
+            pool = torch.zeros(shared + 3, 4, 16, 128, dtype=torch.bfloat16, device="cuda")
+            if not cache:
+                pool[:shared, :, :, 0] = -8
+            for i in range(near):
+                at = L - near + i
+                pool[at // 16, :, at % 16] = pre[:, i]
+            for u in range(t.cap):
+                pool[shared + 2 - u // 16, :, u % 16] = suf[0, :, u]
+            cache.append(pool)
+        pages = -(-t.cap // 16)
+        table = torch.cat([torch.arange(shared), shared + 2 - torch.arange(pages)]).to(torch.int32).cuda()[None].contiguous()
+        plan = fa.Plan.tree_paged_plan(hq, 4, 128, 1, n, L, table.shape[1], shared + 3, t.cap, softmax_scale=1.0)
+        plan.tree_attend_paged(t.dq, *cache, table, t.lens, t.dmasks, t.out, t.lse)
+    else:
+        k, v = (torch.zeros(4, L, 128, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+        k[..., 0] = -8
+        k[:, L - near:], v[:, L - near:] = t.cache[0], t.cache[1]
+        plan = fa.Plan.tree_plan(hq, 4, 128, 1, n, L, t.cap, t.cap, softmax_scale=1.0)
+        plan.tree_attend(t.dq, k, v, t.cache[2], t.cache[3], t.lens, t.dmasks, t.out, t.lse)
+    _close(t, t.want())
