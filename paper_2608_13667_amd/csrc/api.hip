@@ -2539,7 +2539,7 @@ fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const flo
     a.err = err;
     sample_layout(a, static_cast<char *>(workspace));
     // Nothing is left to further kernels where nothing is filtered, and up to 32768 logits to a row: a block searches such a row by itself in
-    // 65 us of a call where the kernels take 50 (5 rows of 32000 bf16, top-p 0.95 of a flat row), but the calls that leave nothing, the
+    // 54 us of a call where the kernels take 50 (5 rows of 32000 bf16, top-p 0.95 of a flat row), but the calls that leave nothing, the
     // usual ones, pay some 5 us for three empty launches (25.4 against 30.2 with top-p 0.9 of a peaked row, 21.9 against 26.3 with k = 20).
     if ((!top_p && !top_k && !min_p) || desc->n_vocab <= 32768) a.max_left = 0;
     const hipError_t e = fka::launch_sample(a, static_cast<hipStream_t>(stream));

@@ -695,8 +695,17 @@ __device__ inline void sample_from_part(const SampleArgs &a, int r, const T *row
     }
 }
 
-// Draws from all that the threshold and min-p keep: the kept weights of each part of the row, then the part, the thread and the place
-// where the sum passes the mark.
+// The part, by the kept weights of each in s.tile, then the thread and the place where their sum passes the mark.
+template <class T>
+__device__ inline void sample_from_parts(const SampleArgs &a, int r, const T *row, const SampleDraw &draw, const SampleKept &kept,
+                                         const SampleWeight &weight, SampleShared &s)
+{
+    constexpr int PART = kSampleThreads * SampleRow<T>::VEC;
+    const SamplePart at = sample_part(s.tile, (a.n_vocab + PART - 1) / PART, [&](u64 total) { return draw.mark(total); });
+    sample_from_part<PART>(a, r, row, at.part * PART, [&](u64) { return at.mark; }, (double)at.total, s, draw, kept, weight);
+}
+
+// Draws from all that the threshold and min-p keep: the kept weights of each part of the row, then as above.
 template <class T>
 __device__ inline void sample_from_row(const SampleArgs &a, int r, const T *row, const SampleDraw &draw, const SampleKept &kept,
                                        const SampleWeight &weight, SampleShared &s)
@@ -717,8 +726,7 @@ __device__ inline void sample_from_row(const SampleArgs &a, int r, const T *row,
         if ((tid & 63) == 0 && sum) atomicAdd(&s.tile[i / PART], sum);
     });
     __syncthreads();
-    const SamplePart at = sample_part(s.tile, parts, [&](u64 total) { return draw.mark(total); });
-    sample_from_part<PART>(a, r, row, at.part * PART, [&](u64) { return at.mark; }, (double)at.total, s, draw, kept, weight);
+    sample_from_parts(a, r, row, draw, kept, weight, s);
 }
 
 // Lane i: tile i's share of the sum of all weights, in units of the largest one's 2^-44: 0 for a tile whose largest rounds to 0 there.
@@ -761,17 +769,18 @@ struct SampleNucleusBin {
     __device__ inline int operator()(float x) const { return x == max ? 0 : (int)fminf((max - x) * step, (float)(kSampleLeftBins - 1)); }
 };
 
-// The threshold of top-p alone, by one block: the histogram of the weights, the list of the bin where their sum passes the limit; false where
-// that does not fit.
+// top-p alone, by one block: the histogram of the weights; the list of the bin where their sum passes the limit, and the sums of each part's
+// weights above it; the draw.  False where the list does not fit.
 template <class T>
-__device__ inline bool sample_nucleus(const T *row, int n, const SampleWeight &weight, uint32_t max_key, float t, double limit,
-                                      SampleShared &s, SampleKept &kept)
+__device__ inline bool sample_nucleus(const SampleArgs &a, int r, const T *row, const SampleDraw &draw, const SampleWeight &weight,
+                                      uint32_t max_key, double limit, SampleShared &s)
 {
-    constexpr int VEC = SampleRow<T>::VEC;
-    const int tid = threadIdx.x;
-    const SampleNucleusBin bin(max_key, t);
+    constexpr int VEC = SampleRow<T>::VEC, PART = kSampleThreads * VEC;
+    const int tid = threadIdx.x, n = a.n_vocab, parts = (n + PART - 1) / PART;
+    const SampleNucleusBin bin(max_key, draw.t);
     sample_clear(s);
     if (tid == 0) s.count = 0;
+    if (tid < parts) s.tile[tid] = 0;
     sample_walk(row, n, [&](const uint32_t(&x)[VEC], int) {
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
@@ -784,8 +793,16 @@ __device__ inline bool sample_nucleus(const T *row, int n, const SampleWeight &w
     const int border = sample_bin(limit, 0, s, front);
     sample_walk(row, n, [&](const uint32_t(&x)[VEC], int i) {
         uint32_t take = 0;
+        u64 sum = 0;
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) take |= x[j] > kNoLogit && bin(sample_logit(x[j])) == border ? 1u << j : 0;
+        for (int j = 0; j < VEC; ++j) {
+            const int b = x[j] > kNoLogit ? bin(sample_logit(x[j])) : kSampleLeftBins;
+            take |= b == border ? 1u << j : 0;
+            const u64 w = b < border ? weight(x[j]) : 0;
+            sum += w >= draw.least ? w : 0;
+        }
+        sum = sample_wave_sum(sum);
+        if ((tid & 63) == 0 && sum) atomicAdd(&s.tile[i / PART], sum);
         sample_append(s.list, &s.count, take, x, i);
     });
     __syncthreads();
@@ -794,7 +811,10 @@ __device__ inline bool sample_nucleus(const T *row, int n, const SampleWeight &w
     for (int i = tid; i < count; i += kSampleThreads) s.weight[i] = weight((uint32_t)(s.list[i] >> 32));
     __syncthreads();
     const u64 last = sample_list_select(count, 0, limit, front, s, [&](int i) { return s.weight[i]; });
-    kept = SampleKept{(uint32_t)(last >> 32), (int)~(uint32_t)last};
+    for (int i = tid; i < count; i += kSampleThreads)
+        if (s.list[i] >= last && s.weight[i] >= draw.least) atomicAdd(&s.tile[~(uint32_t)s.list[i] / PART], s.weight[i]);
+    __syncthreads();
+    sample_from_parts(a, r, row, draw, SampleKept{(uint32_t)(last >> 32), (int)~(uint32_t)last}, weight, s);
     return true;
 }
 
@@ -976,10 +996,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(SampleArgs a
         __syncthreads();
     }
     if (nucleus && sample_leave(a, s, SampleLeft{limit, 0, r, max_key, 0, SampleLeft::kNucleus, 0.f})) return;
-    SampleKept kept{0, n};
-    if (by_rank && !(nucleus && sample_nucleus(row, n, weight, max_key, draw.t, limit, s, kept)))
-        kept = sample_whole_row(row, n, weight, draw, limit, s);
-    sample_from_row(a, r, row, draw, kept, weight, s);
+    if (nucleus && sample_nucleus(a, r, row, draw, weight, max_key, limit, s)) return;
+    sample_from_row(a, r, row, draw, by_rank ? sample_whole_row(row, n, weight, draw, limit, s) : SampleKept{0, n}, weight, s);
 }
 
 // The rows that are left: block c of the a.shares of a row takes every a.shares-th tile of it.
