@@ -47,24 +47,24 @@ constexpr uint32_t kNoLogit = 0x007fffffu;        // the key of -inf (NaN counts
 
 typedef unsigned long long u64;
 
-// 2^(j / 64), to nearest
+// 2^(44 + j / 64), to nearest
 __device__ const double kSampleTable[64] = {
-    0x1.0000000000000p+0, 0x1.02c9a3e778061p+0, 0x1.059b0d3158574p+0, 0x1.0874518759bc8p+0,
-    0x1.0b5586cf9890fp+0, 0x1.0e3ec32d3d1a2p+0, 0x1.11301d0125b51p+0, 0x1.1429aaea92de0p+0,
-    0x1.172b83c7d517bp+0, 0x1.1a35beb6fcb75p+0, 0x1.1d4873168b9aap+0, 0x1.2063b88628cd6p+0,
-    0x1.2387a6e756238p+0, 0x1.26b4565e27cddp+0, 0x1.29e9df51fdee1p+0, 0x1.2d285a6e4030bp+0,
-    0x1.306fe0a31b715p+0, 0x1.33c08b26416ffp+0, 0x1.371a7373aa9cbp+0, 0x1.3a7db34e59ff7p+0,
-    0x1.3dea64c123422p+0, 0x1.4160a21f72e2ap+0, 0x1.44e086061892dp+0, 0x1.486a2b5c13cd0p+0,
-    0x1.4bfdad5362a27p+0, 0x1.4f9b2769d2ca7p+0, 0x1.5342b569d4f82p+0, 0x1.56f4736b527dap+0,
-    0x1.5ab07dd485429p+0, 0x1.5e76f15ad2148p+0, 0x1.6247eb03a5585p+0, 0x1.6623882552225p+0,
-    0x1.6a09e667f3bcdp+0, 0x1.6dfb23c651a2fp+0, 0x1.71f75e8ec5f74p+0, 0x1.75feb564267c9p+0,
-    0x1.7a11473eb0187p+0, 0x1.7e2f336cf4e62p+0, 0x1.82589994cce13p+0, 0x1.868d99b4492edp+0,
-    0x1.8ace5422aa0dbp+0, 0x1.8f1ae99157736p+0, 0x1.93737b0cdc5e5p+0, 0x1.97d829fde4e50p+0,
-    0x1.9c49182a3f090p+0, 0x1.a0c667b5de565p+0, 0x1.a5503b23e255dp+0, 0x1.a9e6b5579fdbfp+0,
-    0x1.ae89f995ad3adp+0, 0x1.b33a2b84f15fbp+0, 0x1.b7f76f2fb5e47p+0, 0x1.bcc1e904bc1d2p+0,
-    0x1.c199bdd85529cp+0, 0x1.c67f12e57d14bp+0, 0x1.cb720dcef9069p+0, 0x1.d072d4a07897cp+0,
-    0x1.d5818dcfba487p+0, 0x1.da9e603db3285p+0, 0x1.dfc97337b9b5fp+0, 0x1.e502ee78b3ff6p+0,
-    0x1.ea4afa2a490dap+0, 0x1.efa1bee615a27p+0, 0x1.f50765b6e4540p+0, 0x1.fa7c1819e90d8p+0,
+    0x1.0000000000000p+44, 0x1.02c9a3e778061p+44, 0x1.059b0d3158574p+44, 0x1.0874518759bc8p+44,
+    0x1.0b5586cf9890fp+44, 0x1.0e3ec32d3d1a2p+44, 0x1.11301d0125b51p+44, 0x1.1429aaea92de0p+44,
+    0x1.172b83c7d517bp+44, 0x1.1a35beb6fcb75p+44, 0x1.1d4873168b9aap+44, 0x1.2063b88628cd6p+44,
+    0x1.2387a6e756238p+44, 0x1.26b4565e27cddp+44, 0x1.29e9df51fdee1p+44, 0x1.2d285a6e4030bp+44,
+    0x1.306fe0a31b715p+44, 0x1.33c08b26416ffp+44, 0x1.371a7373aa9cbp+44, 0x1.3a7db34e59ff7p+44,
+    0x1.3dea64c123422p+44, 0x1.4160a21f72e2ap+44, 0x1.44e086061892dp+44, 0x1.486a2b5c13cd0p+44,
+    0x1.4bfdad5362a27p+44, 0x1.4f9b2769d2ca7p+44, 0x1.5342b569d4f82p+44, 0x1.56f4736b527dap+44,
+    0x1.5ab07dd485429p+44, 0x1.5e76f15ad2148p+44, 0x1.6247eb03a5585p+44, 0x1.6623882552225p+44,
+    0x1.6a09e667f3bcdp+44, 0x1.6dfb23c651a2fp+44, 0x1.71f75e8ec5f74p+44, 0x1.75feb564267c9p+44,
+    0x1.7a11473eb0187p+44, 0x1.7e2f336cf4e62p+44, 0x1.82589994cce13p+44, 0x1.868d99b4492edp+44,
+    0x1.8ace5422aa0dbp+44, 0x1.8f1ae99157736p+44, 0x1.93737b0cdc5e5p+44, 0x1.97d829fde4e50p+44,
+    0x1.9c49182a3f090p+44, 0x1.a0c667b5de565p+44, 0x1.a5503b23e255dp+44, 0x1.a9e6b5579fdbfp+44,
+    0x1.ae89f995ad3adp+44, 0x1.b33a2b84f15fbp+44, 0x1.b7f76f2fb5e47p+44, 0x1.bcc1e904bc1d2p+44,
+    0x1.c199bdd85529cp+44, 0x1.c67f12e57d14bp+44, 0x1.cb720dcef9069p+44, 0x1.d072d4a07897cp+44,
+    0x1.d5818dcfba487p+44, 0x1.da9e603db3285p+44, 0x1.dfc97337b9b5fp+44, 0x1.e502ee78b3ff6p+44,
+    0x1.ea4afa2a490dap+44, 0x1.efa1bee615a27p+44, 0x1.f50765b6e4540p+44, 0x1.fa7c1819e90d8p+44,
 };
 
 // Bits in the order of the logits; -0 equals 0.
@@ -101,7 +101,7 @@ struct SampleWeight {
         if ((double)x == max) return kSampleUnit;
         const double z = times64(x, -64.0 * 1000), n = rint(z);
         const int m = (int)n;
-        return ldexp(table[m & 63] * series(z - n), (m >> 6) + 44);
+        return ldexp(table[m & 63] * series(z - n), m >> 6);
     }
     // The weight + kMark.  What is below 2^-60 of the largest rounds to 0.
     static constexpr u64 kMark = 0x4330000000000000ull;
@@ -110,9 +110,9 @@ struct SampleWeight {
         const double z = times64(x, -64.0 * 60), n = rint(z), p = series(z - n);
         const int m = (int)n;
         const double y = table[m & 63] * p;
-        const u64 scaled = (u64)__double_as_longlong(y) + ((u64)(uint32_t)((m >> 6) + 44) << 52);
+        const double scaled = __hiloint2double(__double2hiint(y) + (int)((uint32_t)(m & ~63) << 14), __double2loint(y));  // 2^(m / 64), below
         // 2^52 added rounds to a whole number in the lowest bits
-        return (u64)__double_as_longlong(__longlong_as_double((long long)scaled) + 4503599627370496.0);
+        return (u64)__double_as_longlong(scaled + 4503599627370496.0);
     }
     __device__ inline u64 operator()(uint32_t key) const
     {
