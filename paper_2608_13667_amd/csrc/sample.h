@@ -23,7 +23,7 @@
 //
 // One block to a row for all of it, by digits from memory, took 64 us for 5 rows of 32000 bf16, 556 for 320 of 128000 fp32 (a quarter of them
 // top-p alone) and 111 for 80 of 200003 bf16, nothing filtered.  Now 20 to 32 (a row with k = 1000 is the
-// slowest of such a call), 103 and 23.7.  The scan is bound by memory (164 MB in 28 us, 5.9 TB/s) or, with sums, by fp64 exponentials (16 million
+// slowest of such a call), 102 and 23.2.  The scan is bound by memory (164 MB in 28 us, 5.9 TB/s) or, with sums, by fp64 exponentials (16 million
 // in 18 us); the row kernel by latency, some twenty steps between barriers (7 us where nothing is filtered, 14 with k = 50 and p,
 // 20 over 320 rows); the three kernels behind it by their start, their loads and the list's (12, 23 and 17).
 #pragma once
