@@ -455,7 +455,8 @@ typedef struct {
     int64_t logits_stride; /* elements from one row to the next, >= n_vocab (any: rows need not be aligned) */
 } fka_sample_desc;
 
-/* Device bytes of fka_sample's workspace (0 for sizes that it refuses). */
+/* Device bytes of fka_sample's workspace (0 for sizes that it refuses).  They fall neither with n_rows nor with n_vocab: a workspace for
+ * the largest call serves every smaller one. */
 size_t fka_sample_bytes(int32_t n_rows, int32_t n_vocab);
 
 /*
@@ -476,7 +477,7 @@ size_t fka_sample_bytes(int32_t n_rows, int32_t n_vocab);
  *   tokens                     int32 [n_rows]
  *   logprob                    fp32 [n_rows] or NULL: ln(w / S) of the token (0 at temperature 0, -inf for the token -1)
  *   err                        int32 (device) or NULL
- *   workspace                  fka_sample_bytes(n_rows, n_vocab) device bytes (16-byte aligned), used by one call at a time; its contents before
+ *   workspace                  fka_sample_bytes(n_rows, n_vocab) device bytes or more (16-byte aligned), used by one call at a time; its contents before
  *                              and after do not matter
  * What is written, the workspace too, may overlap neither itself nor what is read (FKA_ERR_INVALID_ARG).  FKA_ERR_UNSUPPORTED for more than
  * 2^18 logits or 2^17 rows.  The same call gives the same bits.

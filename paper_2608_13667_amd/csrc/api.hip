@@ -2456,12 +2456,16 @@ fka_status fka_tree_accept_paged(const fka_accept_desc *desc, const int32_t *par
                       stream);
 }
 
-// Lays the workspace out (n_rows and n_vocab given); its bytes.
+// Lays the workspace out (n_rows and n_vocab given); its bytes.  They fall neither with n_rows nor with n_vocab, so that a workspace of the
+// largest call serves the others: the shares and groups of a call are given the room of the most that a smaller one has.
 static size_t sample_layout(fka::SampleArgs &a, char *at)
 {
-    const size_t R = a.n_rows, tiles = ceil_div(a.n_vocab, fka::kSampleTile), groups = ceil_div(a.n_vocab, fka::sample_group_of(a.n_vocab));
+    const size_t R = a.n_rows, tiles = ceil_div(a.n_vocab, fka::kSampleTile);
+    const size_t groups = std::min(ceil_div(a.n_vocab, 16), fka::kSampleGroups);  // (groups of 64 are fewer)
+    constexpr int32_t kShares = 4096;
     a.max_left = std::min(a.n_rows, fka::kSampleMaxLeft);
-    a.shares = std::max(1, std::min((int32_t)tiles, 4096 / std::max(1, a.max_left)));
+    a.shares = std::max(1, std::min((int32_t)tiles, kShares / std::max(1, a.max_left)));
+    const size_t shares = std::min<size_t>(kShares, a.max_left * tiles);  // at least max_left x a.shares
     size_t bytes = 0;
     auto take = [&](auto *&p, size_t n) {
         using X = std::remove_reference_t<decltype(*p)>;
@@ -2471,7 +2475,7 @@ static size_t sample_layout(fka::SampleArgs &a, char *at)
     take(a.n_left, 1);
     take(a.left, a.max_left);
     take(a.list, (size_t)a.max_left * fka::kSampleList);
-    take(a.hist, (size_t)a.max_left * a.shares * fka::kSampleLeftBins);
+    take(a.hist, shares * fka::kSampleLeftBins);
     take(a.tile_sum, R * tiles);
     take(a.tile_max, R * tiles);
     take(a.group_max, R * groups);

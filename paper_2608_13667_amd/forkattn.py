@@ -775,7 +775,7 @@ def tree_layout(parents, base, masks, positions, *, err=None, stream=None):
 
 
 def sample_workspace(n_rows, n_vocab, device="cuda"):
-    """A workspace for sample over up to n_rows rows of n_vocab logits."""
+    """A workspace for sample over up to n_rows rows of up to n_vocab logits."""
     return torch.empty(_lib.fka_sample_bytes(n_rows, n_vocab), dtype=torch.uint8, device=device)
 
 

@@ -348,3 +348,23 @@ def test_two_streams_at_once(fa):
 def test_no_rows(fa):
     empty = torch.empty(0, dtype=torch.int32, device="cuda")
     fa.sample(torch.empty(0, 10, device="cuda"), torch.empty(0, device="cuda"), empty, workspace=fa.sample_workspace(0, 10))
+
+
+def test_one_workspace_for_calls_of_many_sizes(fa):
+    """A workspace of the largest call, its bytes left as they are, serves fewer rows and smaller vocabularies; where a smaller call has more
+    shares of a row or more groups than the largest, too."""
+    rng = np.random.default_rng(6)
+    R, V = 84, 200003
+    work = fa.sample_workspace(R, V)
+    work.fill_(255)
+    x = _logits(rng, R, V, True).cuda()
+    f32 = lambda v: torch.tensor(np.asarray(v, np.float32), device="cuda")  # noqa: E731
+    u, t, p = f32(rng.random(R)), f32(rng.choice([0.7, 2.0], R)), f32(rng.choice([1.0, 0.95], R))
+    k = torch.tensor(rng.choice([0, 0, 50, 700], R).astype(np.int32), device="cuda")
+    for r, v in ((84, 200003), (83, 200003), (1, 200003), (84, 65536), (40, 70001), (84, 20000), (3, 100), (84, 200003)):
+        rows = [a[:r] for a in (u, t, p, k)]
+        got, want = (torch.empty(r, dtype=torch.int32, device="cuda") for _ in "gw")
+        lp, lp_want = (torch.empty(r, device="cuda") for _ in "gw")
+        for tokens, logprob, w in ((got, lp, work), (want, lp_want, fa.sample_workspace(r, v))):
+            fa.sample(x[:r, :v], rows[0], tokens, logprob, temperature=rows[1], top_p=rows[2], top_k=rows[3], workspace=w)
+        assert torch.equal(got, want) and torch.equal(lp, lp_want), (r, v)

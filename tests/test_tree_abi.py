@@ -190,3 +190,17 @@ def test_sample_binding_checks_shapes(fa):
         fa.sample(f(2, 5), f(3), i, workspace=w)
     with pytest.raises(ValueError, match="on the GPU"):
         fa.sample(f(2, 5), f(2), i, workspace=w)
+
+
+def test_sample_workspace_of_a_larger_call_serves_a_smaller_one(fa):
+    """The bytes fall neither with the rows nor with the vocabulary."""
+    size = lambda r, v: fa.raw_call("fka_sample_bytes", r, v)  # noqa: E731
+    many = sorted({*range(0, 1100), *(2**k + e for k in range(10, 17) for e in (-1, 0, 1)), 2**17})
+    for v in (1, 100, 4097, 32000, 32768, 32769, 50000, 65536, 65537, 128000, 200003, 2**18):
+        of = [size(r, v) for r in many]
+        assert all(x > 0 for x in of)
+        assert [(r, v) for r, x, y in zip(many[1:], of, of[1:]) if y < x] == []
+    words = sorted({1, 2, *(at + e for at in range(4096, 2**18 + 1, 4096) for e in (-1, 0, 1) if at + e <= 2**18)})
+    for r in (0, 1, 5, 63, 64, 65, 320, 819, 820, 1024, 1025, 5000, 2**17):
+        of = [size(r, v) for v in words]
+        assert [(r, v) for v, x, y in zip(words[1:], of, of[1:]) if y < x] == []
