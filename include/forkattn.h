@@ -413,7 +413,8 @@ fka_status fka_prefill_paged(const fka_plan *plan, const void *q, const void *k_
  *   fka_rotate_append  (for each layer) the nodes' K and V at suffix positions [suffix_len[b], suffix_len[b] + n), advance = 0
  *   fka_tree_attend    (for each layer) every node over the prefix, its branch's suffix and the nodes that it reads
  *   fka_sample         the token that the model chooses behind each node
- *   fka_tree_accept    (for each layer) the nodes that these tokens confirm stay in the cache
+ *   fka_tree_accept    (for each layer) the nodes that these tokens confirm stay in the cache; where the layers share suffix_len, advance = 1
+ *                      with the last of them only: each call finds the nodes' rows behind it
  */
 
 /*
@@ -492,7 +493,7 @@ typedef struct {
     int32_t n_kv_heads;
     int32_t head_dim;   /* 64 or 128 */
     int32_t max_len;    /* bound on suffix_len[b] + n (contiguous: at most suffix_cap) */
-    int32_t advance;    /* 1: suffix_len[b] += count[b] (0: the caller advances it: one layer of several) */
+    int32_t advance;    /* 1: suffix_len[b] += count[b] (0: it stays: every layer but the last of those that share it) */
 } fka_accept_desc;
 
 /*

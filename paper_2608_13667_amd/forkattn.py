@@ -809,7 +809,8 @@ def _accept_tree(parents, masks, tokens, targets, path, count, next_token, suffi
 def tree_accept(parents, masks, tokens, targets, suffix_k, suffix_v, suffix_len, path, count, next_token, *, max_len=None,
                 advance=True, err=None, stream=None):
     """fka_tree_accept: the nodes that targets int32 [N][n] (chosen behind each node) confirm -> path int32 [N][n], count and
-    next_token int32 [N]; their rows of suffix_k / suffix_v bf16 [N][Hkv][cap][d] move behind suffix_len int32 [N]."""
+    next_token int32 [N]; their rows of suffix_k / suffix_v bf16 [N][Hkv][cap][d] move behind suffix_len int32 [N], which `advance` moves
+    on by count: where several layers share it, every call but the last layer's needs advance=False."""
     dev, tree, result = _accept_tree(parents, masks, tokens, targets, path, count, next_token, suffix_len)
     N, n = parents.shape
     if suffix_k.dim() != 4 or suffix_k.shape[0] != N or suffix_v.shape != suffix_k.shape:
@@ -822,7 +823,8 @@ def tree_accept(parents, masks, tokens, targets, suffix_k, suffix_v, suffix_len,
 
 def tree_accept_paged(parents, masks, tokens, targets, k_pool, v_pool, page_table, prefix_len, suffix_len, path, count, next_token, *,
                       max_len=None, advance=True, err=None, stream=None):
-    """fka_tree_accept_paged: as tree_accept, in the pages of page_table int32 [N][max_pages] behind prefix_len int32 [N]."""
+    """fka_tree_accept_paged: as tree_accept, in the pages of page_table int32 [N][max_pages] behind prefix_len int32 [N] (advance=False in every
+    call but the last layer's here too)."""
     dev, tree, result = _accept_tree(parents, masks, tokens, targets, path, count, next_token, suffix_len)
     N, n = parents.shape
     if k_pool.dim() != 4 or k_pool.shape[2] != 16 or v_pool.shape != k_pool.shape:

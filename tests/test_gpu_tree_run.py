@@ -1,6 +1,8 @@
 """The operators of drafted trees together, as a serving program runs them: a small model of one attention layer decodes greedily,
 token by token with the plain step, and again with trees of drafted tokens, some of them right.  Both give the same tokens,
 and after each step the same cache rows bit for bit."""
+import os
+
 import numpy as np
 import pytest
 import torch
@@ -156,3 +158,60 @@ def test_trees_decode_what_single_tokens_do(fa, paged, n):
     assert cache.lens.tolist() == [len(g) for g in got]
     assert accepted > 0 or n == 1
     assert int(err) == 0 and plan.device_error() == 0
+
+
+class Layer:
+    """One of several layers that share the lengths; `rest` keeps what the cache holds when the nodes are in it."""
+
+    def __init__(self, g, heads, d, n_branches, n, prefix_len, cap):
+        hq, hkv = heads
+        r = lambda *s: torch.randn(*s, generator=g).bfloat16().cuda()  # noqa: E731
+        self.new = r(n_branches, n, hq, d), r(n_branches, n, hkv, d), r(n_branches, n, hkv, d)
+        self.prefix_k, self.prefix_v = r(hkv, prefix_len, d), r(hkv, prefix_len, d)
+        self.suffix_k, self.suffix_v = r(n_branches, hkv, cap, d), r(n_branches, hkv, cap, d)
+
+    def project(self, hidden):
+        return self.new
+
+    def rest(self, hidden, out):
+        self.before = self.suffix_k.clone(), self.suffix_v.clone()
+        return hidden
+
+
+def test_the_documented_step_through_several_layers(fa):
+    """The step of README.md as it stands there, three layers: each layer's accepted rows move together, the lengths advance once."""
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")).read()
+    step = text[text.index("A step with drafted trees"):].split("```python\n")[1].split("```")[0]
+    n_q_heads, n_kv_heads, d, n_branches, n, prefix_len, cap, max_len, vocab = 8, 2, 64, 3, 9, 100, 64, 64, WORDS
+    g = torch.Generator().manual_seed(1)
+    layers = [Layer(g, (n_q_heads, n_kv_heads), d, n_branches, n, prefix_len, cap) for _ in range(3)]
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    start = [0, 17, 40]
+    logits = torch.full((n_branches * n, vocab), -5.0, device="cuda")
+    said = torch.randint(vocab, (n_branches, n), generator=g)  # behind each node
+    logits[torch.arange(n_branches * n, device="cuda"), said.flatten().cuda()] = 9.0
+    parents = [[-1, 0, 0, 2, 3, 2, 5, 4, 7]] * n_branches
+    tokens = said.new_zeros(n_branches, n)
+    for b in range(n_branches):
+        for i in range(1, n):  # wrong at the first child, and (branch by branch) from some depth on
+            tokens[b, i] = (said[b, parents[b][i]] + (i == 1 or i in (5, 6) or (b == 1 and i >= 7))) % vocab
+    names = dict(fa=fa, torch=torch, n_q_heads=n_q_heads, n_kv_heads=n_kv_heads, d=d, n_branches=n_branches, n=n, prefix_len=prefix_len, cap=cap,
+                 max_len=max_len, vocab=vocab, layers=layers, hidden=None, head=lambda hidden: logits, parents=i32(parents), base=i32(start) + prefix_len,
+                 tokens=i32(tokens.tolist()), suffix_len=i32(start), u=torch.zeros(n_branches * n, device="cuda"),
+                 t=torch.zeros(n_branches * n, device="cuda"), p=torch.ones(n_branches * n, device="cuda"),
+                 freq=(1e4 ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)).cuda(),
+                 masks=torch.empty(n_branches, n, dtype=torch.int64, device="cuda"), q_rot=torch.empty(n_branches, n, n_q_heads, d, dtype=torch.bfloat16, device="cuda"),
+                 out=torch.empty(n_branches, n, n_q_heads, d, device="cuda"))
+    for name in ("positions", "path"):
+        names[name] = torch.empty(n_branches, n, dtype=torch.int32, device="cuda")
+    names.update(targets=torch.empty(n_branches * n, dtype=torch.int32, device="cuda"), count=i32([0] * n_branches), next_token=i32([0] * n_branches))
+    exec(step, names)
+    want = [[0, 2, 3, 4, 7, 8], [0, 2, 3, 4], [0, 2, 3, 4, 7, 8]]
+    assert names["path"].tolist() == [w + [-1] * (n - len(w)) for w in want] and names["count"].tolist() == [len(w) for w in want]
+    assert names["suffix_len"].tolist() == [s + len(w) for s, w in zip(start, want)]
+    assert names["next_token"].tolist() == [int(said[b, w[-1]]) for b, w in enumerate(want)]
+    for layer in layers:
+        for cache, before in zip((layer.suffix_k, layer.suffix_v), layer.before):
+            for b, (s, w) in enumerate(zip(start, want)):
+                before[b, :, s: s + len(w)] = before[b, :, [s + i for i in w]].clone()
+            assert torch.equal(cache, before)
