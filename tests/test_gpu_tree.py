@@ -626,3 +626,46 @@ def test_attend_past_four_gib(fa, hq, n, paged):
         plan = fa.Plan.tree_plan(hq, 4, 128, 1, n, L, t.cap, t.cap, softmax_scale=1.0)
         plan.tree_attend(t.dq, k, v, t.cache[2], t.cache[3], t.lens, t.dmasks, t.out, t.lse)
     _close(t, t.want())
+
+
+def _bf16_round(x):
+    m, e = np.frexp(x)
+    return np.ldexp(np.rint(np.ldexp(m, 8)), e - 8)
+
+
+def _adverse_keys():
+    """64 scores whose p = exp(score) lose the most in two bf16 terms (62 of them, and 0 at places 0 and 32, each half's largest), and
+    values of 1 and -1 with the sign of what is lost: the losses add up, while the sums of p v stay near 0."""
+    bits = np.arange(0xbc01, 0xbf30, dtype=np.uint32) << 16  # bf16 from -0.69 to -2^-7
+    x = bits.view(np.float32).astype(np.float64)
+    x = x[(x > -0.69) & (x < -2.0 ** -7)]
+    p = np.exp(x)
+    hi = _bf16_round(p)
+    lost = p - hi - _bf16_round(p - hi)
+    picks = [sorted(np.nonzero(lost * sign > 0)[0][np.argsort(-lost[lost * sign > 0] * sign)][:31], key=lambda i: p[i]) for sign in (1, -1)]
+    pairs = [i for both in zip(*picks) for i in both]
+    s = np.concatenate([[0], x[pairs[:31]], [0], x[pairs[31:]]])
+    v = np.concatenate([[1], np.sign(lost[pairs[:31]]), [-1], np.sign(lost[pairs[31:]])])
+    return s, v, np.abs(lost[pairs]).sum() / np.exp(s).sum()
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,N", [(4, 2, 2), (64, 1, 3)], ids=["halves", "stream"])
+def test_attend_of_few_rows_keeps_three_terms_of_p(fa, hq, hkv, N, d, paged):
+    """A score is one exact product, 64 keys a row.  What a result is off by, in parts of the sum of p (55): p's exponential (a last bit, 2^-23), its argument in (-1, 0]
+    and the scale (2^-25 each, times ln 2) and the third term (2^-27) come to 1.8e-7; six products over 32 keys add in at most 192 roundings of partial sums
+    of at most 3.2, the signs alternating, 6.7e-7.  The division, and a merge of two halves, scale a result near 0.  2^-20 holds all of that; two
+    terms lose four times as much."""
+    s, v, lost = _adverse_keys()
+    assert np.abs(np.cumsum(np.exp(s) * v)).max() < 3.2 and lost > 4 * 2.0 ** -20
+    t = Tree(hq, hkv, d, 1, 0, [63] * N, [[1]] * N, paged, scale=1.0)
+    t.q.zero_()
+    t.q[..., 0] = 1
+    t.sk[:, :, :64, 0] = torch.from_numpy(s).bfloat16()
+    t.sv[:, :, :64] = torch.from_numpy(v).bfloat16()[:, None]
+    assert torch.equal(t.sk[0, 0, :64, 0].double(), torch.from_numpy(s))
+    t.place()
+    t.call(t.plan(fa))
+    want = float((np.exp(s) * v).sum() / np.exp(s).sum())
+    assert float((t.out.double() - want).abs().max()) <= 2.0 ** -20
