@@ -2463,7 +2463,10 @@ static size_t sample_layout(fka::SampleArgs &a, char *at)
     const size_t R = a.n_rows, tiles = ceil_div(a.n_vocab, fka::kSampleTile);
     const size_t groups = std::min(ceil_div(a.n_vocab, 16), fka::kSampleGroups);  // (groups of 64 are fewer)
     constexpr int32_t kShares = 4096;
-    a.max_left = std::min(a.n_rows, fka::kSampleMaxLeft);
+    // Nothing is left to further kernels up to 32768 logits to a row: a block searches such a row by itself in 54 us of a call where the
+    // kernels take 50 (5 rows of 32000 bf16, top-p 0.95 of a flat row), but the calls that leave nothing, the usual ones, pay some 5 us
+    // for three empty launches (25.4 against 30.2 with top-p 0.9 of a peaked row, 21.9 against 26.3 with k = 20).
+    a.max_left = a.n_vocab <= 32768 ? 0 : std::min(a.n_rows, fka::kSampleMaxLeft);
     a.shares = std::max(1, std::min((int32_t)tiles, kShares / std::max(1, a.max_left)));
     const size_t shares = std::min<size_t>(kShares, a.max_left * tiles);  // at least max_left x a.shares
     size_t bytes = 0;
@@ -2542,10 +2545,7 @@ fka_status fka_sample(const fka_sample_desc *desc, const void *logits, const flo
     a.logprob = logprob;
     a.err = err;
     sample_layout(a, static_cast<char *>(workspace));
-    // Nothing is left to further kernels where nothing is filtered, and up to 32768 logits to a row: a block searches such a row by itself in
-    // 54 us of a call where the kernels take 50 (5 rows of 32000 bf16, top-p 0.95 of a flat row), but the calls that leave nothing, the
-    // usual ones, pay some 5 us for three empty launches (25.4 against 30.2 with top-p 0.9 of a peaked row, 21.9 against 26.3 with k = 20).
-    if ((!top_p && !top_k && !min_p) || desc->n_vocab <= 32768) a.max_left = 0;
+    if (!top_p && !top_k && !min_p) a.max_left = 0;  // nothing is filtered: no row is left to further kernels
     const hipError_t e = fka::launch_sample(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "sample kernel launch");
     return ok();

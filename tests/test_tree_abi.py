@@ -204,3 +204,9 @@ def test_sample_workspace_of_a_larger_call_serves_a_smaller_one(fa):
     for r in (0, 1, 5, 63, 64, 65, 320, 819, 820, 1024, 1025, 5000, 2**17):
         of = [size(r, v) for v in words]
         assert [(r, v) for v, x, y in zip(words[1:], of, of[1:]) if y < x] == []
+
+
+def test_sample_workspace_has_no_room_for_rows_that_are_not_shared(fa):
+    """Up to 32768 logits a row's own block searches it: what is left are the tiles' sums and maxima and the groups' maxima, 12 bytes to 4096 logits and 4 to 16."""
+    for r, v in ((320, 32000), (820, 32000), (5, 32768), (2**17, 1000)):
+        assert fa.raw_call("fka_sample_bytes", r, v) <= r * (-(-v // 4096) * 12 + -(-v // 16) * 4) + 8 * 16
