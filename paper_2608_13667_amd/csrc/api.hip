@@ -678,8 +678,19 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
         } else {
             R = std::max(RP, std::min<int64_t>(R, std::min<int64_t>(64, (keys_tiles + 3) / 4)));
         }
-        // the partials of one range: S Hq rows of d floats; the ranges together stay below 256 MiB
-        const int64_t range_bytes = S * p->Hq * (int64_t)p->d * 4;
+        // Up to four units, two waves to each: us a call of 5 branches over 32k keys (40 / 8 heads), one wave to a unit / two: 1 unit
+        // 42.3 / 39.0, 2 units 43.6 / 41.2, 3 46.7 / 45.6, 4 51.5 / 51.2 (40.8 for the first with the third term of p).
+        // More units take the third term and the plain stream of tiles where that costs little: d 128, 8 KV heads, phases / stream 13 units 500 keys
+        // 35.4 / 30.4, 2000 33.3 / 35.0, 8000 43.9 / 52.3, 19000 65 / 86; 50 units 500 keys 37.4 / 39.1, 2000 49.4 / 58.5, 8000 93 / 130;
+        // 7 units 8000 keys 36.0 / 39.4; d 64, 2 KV heads, 10 units 8000 keys 20.3 / 20.4.  Two terms leave 2.4e-6 of a result,
+        // three what fp32 sums leave, 3e-7 over 500 keys, 5e-7 over 30000.
+        if (tree && U <= tile_waves / 2)
+            p->tree_kind = fka::TreeKind::kHalves;
+        else if (tree && (int64_t)U * ((int64_t)Lp + max_suffix_len) <= 100000)
+            p->tree_kind = fka::TreeKind::kStream;
+        // the partials of one range: S Hq rows of d floats, twice where two waves share a unit; the ranges together stay below 256 MiB
+        const int32_t parts = p->tree_kind == fka::TreeKind::kHalves ? 2 : 1;
+        const int64_t range_bytes = S * p->Hq * (int64_t)p->d * 4 * parts;
         R = std::max<int64_t>(1, std::min<int64_t>(R, ((int64_t)256 << 20) / range_bytes));
         RP = std::min(R, RP);
         p->prefill_tiles = true;
@@ -706,17 +717,7 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
         p->prefill_groups = tile_waves;
         p->n_blocks = (int32_t)(base * R);
         p->rounds = 1;
-        // Up to four units, two waves to each: us a call of 5 branches over 32k keys (40 / 8 heads), one wave to a unit / two: 1 unit
-        // 42.3 / 39.0, 2 units 43.6 / 41.2, 3 46.7 / 45.6, 4 51.5 / 51.2 (40.8 for the first with the third term of p).
-        // More units take the third term and the plain stream of tiles where that costs little: d 128, 8 KV heads, phases / stream 13 units 500 keys
-        // 35.4 / 30.4, 2000 33.3 / 35.0, 8000 43.9 / 52.3, 19000 65 / 86; 50 units 500 keys 37.4 / 39.1, 2000 49.4 / 58.5, 8000 93 / 130;
-        // 7 units 8000 keys 36.0 / 39.4; d 64, 2 KV heads, 10 units 8000 keys 20.3 / 20.4.  Two terms leave 2.4e-6 of a result,
-        // three what fp32 sums leave, 3e-7 over 500 keys, 5e-7 over 30000.
-        if (tree && U <= tile_waves / 2)
-            p->tree_kind = fka::TreeKind::kHalves;
-        else if (tree && (int64_t)U * ((int64_t)Lp + max_suffix_len) <= 100000)
-            p->tree_kind = fka::TreeKind::kStream;
-        p->n_slots = (int32_t)R * (p->tree_kind == fka::TreeKind::kHalves ? 2 : 1);
+        p->n_slots = (int32_t)R * parts;
         fka_status st = finish_plan(p);
         if (st != FKA_OK) return bail(st);
         *out = p;

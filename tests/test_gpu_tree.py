@@ -669,3 +669,16 @@ def test_attend_of_few_rows_keeps_three_terms_of_p(fa, hq, hkv, N, d, paged):
     t.call(t.plan(fa))
     want = float((np.exp(s) * v).sum() / np.exp(s).sum())
     assert float((t.out.double() - want).abs().max()) <= 2.0 ** -20
+
+
+def test_plans_keep_their_partial_results_below_256_mib(fa):
+    """However many blocks the caller asks for, also where two waves share a unit and write a part each."""
+    for heads, n, paged in (((128, 64, 128), 64, False), ((128, 64, 128), 64, True), ((64, 64, 64), 8, False), ((640, 64, 128), 16, False)):
+        if paged:
+            plan = fa.Plan.tree_paged_plan(*heads, 1, n, 64 * 300, 1300, 1300, n, blocks=64 * 300)
+        else:
+            plan = fa.Plan.tree_plan(*heads, 1, n, 64 * 300, n, n, blocks=64 * 300)
+        info = plan.info()
+        rows = n * heads[0] * info.n_slots
+        assert info.n_slots > 8 and rows * heads[2] * 4 <= 256 << 20 and info.workspace_bytes <= (256 << 20) + rows * 4 + (8 << 20)
+        plan.close()
