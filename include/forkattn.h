@@ -442,6 +442,7 @@ fka_status fka_plan_create_tree_paged(const fka_heads *heads, const fka_prefill_
  *          included or not (bits from n on are ignored); a row without any key gets out = 0 and out_lse = -inf.
  * A key that no bit shows has no influence on a row, whatever it holds.  A non-finite value of a suffix or node's V makes the rows that
  * read its key NaN.
+ * out and out_lse may overlap neither each other nor the caches, page_table, suffix_len or masks (FKA_ERR_INVALID_ARG); q may be theirs.
  */
 fka_status fka_tree_attend(const fka_plan *plan, const void *q, const void *prefix_k, const void *prefix_v, const void *suffix_k,
                            const void *suffix_v, const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse,

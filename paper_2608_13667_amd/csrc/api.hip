@@ -6,6 +6,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 #include <set>
@@ -1400,6 +1401,18 @@ fka_status fka_fork_decode_noalloc(const fka_heads *heads, const fka_contig_desc
     return run_decode(&p, a, suffix_len, out, out_lse, static_cast<hipStream_t>(stream));
 }
 
+// What a tree plan's call writes: out and out_lse come from a kernel behind the one that reads the inputs, so that a reused q does no harm, but
+// the caches, lengths and masks are the caller's beyond the call.
+static fka_status check_tree_apart(const fka_plan *p, const float *out, const float *out_lse, std::initializer_list<Span> read)
+{
+    const size_t rows = (size_t)p->n_seqs * p->Hq;
+    const Span o{out, rows * p->d * 4, "out"}, lse{out_lse, rows * 4, "out_lse"};
+    REQUIRE(!overlap(o, lse), "out overlaps out_lse");
+    for (const Span &r : read)
+        for (const Span *w : {&o, &lse}) REQUIRE(!overlap(*w, r), "%s overlaps %s", w->name, r.name);
+    return FKA_OK;
+}
+
 // masks: a tree plan's
 static fka_status prefill_contig(const fka_plan *p, const void *q, const void *prefix_k, const void *prefix_v, const void *suffix_k,
                                  const void *suffix_v, const int32_t *suffix_len, const uint64_t *masks, float *out, float *out_lse,
@@ -1415,6 +1428,17 @@ static fka_status prefill_contig(const fka_plan *p, const void *q, const void *p
     REQUIRE_PTR4(suffix_len);
     REQUIRE_PTR16(out);
     REQUIRE_OPT4(out_lse);
+    if (masks) {
+        const size_t row = (size_t)p->d * 2, prefix = (size_t)p->Hkv * p->prefix_len * row, suffix = (size_t)p->n_branches * p->Hkv * p->suffix_cap * row;
+        const fka_status st = check_tree_apart(p, out, out_lse,
+                                               {{prefix_k, prefix, "prefix_k"},
+                                                {prefix_v, prefix, "prefix_v"},
+                                                {suffix_k, suffix, "suffix_k"},
+                                                {suffix_v, suffix, "suffix_v"},
+                                                {suffix_len, (size_t)p->n_branches * 4, "suffix_len"},
+                                                {masks, (size_t)p->n_seqs * 8, "masks"}});
+        if (st != FKA_OK) return st;
+    }
     fka::AttnArgs a = attn_args(p);
     a.q = static_cast<const uint16_t *>(q);
     a.prefix_k = static_cast<const uint16_t *>(prefix_k);
@@ -1436,6 +1460,16 @@ static fka_status prefill_pool(const fka_plan *p, const void *q, const void *k_p
     REQUIRE_PTR4(suffix_len);
     REQUIRE_PTR16(out);
     REQUIRE_OPT4(out_lse);
+    if (masks) {
+        const size_t pool = (size_t)p->n_pool_pages * p->Hkv * fka::kPageSize * p->d * 2;
+        const fka_status st = check_tree_apart(p, out, out_lse,
+                                               {{k_pool, pool, "k_pool"},
+                                                {v_pool, pool, "v_pool"},
+                                                {page_table, (size_t)p->n_branches * p->max_pages * 4, "page_table"},
+                                                {suffix_len, (size_t)p->n_branches * 4, "suffix_len"},
+                                                {masks, (size_t)p->n_seqs * 8, "masks"}});
+        if (st != FKA_OK) return st;
+    }
     fka::AttnArgs a = attn_args(p);
     a.q = static_cast<const uint16_t *>(q);
     a.k_pool = static_cast<const uint16_t *>(k_pool);

@@ -682,3 +682,35 @@ def test_plans_keep_their_partial_results_below_256_mib(fa):
         rows = n * heads[0] * info.n_slots
         assert info.n_slots > 8 and rows * heads[2] * 4 <= 256 << 20 and info.workspace_bytes <= (256 << 20) + rows * 4 + (8 << 20)
         plan.close()
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+def test_attend_refuses_outputs_upon_what_outlives_the_call(fa, paged):
+    """out and out_lse upon each other, the caches, the page table, the lengths and the masks; behind or upon q they may be."""
+    t = Tree(8, 2, 64, 4, 64, [10, 20], _trees(1, 2, 4), paged, seed=3)
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    torch.cuda.synchronize()
+    want, lse = t.out.clone(), t.lse.clone()
+    inputs = dict(zip(("k_pool", "v_pool", "page_table") if paged else ("prefix_k", "prefix_v", "suffix_k", "suffix_v"), t.cache),
+                  suffix_len=t.lens, masks=t.dmasks)
+    name = "fka_tree_attend_paged" if paged else "fka_tree_attend"
+    tail = [t.lens.data_ptr(), t.dmasks.data_ptr()]
+
+    def call(out, out_lse):
+        return fa.raw_call(name, plan.handle, t.dq.data_ptr(), *[c.data_ptr() for c in t.cache], *tail, out, out_lse, None)
+
+    for what, x in inputs.items():
+        size = x.numel() * x.element_size()
+        for at in (x.data_ptr(), x.data_ptr() + (size - 1) // 16 * 16):
+            assert call(at, t.lse.data_ptr()) == -1 and f"out overlaps {what}" in fa.last_error()
+            assert call(t.out.data_ptr(), at) == -1 and f"out_lse overlaps {what}" in fa.last_error()
+    assert call(t.out.data_ptr(), t.out.data_ptr() + 4 * t.out.numel() - 4) == -1 and "out overlaps out_lse" in fa.last_error()
+    # q at the start of out's memory
+    both = torch.empty_like(t.out)
+    t.dq = both.view(-1).view(torch.bfloat16)[: t.q.numel()].view(t.q.shape)
+    t.dq.copy_(t.q)
+    t.out = both
+    t.call(plan)
+    assert torch.equal(t.out, want) and torch.equal(t.lse, lse)
