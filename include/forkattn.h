@@ -440,8 +440,9 @@ fka_status fka_plan_create_tree_paged(const fka_heads *heads, const fka_prefill_
  *   masks  uint64 [N][n] (device, 8-byte aligned): node i of branch b reads the whole prefix, b's suffix positions
  *          [0, suffix_len[b]) and position suffix_len[b] + j for every bit j < n of masks[b][i].  Any set of bits will do, its own bit and later nodes'
  *          included or not (bits from n on are ignored); a row without any key gets out = 0 and out_lse = -inf.
- * A key that no bit shows has no influence on a row, whatever it holds.  A non-finite value of a suffix or node's V makes the rows that
- * read its key NaN.
+ * A key that no bit shows has no influence on a row, whatever it holds.  An infinite value of V, in the prefix, a suffix or a node, is that
+ * infinity in its channel of the rows that read its key (both signs: NaN).  A NaN of the prefix's V stays in its channel, one of a suffix or node's makes
+ * the rows that read its key NaN.
  * out and out_lse may overlap neither each other nor the caches, page_table, suffix_len or masks (FKA_ERR_INVALID_ARG); q may be theirs.
  */
 fka_status fka_tree_attend(const fka_plan *plan, const void *q, const void *prefix_k, const void *prefix_v, const void *suffix_k,

@@ -36,7 +36,8 @@
 //     The ranges share these tiles like the others (their number follows from the suffix lengths
 //     on the device).  A non-finite value of a suffix is replaced by zero for the product and the rows
 //     that read its key are made NaN, so that it reaches no row of another branch or of an earlier
-//     token.
+//     token.  (A tree's infinities instead go to their channel of the rows that read them, in a pass over the
+//     suffixes that only a wave that met one makes.)
 // What bounds it: beside a wave that issues matrix products at full rate the other wave of the SIMD
 // gets one vector issue per 8.7 cycles (two per product), so a step cannot be shorter than 2 x 96
 // products (3340 cycles) nor than the two softmaxes' ~225 issue slots each (3900); it takes 3940
@@ -808,6 +809,7 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
     static_assert(!TREE || MT * GRP <= 32, "a row's keys of the lane's groups are bits of a word");
     [[maybe_unused]] uint32_t vis[2] = {~0u, ~0u};  // a tree's row t reads key k of group 2 i + q4 / 2 where bit 8 i + k is set
     uint32_t suffix_groups = 0;  // bit i: that group holds suffix keys (not the prefix's, which every row reads)
+    [[maybe_unused]] uint64_t suffix_inf = 0;  // a tree: not 0 once a suffix value that was replaced was an infinity
 #pragma unroll
     for (int i = 0; i < MT; ++i) lim[0][i] = lim[1][i] = KT;
     int row_bt[2];  // the rows' branch (past every branch beyond the head's rows) << 16 | token
@@ -904,6 +906,7 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
                 // key are made NaN (through their sums), so that it reaches no row of another branch or of
                 // an earlier token (a masked row's p is 0, and 0 times such a value would be NaN).  The
                 // prefix's keys are read by every row: theirs stay in the product, as in the whole tiles.
+                // (A tree's infinities are looked up at the end: they stay in their channel.)
                 uint32_t bits = 0;
 #pragma unroll
                 for (int e = 0; e < PG; ++e)
@@ -920,18 +923,23 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
                     for (int y = 0; y < 2; ++y) {
                         // the exponent bits that count as non-finite (none for the prefix's keys)
                         const uint32_t bad = (suffix_groups >> (2 * kk + y) & 1) ? 0x7f80u : ~0u;
-                        int first = TREE ? 0 : 0x7fffffff;  // (a tree: the bits of all such keys)
+                        int first = TREE ? 0 : 0x7fffffff;  // (a tree: the bits of all keys with a NaN)
+                        [[maybe_unused]] bool inf = false;
 #pragma unroll
                         for (int e = 0; e < PG; ++e) {
                             uint64_t w = (uint64_t)v[e / EG][e % EG][y];
 #pragma unroll
                             for (int k = 0; k < 4; ++k)
                                 if (((uint32_t)(w >> (16 * k)) & 0x7f80u) == bad) {
-                                    first = TREE ? first | 1 << (k0 + k) : min(first, k0 + k);
+                                    if (TREE && ((uint32_t)(w >> (16 * k)) & 0x7fu) == 0)
+                                        inf = true;
+                                    else
+                                        first = TREE ? first | 1 << (k0 + k) : min(first, k0 + k);
                                     w &= ~((uint64_t)0xffffu << (16 * k));
                                 }
                             v[e / EG][e % EG][y] = (vtr_t)w;
                         }
+                        if constexpr (TREE) suffix_inf |= __builtin_amdgcn_ballot_w64(inf);
 #pragma unroll
                         for (int off = 1; off < 32; off <<= 1) {
                             const int other = __shfl_xor(first, off);
@@ -1119,6 +1127,51 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
                 for (int t = 0; t < 2; ++t)
                     if (l_run[t] < INFINITY && (f == 1 || f == 2)) acc[t][e][j] = f == 1 ? INFINITY : -INFINITY;
             }
+    }
+    // A tree: the suffix values of the unit's branches that are infinite, each added to the channel of the rows that read its key.  (Also those of
+    // other ranges: a row's result holds them all, and where it reads no key of this range its part does not count.)
+    if constexpr (TREE) {
+        if (__builtin_expect(suffix_inf != 0, 0)) {
+            constexpr int CL = HD / 64;
+            const uint32_t at = mask_at();
+            uint64_t row_mask[2] = {ds_read_b64_at<0>(at), ds_read_b64_at<128>(at)};
+            lds_wait();
+            asm volatile("" : "+v"(row_mask[0]), "+v"(row_mask[1]));
+            const int b_z = (min(u * 32 + 32, rows_head) - 1) / a.split.branch_rows;
+            for (int b = (u * 32) / a.split.branch_rows; b <= b_z; ++b) {
+                const int L = min(max(scalar_load(a.suffix_len + b), 0), a.max_suffix_len - n);
+                for (int k = 0; k < L + n; ++k) {
+                    size_t off = ((size_t)b * Hkv + g) * a.suffix_cap + k;
+                    if constexpr (PAGED) {
+                        const int i = (Lp + kPageSize - 1) / kPageSize + k / kPageSize;
+                        const int32_t page = scalar_load(a.page_table + (size_t)b * a.max_pages + min(i, a.max_pages - 1));
+                        if (page < 0 || page >= a.n_pool_pages) continue;
+                        off = ((size_t)page * Hkv + g) * kPageSize + k % kPageSize;
+                    }
+                    const uint16_t *row = reinterpret_cast<const uint16_t *>(PAGED ? pv : reinterpret_cast<const char *>(a.suffix_v)) + off * HD;
+                    uint32_t seen = 0;  // bits 2 i of lane l: channel CL l + i is +inf, -inf
+#pragma unroll
+                    for (int i = 0; i < CL; ++i) {
+                        const uint32_t x = row[CL * lane_c + i];
+                        seen |= (x == 0x7f80u ? 1u : x == 0xff80u ? 2u : 0u) << (2 * i);
+                    }
+                    if (__builtin_amdgcn_ballot_w64(seen != 0) == 0) continue;
+                    bool reads[2];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) reads[t] = row_bt[t] >> 16 == b && (k < L || (row_mask[t] >> (k - L) & 1) != 0);
+#pragma unroll
+                    for (int e = 0; e < NE; ++e)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int c = 16 * e + 4 * q4c + j;
+                            const uint32_t f = (uint32_t)__shfl((int)seen, c / CL) >> (2 * (c % CL)) & 3u;
+#pragma unroll
+                            for (int t = 0; t < 2; ++t)
+                                if (reads[t] && f) acc[t][e][j] += f == 1 ? INFINITY : -INFINITY;
+                        }
+                }
+            }
+        }
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {

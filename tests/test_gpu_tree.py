@@ -714,3 +714,42 @@ def test_attend_refuses_outputs_upon_what_outlives_the_call(fa, paged):
     t.out = both
     t.call(plan)
     assert torch.equal(t.out, want) and torch.equal(t.lse, lse)
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("kind", KINDS, ids=["halves", "stream", "phases"])
+def test_attend_infinite_suffix_values(fa, kind, d, paged):
+    """An infinity of a suffix or node's V is that infinity in its channel of the rows that read its key, both signs there are NaN, and nothing else changes."""
+    hq, hkv, N, n, prefix = kind
+    masks = _trees(11, N, n)
+    t = Tree(hq, hkv, d, n, prefix, [70, 5, 0, 33, 12][:N], masks, paged, seed=3)
+    inf = float("inf")
+    plants = [  # branch (None: the prefix), suffix position, KV head, channel, value
+        (0, 2, 0, 3, inf), (0, 69, 0, d - 1, -inf), (0, 64, 0, 17, inf), (0, 1, 0, 17, -inf),  # committed, the last of them of both signs
+        (1, 5 + n - 1, 1, 9, -inf), (1, 5, 1, 20, inf),                                        # the last node, the root
+        (2, 1, 0, 30, inf), (2, 0, 0, 30, -inf), (2, 2, 1, 31, -inf),                          # nodes of both signs, no committed key
+        (None, 100, 1, 40, inf), (0, 7, 1, 40, -inf), (1, 3, 1, 40, inf),                      # one in the prefix too
+    ]
+    for b, u, g, c, x in plants:
+        (t.pv[g] if b is None else t.sv[b, g])[u, c] = x
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    for b, u, g, c, _ in plants:
+        (t.pv[g] if b is None else t.sv[b, g])[u, c] = 0
+    out, lse, tol, tol_lse = t.want()
+    G = hq // hkv
+    for row in np.ndindex(N, n):
+        for b, u, g, c, x in plants:
+            at = u - t.suffix[row[0]]
+            if b is None or b == row[0] and (at < 0 or int(masks[b][row[1]]) >> at & 1):
+                with np.errstate(invalid="ignore"):
+                    out[row][g * G: (g + 1) * G, c] += x
+    special = ~np.isfinite(out)
+    got = t.out.double().cpu().numpy()
+    assert special.any(-1).any(-1).sum() >= N and np.isnan(out).any() and np.isinf(out).any()
+    assert np.array_equal(got[special], out[special], equal_nan=True)
+    assert (np.abs(got[~special] - out[~special]) <= tol[~special]).all()
+    assert (np.abs(t.lse.double().cpu().numpy() - lse) <= tol_lse).all()
+    assert plan.device_error() == 0
