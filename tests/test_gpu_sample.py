@@ -368,3 +368,24 @@ def test_one_workspace_for_calls_of_many_sizes(fa):
         for tokens, logprob, w in ((got, lp, work), (want, lp_want, fa.sample_workspace(r, v))):
             fa.sample(x[:r, :v], rows[0], tokens, logprob, temperature=rows[1], top_p=rows[2], top_k=rows[3], workspace=w)
         assert torch.equal(got, want) and torch.equal(lp, lp_want), (r, v)
+
+
+@pytest.mark.parametrize("V", [32768, 50000, 128000])
+def test_masked_rows(fa, V):
+    """Rows of which a mask leaves few logits, top-k both less and more than these."""
+    rng = np.random.default_rng(V)
+    picks = [(live, k, p) for live in (1, 30, 3000) for k in (0, 20, 50, 1000, 4000) for p in (1.0, 0.9)]
+    x = np.full((len(picks), V), -np.inf, np.float32)
+    for r, (live, _, _) in enumerate(picks):
+        at = rng.choice(V, live, replace=False)
+        x[r, at] = 2.5 * rng.standard_normal(live)
+    _, k, p = (np.array(c) for c in zip(*picks))
+    _check(fa, torch.from_numpy(x), 0.5 + rng.random(len(picks)), k, p, None, rng.random(len(picks)))
+
+
+@pytest.mark.parametrize("bf16", [False, True], ids=["fp32", "bf16"])
+def test_flat_rows_of_the_largest_vocabulary(fa, bf16):
+    """So flat that thousands of different logits are as near to top-p's threshold as its histogram tells apart."""
+    V, rng = 262144, np.random.default_rng(8)
+    x = torch.from_numpy((2.5 * rng.standard_normal((6, V))).astype(np.float32))
+    _check(fa, x.bfloat16() if bf16 else x, [1.6, 2.0, 2.0, 3.0, 3.0, 1.0], None, [0.95, 0.95, 0.5, 0.3, 0.9, 0.95], [0.0, 0.0, 0.01, 0.0, 0.05, 0.0], rng.random(6))

@@ -753,3 +753,21 @@ def test_attend_infinite_suffix_values(fa, kind, d, paged):
     assert (np.abs(got[~special] - out[~special]) <= tol[~special]).all()
     assert (np.abs(t.lse.double().cpu().numpy() - lse) <= tol_lse).all()
     assert plan.device_error() == 0
+
+
+@pytest.mark.parametrize("paged", [False, True], ids=["contiguous", "paged"])
+@pytest.mark.parametrize("N,n", [(200, 1), (100, 2)])
+def test_attend_more_than_64_branches_in_one_block(fa, N, n, paged):
+    """One query row to a token: a block's rows are of 200 or 100 branches, more than a wave has lanes."""
+    t = Tree(2, 2, 64, n, 40, [i % 7 for i in range(N)], _trees(8, N, n), paged, seed=n)
+    bad = 94  # (suffix of 3)
+    t.sv[bad, 1, 1, 5] = float("inf")
+    t.place()
+    plan = t.plan(fa)
+    t.call(plan)
+    assert (t.out[bad, :, 1, 5] == float("inf")).all()
+    t.sv[bad, 1, 1, 5] = 0
+    want = t.want()
+    t.out[bad, :, 1, 5] = torch.from_numpy(want[0][bad, :, 1, 5]).float().cuda()
+    _close(t, want)
+    assert plan.device_error() == 0
