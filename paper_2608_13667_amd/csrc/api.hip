@@ -681,7 +681,7 @@ fka_status create_prefill(const fka_heads *heads, int32_t N, int32_t n, int32_t 
         }
         // Up to four units, two waves to each: us a call of 5 branches over 32k keys (40 / 8 heads), one wave to a unit / two: 1 unit
         // 42.3 / 39.0, 2 units 43.6 / 41.2, 3 46.7 / 45.6, 4 51.5 / 51.2 (40.8 for the first with the third term of p).
-        // More units take the third term and the plain stream of tiles where that costs little: d 128, 8 KV heads, phases / stream 13 units 500 keys
+        // More units take the third term and the plain stream of tiles where that costs up to a tenth: d 128, 8 KV heads, phases / stream 13 units 500 keys
         // 35.4 / 30.4, 2000 33.3 / 35.0, 8000 43.9 / 52.3, 19000 65 / 86; 50 units 500 keys 37.4 / 39.1, 2000 49.4 / 58.5, 8000 93 / 130;
         // 7 units 8000 keys 36.0 / 39.4; d 64, 2 KV heads, 10 units 8000 keys 20.3 / 20.4.  Two terms leave 2.4e-6 of a result,
         // three what fp32 sums leave, 3e-7 over 500 keys, 5e-7 over 30000.
@@ -2498,9 +2498,11 @@ static size_t sample_layout(fka::SampleArgs &a, char *at)
     const size_t R = a.n_rows, tiles = ceil_div(a.n_vocab, fka::kSampleTile);
     const size_t groups = std::min(ceil_div(a.n_vocab, 16), fka::kSampleGroups);  // (groups of 64 are fewer)
     constexpr int32_t kShares = 4096;
-    // Nothing is left to further kernels up to 32768 logits to a row: a block searches such a row by itself in 54 us of a call where the
-    // kernels take 50 (5 rows of 32000 bf16, top-p 0.95 of a flat row), but the calls that leave nothing, the usual ones, pay some 5 us
-    // for three empty launches (25.4 against 30.2 with top-p 0.9 of a peaked row, 21.9 against 26.3 with k = 20).
+    // Nothing is left to further kernels up to 32768 logits to a row.  Three empty launches cost the calls that leave nothing, the usual
+    // ones, some 4.5 us at any size; what a flat row gains grows with its length.  us a call in a graph, 5 rows of bf16, rows left / each by
+    // its own block: k = 20 32000 18.3 / 13.8, 50257 19.1 / 14.5, 128000 18.3 / 13.7; top-p 0.9 of a peaked row (t 0.5) 23.1 / 18.7, 25.7 / 19.5,
+    // 25.7 / 21.5; top-p 0.95 of a flat one (t 1.5) 20000 43.1 / 43.8, 32000 39.2 / 55.9, 50257 42.4 / 76.4, 65536 42.3 / 87, 128000 49.8 / 151.
+    // 320 such flat rows: 32000 98 / 88, 65536 143 / 149, 128000 205 / 265.
     a.max_left = a.n_vocab <= 32768 ? 0 : std::min(a.n_rows, fka::kSampleMaxLeft);
     a.shares = std::max(1, std::min((int32_t)tiles, kShares / std::max(1, a.max_left)));
     const size_t shares = std::min<size_t>(kShares, a.max_left * tiles);  // at least max_left x a.shares

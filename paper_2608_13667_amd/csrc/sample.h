@@ -17,15 +17,20 @@
 //   * where it has not, the row is left to three more kernels, in which many blocks share it: a histogram of the weights by
 //     (M - l) / t; the bin where their sum passes p, whose logits are listed, and the sums of each tile's logits above it; the draw.
 //     So are rows of which more than 256 groups have to be read, for the list or, with min-p alone, the draw;
-//   * where a list does not fit (thousands of equal logits, a k of some 2000 or more), the block goes over the row by itself: the threshold
-//     digit by digit of the logit's bits (11, 11, 10 from the top, as unsigned numbers in the logits' order), a histogram of each
-//     digit's values among what agrees in the digits before.
+//   * where a list does not do, the block goes over the row by itself: the threshold digit by digit of the logit's bits (11, 11, 10 from the
+//     top, as unsigned numbers in the logits' order), a histogram of each digit's values among what agrees in the digits before.  That
+//     is slow, by one logit to a load, and happens
+//       - with thousands of equal logits, or a k of some 2000 or more;
+//       - with a k of up to half of the groups that is more than the groups with a logit above -inf: masked rows (5 rows of 128000 fp32 with 30 such logits,
+//         us a call: k = 50 377, k = 20 18.3, no k 16.3; of 32000 107, 13.7, 11.7);
+//       - with top-p alone, where one bin of the histogram, 1/32 of a temperature wide, has more than 2048 logits, as wide rows have at high temperatures
+//         (5 rows of N(0, 2.5), top-p 0.95: 262144 fp32 t 1 51, t 1.6 635, t 3 818; 200003 t 2 49.5, t 3 566; 128000 t 3 46).
 //
 // One block to a row for all of it, by digits from memory, took 64 us for 5 rows of 32000 bf16, 556 for 320 of 128000 fp32 (a quarter of them
 // top-p alone) and 111 for 80 of 200003 bf16, nothing filtered.  Now 20 to 32 (a row with k = 1000 is the
-// slowest of such a call), 102 and 23.2.  The scan is bound by memory (164 MB in 28 us, 5.9 TB/s) or, with sums, by fp64 exponentials (16 million
-// in 18 us); the row kernel by latency, some twenty steps between barriers (7 us where nothing is filtered, 14 with k = 50 and p,
-// 20 over 320 rows); the three kernels behind it by their start, their loads and the list's (12, 23 and 17).
+// slowest of such a call), 102 and 23.2.  The scan is bound by memory (164 MB in 28 us, 5.9 TB/s) or, with sums, by vector instructions (16 million
+// fp64 exponentials in 18 us: 31 instructions a logit, a third of them fp64, issue in 12.7 of these); the row kernel by latency, some twenty steps
+// between barriers (7 us where nothing is filtered, 14 with k = 50 and p, 20 over 320 rows); the three kernels behind it by their start, their loads and the list's (12, 23 and 17).
 #pragma once
 
 #include <type_traits>
