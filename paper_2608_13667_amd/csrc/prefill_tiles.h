@@ -1140,35 +1140,47 @@ __device__ INLINE inline void prefill_tiles(const Args &a)
             const int b_z = (min(u * 32 + 32, rows_head) - 1) / a.split.branch_rows;
             for (int b = (u * 32) / a.split.branch_rows; b <= b_z; ++b) {
                 const int L = min(max(scalar_load(a.suffix_len + b), 0), a.max_suffix_len - n);
-                for (int k = 0; k < L + n; ++k) {
-                    size_t off = ((size_t)b * Hkv + g) * a.suffix_cap + k;
+                for (int k0 = 0; k0 < L + n; k0 += GRP) {  // eight keys at a time, which are in one page
+                    size_t off = ((size_t)b * Hkv + g) * a.suffix_cap + k0;
                     if constexpr (PAGED) {
-                        const int i = (Lp + kPageSize - 1) / kPageSize + k / kPageSize;
+                        const int i = (Lp + kPageSize - 1) / kPageSize + k0 / kPageSize;
                         const int32_t page = scalar_load(a.page_table + (size_t)b * a.max_pages + min(i, a.max_pages - 1));
                         if (page < 0 || page >= a.n_pool_pages) continue;
-                        off = ((size_t)page * Hkv + g) * kPageSize + k % kPageSize;
+                        off = ((size_t)page * Hkv + g) * kPageSize + k0 % kPageSize;
                     }
-                    const uint16_t *row = reinterpret_cast<const uint16_t *>(PAGED ? pv : reinterpret_cast<const char *>(a.suffix_v)) + off * HD;
-                    uint32_t seen = 0;  // bits 2 i of lane l: channel CL l + i is +inf, -inf
+                    const uint16_t *rows = reinterpret_cast<const uint16_t *>(PAGED ? pv : reinterpret_cast<const char *>(a.suffix_v)) + off * HD;
+                    const int keys = min(GRP, L + n - k0);
+                    auto infs = [&](int k) INLINE {  // bits 2 i of lane l: channel CL l + i of key k is +inf, -inf
+                        uint32_t seen = 0;
 #pragma unroll
-                    for (int i = 0; i < CL; ++i) {
-                        const uint32_t x = row[CL * lane_c + i];
-                        seen |= (x == 0x7f80u ? 1u : x == 0xff80u ? 2u : 0u) << (2 * i);
-                    }
-                    if (__builtin_amdgcn_ballot_w64(seen != 0) == 0) continue;
-                    bool reads[2];
-#pragma unroll
-                    for (int t = 0; t < 2; ++t) reads[t] = row_bt[t] >> 16 == b && (k < L || (row_mask[t] >> (k - L) & 1) != 0);
-#pragma unroll
-                    for (int e = 0; e < NE; ++e)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int c = 16 * e + 4 * q4c + j;
-                            const uint32_t f = (uint32_t)__shfl((int)seen, c / CL) >> (2 * (c % CL)) & 3u;
-#pragma unroll
-                            for (int t = 0; t < 2; ++t)
-                                if (reads[t] && f) acc[t][e][j] += f == 1 ? INFINITY : -INFINITY;
+                        for (int i = 0; i < CL; ++i) {
+                            const uint32_t x = rows[(size_t)k * HD + CL * lane_c + i];
+                            seen |= (x == 0x7f80u ? 1u : x == 0xff80u ? 2u : 0u) << (2 * i);
                         }
+                        return seen;
+                    };
+                    uint32_t any = 0;
+#pragma unroll
+                    for (int k = 0; k < GRP; ++k) any |= infs(min(k, keys - 1));
+                    if (__builtin_amdgcn_ballot_w64(any != 0) == 0) continue;
+#pragma unroll 1
+                    for (int k = 0; k < keys; ++k) {
+                        const uint32_t seen = infs(k);
+                        const int node = k0 + k - L;  // (committed keys: negative)
+                        bool reads[2];
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) reads[t] = row_bt[t] >> 16 == b && (node < 0 || (row_mask[t] >> (node & 63) & 1) != 0);
+#pragma unroll
+                        for (int e = 0; e < NE; ++e)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const int c = 16 * e + 4 * q4c + j;
+                                const uint32_t f = (uint32_t)__shfl((int)seen, c / CL) >> (2 * (c % CL)) & 3u;
+#pragma unroll
+                                for (int t = 0; t < 2; ++t)
+                                    if (reads[t] && f) acc[t][e][j] += f == 1 ? INFINITY : -INFINITY;
+                            }
+                    }
                 }
             }
         }
