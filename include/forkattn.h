@@ -443,8 +443,8 @@ fka_status fka_plan_create_tree_paged(const fka_heads *heads, const fka_prefill_
  * A key's weight enters the product with V to 2^-27 of it in calls of few rows, or of few keys for their rows, and to 2^-18 in the others: many rows
  * over thousands of keys, where a result is off by some 2.5e-6 of the largest.
  * A key that no bit shows has no influence on a row, whatever it holds.  An infinite value of V, in the prefix, a suffix or a node, is that
- * infinity in its channel of the rows that read its key (both signs: NaN).  A NaN of the prefix's V stays in its channel, one of a suffix or node's makes
- * the rows that read its key NaN.
+ * infinity in its channel of the rows that read its key; NaN where both signs meet, and, possibly, where the keys around it have less than 2^-126 of the row's weight.  A
+ * NaN of the prefix's V stays in its channel, one of a suffix or node's makes the rows that read its key NaN.
  * out and out_lse may overlap neither each other nor the caches, page_table, suffix_len or masks (FKA_ERR_INVALID_ARG); q may be theirs.
  */
 fka_status fka_tree_attend(const fka_plan *plan, const void *q, const void *prefix_k, const void *prefix_v, const void *suffix_k,
